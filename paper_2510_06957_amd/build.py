@@ -22,7 +22,8 @@ CSRC = HERE / "csrc"
 LIB = HERE / "libtstgemm.so"
 LAUNCH = HERE / ("_launch" + sysconfig.get_config_var("EXT_SUFFIX"))   # of this Python; the torch it is for is in the module
 SOURCES = ["tcsc_host.cpp", "reblock.hip", "tstgemm_side.hip", "tstgemm_large.hip", "tstgemm_small.hip", "tstgemm_matrix.hip",
-           "tstgemm_decode.hip", "tstgemm_packed.hip", "probes.hip", "tstgemm_noalloc.hip"]
+           "tstgemm_decode.hip", "tstgemm_packed.hip", "probes.hip", "tstgemm_noalloc.hip",
+           "w8_gemm.hip", "moe.hip", "logprobs.hip"]
 ARCH = "gfx950"
 
 

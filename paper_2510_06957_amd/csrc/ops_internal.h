@@ -1,0 +1,58 @@
+// Internal declarations shared by the operators around the ternary product (tst_ops.h).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "tst_ops.h"
+
+namespace tst {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Geometry of packed 8-bit weights (tst_w8_pack): pieces of 16 columns x 64 rows.
+constexpr int kW8Cols = 16, kW8Rows = 64, kW8Piece = kW8Cols * kW8Rows;
+inline __host__ __device__ int blocks_of(int n, int size) { return (n + size - 1) / size; }
+inline size_t w8_bytes(int K, int N) { return (size_t)blocks_of(K, kW8Rows) * blocks_of(N, kW8Cols) * kW8Piece; }
+constexpr int kW8MaxK = 131071;   // 131072 * (-128 * -128) = 2^31
+
+inline bool type_ok(int type) { return type == TST_F32 || type == TST_BF16 || type == TST_F16; }
+inline size_t type_bytes(int type) { return type == TST_F32 ? 4 : 2; }
+inline bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// An entry of a type: bf16 and fp16 held as their 16 bits.
+template <int TYPE> struct Entry;
+template <> struct Entry<TST_F32> {
+    typedef float bits;
+    static __device__ __forceinline__ float get(bits b) { return b; }
+    static __device__ __forceinline__ bits put(float v) { return v; }
+};
+template <> struct Entry<TST_BF16> {
+    typedef uint16_t bits;
+    static __device__ __forceinline__ float get(bits b) { return __uint_as_float((unsigned)b << 16); }
+    static __device__ __forceinline__ bits put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }   // to nearest, ties to even
+};
+template <> struct Entry<TST_F16> {
+    typedef uint16_t bits;
+    static __device__ __forceinline__ float get(bits b) { return (float)__builtin_bit_cast(_Float16, b); }
+    static __device__ __forceinline__ bits put(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+};
+
+inline int status(hipError_t e) { return e == hipSuccess ? TSTGEMM_OK : TSTGEMM_EHIP; }
+
+// call(std::integral_constant<int, type>) for a run-time type
+template <typename F> inline hipError_t for_type(int type, F call)
+{
+    switch (type) {
+    case TST_F32: return call(std::integral_constant<int, TST_F32>{});
+    case TST_BF16: return call(std::integral_constant<int, TST_BF16>{});
+    default: return call(std::integral_constant<int, TST_F16>{});
+    }
+}
+
+}  // namespace tst
