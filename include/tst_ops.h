@@ -52,10 +52,10 @@ int tst_w8_pack(const int8_t *W, int count, int K, int N, void *packed, void *st
 /*
  * Y[m][n] = fl(sum_k Q[m][k] W[k][n]) * scale[m] * w_scale[n] + b[n]: the sum in int32, exact, rounded to fp32 once, then two products
  * and the bias in fp32, rounded to y_type once.
- * Q: DEVICE, M rows of K codes, q_stride bytes apart; Q 16-byte aligned and q_stride a multiple of 16 (or M = 1).  What lies between
- * K and the next 16-byte border of a row is read and does not matter; nothing behind that border is read.
+ * Q: DEVICE, M rows of K codes, q_stride bytes apart; Q 16-byte aligned and q_stride a multiple of 16, at most 4 MiB (or M = 1).
+ * What lies between K and the next 16-byte border of a row is read and does not matter; nothing behind that border is read.
  * scale: DEVICE, M.  packed: DEVICE, tst_w8_pack() of W.  w_scale: DEVICE, N.  b: DEVICE, N, or NULL.  Y: DEVICE, M x N of y_type,
- * row-major, aligned to its type.  M >= 0.  Errors: EINVAL, EHIP.
+ * row-major, aligned to its type.  0 <= M <= 1048560.  Errors: EINVAL, EHIP.
  */
 int tst_w8_gemm(const int8_t *Q, int64_t q_stride, const float *scale, const void *packed, const float *w_scale, const float *b,
                 void *Y, int y_type, int M, int K, int N, void *stream);

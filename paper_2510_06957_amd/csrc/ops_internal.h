@@ -43,6 +43,8 @@ template <> struct Entry<TST_F16> {
     static __device__ __forceinline__ bits put(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };
 
+int compute_units();   // (tstgemm_side.hip)
+
 inline int status(hipError_t e) { return e == hipSuccess ? TSTGEMM_OK : TSTGEMM_EHIP; }
 
 // call(std::integral_constant<int, type>) for a run-time type

@@ -8,7 +8,8 @@ namespace {
 // ------------------------------------------------------------------------------------------------------------------
 // k_quantize: one workgroup per row; the row's largest magnitude, then its codes.  Magnitudes are compared as integers: of
 // non-negative floats the bits order as the values do, with infinity and NaN above every number.
-constexpr int kQuantThreads = 256;
+// The row stays in the registers on the way if it fits (kQuantPieces pieces of 16 bytes for a thread), else it is read twice.
+constexpr int kQuantThreads = 256, kQuantPieces = 4;
 
 __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
@@ -17,27 +18,82 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
     return v;
 }
 
-template <int TYPE>
+// What a row's codes are made with, from the bits of its largest magnitude.
+struct Scaling {
+    bool finite;
+    float factor, scale;
+    __device__ explicit Scaling(unsigned most)
+    {
+        finite = most < 0x7f800000u;
+        const float a = __uint_as_float(most);
+        factor = fminf(127.f / a, 3.402823466e38f);   // a = 0: 0 * FLT_MAX = 0
+        scale = finite ? a / 127.f : __uint_as_float(0x7fc00000u);
+    }
+    __device__ __forceinline__ unsigned code(float x) const { return finite ? (unsigned)(int)rintf(x * factor) & 0xffu : 0u; }
+};
+
+// WIDE: rows of X on 16-byte borders, rows of Q on borders of a piece's codes
+template <int TYPE, bool WIDE>
 __global__ void __launch_bounds__(kQuantThreads)
 k_quantize(const typename Entry<TYPE>::bits *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int K)
 {
     typedef Entry<TYPE> E;
+    typedef typename E::bits bits;
+    constexpr int V = 16 / sizeof(bits);
+    typedef bits piece __attribute__((ext_vector_type(V)));
     __shared__ unsigned most[kQuantThreads / 64];
     const int64_t m = blockIdx.x;
-    const typename E::bits *x = X + m * x_stride;
+    const bits *x = X + m * x_stride;
+    int8_t *q = Q + m * q_stride;
+    piece v[kQuantPieces];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int p = 0; p < kQuantPieces; ++p) {
+            const int k = k0 + (p * kQuantThreads + threadIdx.x) * V;
+            v[p] = piece{};
+            if (WIDE && k + V <= K) {
+                v[p] = *reinterpret_cast<const piece *>(x + k);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (k + i < K) v[p][i] = x[k + i];
+            }
+        }
+    };
+    constexpr int kRound = kQuantPieces * kQuantThreads * V;
     unsigned a = 0;
-    for (int k = threadIdx.x; k < K; k += kQuantThreads) a = max(a, __float_as_uint(E::get(x[k])) & 0x7fffffffu);
+    for (int k0 = 0; k0 < K; k0 += kRound) {
+        load(k0);
+#pragma unroll
+        for (int p = 0; p < kQuantPieces; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) a = max(a, __float_as_uint(E::get(v[p][i])) & 0x7fffffffu);
+    }
     a = wave_max(a);
     if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = a;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kQuantThreads / 64; ++w) a = max(a, most[w]);
-    const bool finite = a < 0x7f800000u;
-    const float f = __uint_as_float(a);
-    const float r = fminf(127.f / f, 3.402823466e38f);   // a = 0: 0 * FLT_MAX = 0
-    if (threadIdx.x == 0) scale[m] = finite ? f / 127.f : __uint_as_float(0x7fc00000u);
-    int8_t *q = Q + m * q_stride;
-    for (int k = threadIdx.x; k < K; k += kQuantThreads) q[k] = finite ? (int8_t)(int)rintf(E::get(x[k]) * r) : (int8_t)0;
+    const Scaling by(a);
+    if (threadIdx.x == 0) scale[m] = by.scale;
+    for (int k0 = 0; k0 < K; k0 += kRound) {
+        if (K > kRound) load(k0);
+#pragma unroll
+        for (int p = 0; p < kQuantPieces; ++p) {
+            const int k = k0 + (p * kQuantThreads + threadIdx.x) * V;
+            unsigned out[V / 4] = {};
+#pragma unroll
+            for (int i = 0; i < V; ++i) out[i / 4] |= by.code(E::get(v[p][i])) << (8 * (i % 4));
+            if (WIDE && k + V <= K) {
+                if constexpr (V == 8) *reinterpret_cast<u32x2 *>(q + k) = u32x2{out[0], out[1]};
+                else *reinterpret_cast<unsigned *>(q + k) = out[0];
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (k + i < K) q[k + i] = (int8_t)(out[i / 4] >> (8 * (i % 4)));
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -70,76 +126,300 @@ struct GemmArgs {
     bool wide;   // four neighbouring results can be stored at once
 };
 
+// Four neighbouring results of row m from column n on.
 template <int TYPE>
-__device__ __forceinline__ void store4(const GemmArgs &a, int m, int n, i32x4 sum)
+__device__ __forceinline__ void store4(const GemmArgs &a, int m, int n, i32x4 sum, float s, const float (&t)[4], const float (&b)[4])
 {
     typedef Entry<TYPE> E;
     typedef typename E::bits bits;
     typedef bits bits4 __attribute__((ext_vector_type(4)));
-    if (m >= a.M) return;
-    const float s = a.scale[m];
     bits *y = static_cast<bits *>(a.Y) + (size_t)m * a.N + n;
     bits4 out;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = min(n + i, a.N - 1);
-        float v = (float)sum[i] * s * a.w_scale[c];
-        if (a.b) v += a.b[c];
-        out[i] = E::put(v);
-    }
-    if (a.wide && n + 4 <= a.N) {
-        *reinterpret_cast<bits4 *>(y) = out;
+    for (int r = 0; r < 4; ++r) out[r] = E::put((float)sum[r] * s * t[r] + b[r]);
+    if (a.wide) {   // N is a multiple of 4: all four or none
+        if (n < a.N) *reinterpret_cast<bits4 *>(y) = out;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < a.N) y[i] = out[i];
+        for (int r = 0; r < 4; ++r)
+            if (n + r < a.N) y[r] = out[r];
     }
 }
 
-constexpr int kRowsWaves = 8;
+constexpr int kBufferFlags = 0x00027000;       // untyped, out of bounds by the byte
+constexpr unsigned kOutside = 0x80000000u;     // of every buffer, also with the lane offsets that are added to it
 
-template <int TYPE, int MT>
-__global__ void __launch_bounds__(kRowsWaves * 64)
+// bytes from `at` on, both the same for all lanes (kept in scalar registers)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *at, unsigned bytes)
+{
+    const uint64_t p = reinterpret_cast<uint64_t>(at);
+    const uint64_t uniform = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)p);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(uniform), 0, __builtin_amdgcn_readfirstlane((int)bytes), kBufferFlags);
+}
+
+// 16 bytes; 0 where lane_offset lies outside the buffer (`offset`, the same for all lanes, never leads there)
+__device__ __forceinline__ i32x4 load16(__amdgpu_buffer_rsrc_t from, unsigned lane_offset, unsigned offset)
+{
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, offset, 0));
+}
+
+// 16 MT rows x 16 NT columns of Y for a workgroup; its wavefronts share K, 128 at a time, and add their sums in the LDS at the end.
+// W comes from memory straight into the registers (a piece of the packed form is an operand of the matrix instruction).  X goes through a
+// part of the LDS that belongs to the wavefront: an operand wants row l % 16 in lane l, and loads whose neighbouring lanes lie in different
+// rows take the address unit a cycle for each lane (64 x 16384 x 4096: 35 us in place of 18), so 8 lanes load 128 bytes of a row together.
+// Chunk c of 8 of a row stands in slot (row % 16) ^ c, which makes both the writes (8 chunks of a row together) and the reads (16 rows
+// of a chunk together) free of bank conflicts.
+constexpr int kRowsWaves = 8, kRowsThreads = kRowsWaves * 64, kStepK = 128;
+
+template <int TYPE, int MT, int NT>
+__global__ void __launch_bounds__(kRowsThreads, 2)
 k_w8_rows(const GemmArgs a)
 {
-    __shared__ i32x4 part[kRowsWaves][MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int nb = blockIdx.x, m0 = blockIdx.y * 16 * MT;
-    const int k_blocks = blocks_of(a.K, kW8Rows);
-    const char *w = a.packed + (size_t)nb * k_blocks * kW8Piece + lane * 16;
-    const int8_t *x[MT];
+    constexpr int kPieces = 2 * MT;   // 16-byte pieces of X for a lane and step
+    constexpr int kStage = 16 * MT * 8, kPart = MT * NT * 64;   // 16 bytes each, for a wavefront
+    __shared__ i32x4 lds[kRowsWaves * (kStage > kPart ? kStage : kPart)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nb0 = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT;
+    const int k_blocks = blocks_of(a.K, kW8Rows), steps = (k_blocks + 1) / 2, n_blocks = blocks_of(a.N, kW8Cols);
+    const unsigned column = k_blocks * kW8Piece, q_stride = (unsigned)a.q_stride;
+    const auto w = buffer(a.packed + (size_t)nb0 * column, min(NT, n_blocks - nb0) * column);
+    const auto x = buffer(a.Q + m0 * a.q_stride, (min(16 * MT, a.M - m0) - 1) * q_stride + ((a.K + 15) & ~15));
+    const int c = lane & 7, r0 = lane >> 3;   // a lane's pieces: chunk c of rows r0, r0 + 8, ...
+    i32x4 *const stage = lds + wave * kStage;
+    i32x4 acc[MT][NT] = {}, xr[kPieces], wr[2][NT], wn[2][NT];
+    auto load_x = [&](int step) {
+        const unsigned k = step * kStepK + c * 16, at = k < (unsigned)a.K ? r0 * q_stride + k : kOutside;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = a.Q + (int64_t)min(m0 + 16 * t + (lane & 15), a.M - 1) * a.q_stride;
-    i32x4 acc[MT] = {};
-    for (int kb = wave; kb < k_blocks; kb += kRowsWaves) {
-        const i32x4 wf = *reinterpret_cast<const i32x4 *>(w + (size_t)kb * kW8Piece);
-        const int k = kb * kW8Rows + 16 * (lane >> 4);
+        for (int p = 0; p < kPieces; ++p) xr[p] = load16(x, at + p * 8 * q_stride, 0);
+    };
+    auto load_w = [&](int step, i32x4 (&to)[2][NT]) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            i32x4 xf = {};
-            if (k < a.K) xf = *reinterpret_cast<const i32x4 *>(x[t] + k);   // what lies behind K meets weights of 0
-            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf, xf, acc[t], 0, 0, 0);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) to[s][j] = load16(w, min(2 * step + s, k_blocks - 1) * kW8Piece + j * column + lane * 16, 0);
+    };
+    auto store_x = [&]() {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int row = p * 8 + r0;
+            stage[((row >> 4) * 8 + c) * 16 + ((row & 15) ^ c)] = xr[p];
+        }
+    };
+    auto order = [&]() {   // of the wavefront's own stores and reads; the LDS takes them in this order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+    };
+    load_x(wave);
+    load_w(wave, wr);
+    for (int step = wave; step < steps; step += kRowsWaves) {
+        store_x();
+        order();
+        load_x(step + kRowsWaves);   // behind the last step: X reads as 0
+        load_w(step + kRowsWaves, wn);
+        __builtin_amdgcn_sched_barrier(0);   // or the compiler moves the loads to where they are used
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const int chunk = 4 * s + (lane >> 4);
+                const i32x4 xf = stage[(t * 8 + chunk) * 16 + ((lane & 15) ^ chunk)];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[t][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[s][j], xf, acc[t][j], 0, 0, 0);
+            }
+        order();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) wr[s][j] = wn[s][j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) lds[(wave * MT * NT + t * NT + j) * 64 + lane] = acc[t][j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < MT * NT * 64; i += kRowsThreads) {
+        const int l = i & 63, t = (i >> 6) / NT, j = (i >> 6) % NT;
+        i32x4 sum = lds[i];
+#pragma unroll
+        for (int v = 1; v < kRowsWaves; ++v) sum += lds[v * kPart + i];
+        const int m = m0 + 16 * t + (l & 15), n = (nb0 + j) * kW8Cols + 4 * (l >> 4);
+        float ws[4], b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            ws[r] = a.w_scale[min(n + r, a.N - 1)];
+            b[r] = a.b ? a.b[min(n + r, a.N - 1)] : 0.f;
+        }
+        if (m < a.M) store4<TYPE>(a, m, n, sum, a.scale[m], ws, b);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// k_w8_tiles: 256 columns x 16 MF rows of Y for a workgroup of four wavefronts, 64 columns x all its rows each.  What a wavefront
+// takes of W nobody else in the workgroup needs, so it goes from memory straight into the registers (a piece of the packed form is an
+// operand of the matrix instruction); X goes through the LDS, 128 of K at a time in two buffers, in slots as in k_w8_rows.
+constexpr int kTileThreads = 256, kTileCols = 256;
+
+template <int TYPE, int MF>
+__global__ void __launch_bounds__(kTileThreads, 2)
+k_w8_tiles(const GemmArgs a, int m_tiles, int n_tiles)
+{
+    constexpr int kRows = 16 * MF, kPieces = MF / 2;   // 16-byte pieces of X for a thread and step
+    __shared__ i32x4 xs[2][kRows * 8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // tiles that follow one another share rows or columns and run on one XCD (workgroups go to the eight XCDs in turn)
+    const int total = m_tiles * n_tiles, per = total / 8, id = blockIdx.x;
+    const int tile = id < per * 8 ? (id % 8) * per + id / 8 : id;
+    constexpr int kGroup = 32 / MF;   // row tiles that go through the columns together: 512 rows
+    const int group = tile / (kGroup * n_tiles), rest = tile % (kGroup * n_tiles);
+    const int height = min(kGroup, m_tiles - group * kGroup);
+    const int m0 = __builtin_amdgcn_readfirstlane((group * kGroup + rest % height) * kRows);
+    const int nb0 = __builtin_amdgcn_readfirstlane(rest / height * (kTileCols / 16) + wave * 4);
+
+    // Rows behind M, and chunks of X behind K, read as 0 by the hardware's bounds; what of W has no counterpart there does not matter, and
+    // is read from the last block or column that there is.
+    const int k_blocks = blocks_of(a.K, kW8Rows), n_blocks = blocks_of(a.N, kW8Cols), steps = (k_blocks + 1) / 2;
+    const unsigned column = k_blocks * kW8Piece, q_stride = (unsigned)a.q_stride;   // (launch_gemm() sees to it that offsets fit)
+    const int first = min(nb0, n_blocks - 1), more = min(3, n_blocks - 1 - first);
+    const auto w = buffer(a.packed + (size_t)first * column, (more + 1) * column);
+    const auto x = buffer(a.Q + m0 * a.q_stride, (min(kRows, a.M - m0) - 1) * q_stride + ((a.K + 15) & ~15));
+    const int c = threadIdx.x & 7, r0 = threadIdx.x >> 3;   // a thread's pieces: chunk c of rows r0, r0 + 32, ...
+    const unsigned x_at = r0 * q_stride + c * 16;
+    const int slot = ((r0 >> 4) * 8 + c) * 16 + ((r0 & 15) ^ c);
+    i32x4 xr[kPieces], w0[2][4], w1[2][4], acc[4][MF] = {};
+    auto load_x = [&](int step) {
+        const unsigned at = step * kStepK + c * 16 < a.K ? x_at + step * kStepK : kOutside;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) xr[p] = load16(x, at + p * 32 * q_stride, 0);
+    };
+    auto store_x = [&](int step) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) xs[step & 1][slot + p * 256] = xr[p];
+    };
+    auto load_w = [&](int step, int s, i32x4 (&to)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[j] = load16(w, lane * 16, min(j, more) * column + min(2 * step + s, k_blocks - 1) * kW8Piece);
+    };
+    auto meet = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    // One step.  As soon as a half of its W has been multiplied, the same registers are loaded for the step after the next.  X of
+    // the next step, requested a step ago, goes into the other buffer, which was read in the step before; everybody has met since.
+    auto compute = [&](int step, i32x4 (&wr)[2][4]) {
+        const i32x4 *const from = xs[step & 1];
+#pragma unroll
+        for (int q = 0; q < 2 * MF; ++q) {
+            const int s = q / MF, i = q % MF, chunk = 4 * s + (lane >> 4);
+            const i32x4 xf = from[(i * 8 + chunk) * 16 + ((lane & 15) ^ chunk)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[s][j], xf, acc[j][i], 0, 0, 0);
+            if (q == MF - 1) {
+                load_w(step + 2, 0, wr[0]);
+                store_x(step + 1);
+                load_x(step + 2);
+            }
+        }
+        load_w(step + 2, 1, wr[1]);
+        // the order of issue: reads of X three ahead of their products; loads and stores between the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+        for (int q = 0; q < 2 * MF; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            if (q >= MF && q < MF + kPieces) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            if (q >= MF && q < MF + 4) __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            if (q < 2 * MF - 3) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        meet();
+    };
+    load_x(0);
+    load_w(0, 0, w0[0]);
+    load_w(0, 1, w0[1]);
+    store_x(0);
+    load_x(1);
+    load_w(1, 0, w1[0]);
+    load_w(1, 1, w1[1]);
+    meet();
+    for (int step = 0;;) {   // (left, not skipped over: waits are counted along the paths there are)
+        compute(step, w0);
+        if (++step >= steps) break;
+        compute(step, w1);
+        if (++step >= steps) break;
+    }
+
+    float t[4][4], b[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int n = min((nb0 + j) * 16 + 4 * (lane >> 4) + r, a.N - 1);
+            t[j][r] = a.w_scale[n];
+            b[j][r] = a.b ? a.b[n] : 0.f;
+        }
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+        const int m = m0 + 16 * i + (lane & 15);
+        const float s = a.scale[min(m, a.M - 1)];
+        if (m < a.M) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store4<TYPE>(a, m, (nb0 + j) * 16 + 4 * (lane >> 4), acc[j][i], s, t[j], b[j]);
         }
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
-    __syncthreads();
-    for (int i = threadIdx.x; i < MT * 64; i += kRowsWaves * 64) {
-        const int t = i >> 6, l = i & 63;
-        i32x4 sum = part[0][t][l];
-#pragma unroll
-        for (int v = 1; v < kRowsWaves; ++v) sum += part[v][t][l];
-        store4<TYPE>(a, m0 + 16 * t + (l & 15), nb * kW8Cols + 4 * (l >> 4), sum);
+}
+
+// Which kernel and tile.  All of them are bound by what a compute unit can load (about 65 GB/s each, over all sizes measured), so the
+// choice is the one for which the busiest compute unit loads least: rounds of workgroups x bytes of a workgroup, and for k_w8_rows the
+// sums that its wavefronts exchange.  Measured with K = N = 4096 (us): 256 rows 11.8 with 64 x 64 tiles of k_w8_rows, 23 with k_w8_tiles<4>,
+// 31 with k_w8_tiles<8>; 512 rows 20 / 24 / 31; 1024 rows 36 / 24 / 32; 2048 rows 70 / 38 / 36; 4096 rows 61 with k_w8_tiles<8>, 72
+// with <4>.  64 x 16384 x 4096: 17.3 with 32 x 32 tiles of k_w8_rows, 18.3 with 64 x 16, 26 with 64 x 64.
+struct GemmTile {
+    bool rows;
+    int mt, nt;   // 16 mt rows x 16 nt columns
+};
+constexpr GemmTile kGemmTiles[] = {{true, 1, 1}, {true, 1, 2}, {true, 2, 2}, {true, 4, 2}, {true, 4, 4}, {false, 4, 16}, {false, 8, 16}};
+
+GemmTile choose_tile(int M, int K, int N)
+{
+    const double compute_units = tst::compute_units(), steps = blocks_of(K, kStepK);
+    GemmTile best = kGemmTiles[0];
+    double least = 1e300;
+    for (const GemmTile &t : kGemmTiles) {
+        const double groups = (double)blocks_of(M, 16 * t.mt) * blocks_of(N, 16 * t.nt);
+        const double rounds = groups > compute_units ? (double)(int64_t)((groups + compute_units - 1) / compute_units) : 1;
+        const double x_rows = M < 16 * t.mt ? M : 16 * t.mt;
+        const double bytes = rounds * (steps * kStepK * (x_rows + 16 * t.nt) + (t.rows ? 20e3 + 6e3 * t.mt * t.nt : 0));
+        if (bytes < least) {
+            least = bytes;
+            best = t;
+        }
     }
+    return best;
 }
 
 hipError_t launch_gemm(const GemmArgs &a, int y_type, hipStream_t stream)
 {
+    const GemmTile tile = choose_tile(a.M, a.K, a.N);
+    const int m = blocks_of(a.M, 16 * tile.mt), n = blocks_of(a.N, 16 * tile.nt);
     return for_type(y_type, [&](auto type) {
         constexpr int T = decltype(type)::value;
-        const unsigned cols = blocks_of(a.N, kW8Cols);
-        if (a.M <= 16) k_w8_rows<T, 1><<<dim3(cols, 1), kRowsWaves * 64, 0, stream>>>(a);
-        else k_w8_rows<T, 4><<<dim3(cols, blocks_of(a.M, 64)), kRowsWaves * 64, 0, stream>>>(a);
+        const dim3 grid(n, m);
+        if (!tile.rows) {
+            if (tile.mt == 4) k_w8_tiles<T, 4><<<m * n, kTileThreads, 0, stream>>>(a, m, n);
+            else k_w8_tiles<T, 8><<<m * n, kTileThreads, 0, stream>>>(a, m, n);
+        } else if (tile.nt == 1) {
+            k_w8_rows<T, 1, 1><<<grid, kRowsThreads, 0, stream>>>(a);
+        } else if (tile.nt == 4) {
+            k_w8_rows<T, 4, 4><<<grid, kRowsThreads, 0, stream>>>(a);
+        } else if (tile.mt == 1) {
+            k_w8_rows<T, 1, 2><<<grid, kRowsThreads, 0, stream>>>(a);
+        } else if (tile.mt == 2) {
+            k_w8_rows<T, 2, 2><<<grid, kRowsThreads, 0, stream>>>(a);
+        } else {
+            k_w8_rows<T, 4, 2><<<grid, kRowsThreads, 0, stream>>>(a);
+        }
         return hipGetLastError();
     });
 }
@@ -149,13 +429,16 @@ hipError_t launch_quantize(const void *X, int type, int64_t x_stride, int8_t *Q,
 {
     return for_type(type, [&](auto t) {
         typedef typename Entry<decltype(t)::value>::bits bits;
-        k_quantize<decltype(t)::value><<<M, kQuantThreads, 0, stream>>>(static_cast<const bits *>(X), x_stride, Q, q_stride, scale, K);
+        constexpr int T = decltype(t)::value, V = 16 / sizeof(bits);
+        const bool wide = aligned(X, 16) && x_stride % V == 0 && aligned(Q, V) && q_stride % V == 0;
+        if (wide) k_quantize<T, true><<<M, kQuantThreads, 0, stream>>>(static_cast<const bits *>(X), x_stride, Q, q_stride, scale, K);
+        else k_quantize<T, false><<<M, kQuantThreads, 0, stream>>>(static_cast<const bits *>(X), x_stride, Q, q_stride, scale, K);
         return hipGetLastError();
     });
 }
 
-// the most rows of 64 that a grid's second dimension holds
-constexpr int kMaxRows = 65535 * 64;
+// the most rows that a grid's second dimension holds with the smallest tile, and bytes between rows whose offsets in a tile fit 31 bits
+constexpr int kMaxRows = 65535 * 16, kMaxStride = 1 << 22;
 
 int check_gemm(const void *X, const void *packed, const float *w_scale, const void *Y, int type, int M, int K, int N)
 {
@@ -206,7 +489,8 @@ int tst_w8_gemm(const int8_t *Q, int64_t q_stride, const float *scale, const voi
 {
     if (int rc = tst::check_gemm(Q, packed, w_scale, Y, y_type, M, K, N)) return rc;
     if (M == 0) return TSTGEMM_OK;
-    if (!scale || !tst::aligned(Q, 16) || (M > 1 && (q_stride < K || q_stride % 16))) return TSTGEMM_EINVAL;
+    if (!scale || !tst::aligned(Q, 16) || (M > 1 && (q_stride < K || q_stride % 16 || q_stride > tst::kMaxStride))) return TSTGEMM_EINVAL;
+    if (M == 1) q_stride = 0;
     return tst::status(tst::launch_gemm(tst::gemm_args(Q, q_stride, scale, packed, w_scale, b, Y, y_type, M, K, N), y_type,
                                         static_cast<hipStream_t>(stream)));
 }
