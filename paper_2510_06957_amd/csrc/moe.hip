@@ -15,6 +15,9 @@ namespace {
 constexpr int kMaxTokens = 64;   // of one launch; more go in slabs
 constexpr int kMaxE = TST_MOE_MAX_EXPERTS, kMaxTop = TST_MOE_MAX_TOP;
 
+// Activations as operands: for each 64 rows of a product and plane two operands of the matrix instruction, in each 16 bytes for a quarter of
+// the rows and a token, [block][plane][half][quarter][token][8 bf16], the row being 64 block + 16 quarter + 8 half + i, as in the pieces
+// of the weights.  Neighbouring lanes read neighbouring tokens.
 struct MoeArgs {
     const void *X;
     int64_t x_stride;
@@ -25,11 +28,11 @@ struct MoeArgs {
     int32_t *ids;
     float *p;
     int E, D, F, T, top;
-    bool normalize;
+    bool normalize, wide;   // wide: rows of X and of the router can be loaded 16 bytes at a time
     // workspace
-    float *logits;      // [T][E]
-    uint16_t *x;        // [planes][T][D_pad] bf16, zero behind D
-    uint16_t *h;        // [h planes][T * top][F_pad] bf16, zero behind F
+    float *logits;   // [T][E]
+    u32x4 *x;        // operands of X, zero behind D
+    u32x4 *h;        // operands of h, a row for each token and expert it chose, zero behind F
 };
 
 constexpr int planes_of(int type) { return type == TST_F32 ? 3 : type == TST_F16 ? 2 : 1; }
@@ -52,42 +55,68 @@ __device__ __forceinline__ float wave_sum(float v)
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// k_moe_router: a wavefront per (token, expert) for the logits, and the planes of X.
+// k_moe_router: a wavefront per (token, expert) for the logits, and the operands of X.
 constexpr int kRouterWaves = 4;
 
-template <int TYPE>
+template <int TYPE, bool WIDE>
 __global__ void __launch_bounds__(kRouterWaves * 64)
 k_moe_router(const MoeArgs a)
 {
     typedef Entry<TYPE> E;
     typedef typename E::bits bits;
+    constexpr int V = WIDE ? 16 / sizeof(bits) : 1;
+    typedef bits piece __attribute__((ext_vector_type(V)));
     const int t = blockIdx.y, lane = threadIdx.x & 63, e = blockIdx.x * kRouterWaves + (threadIdx.x >> 6);
     const bits *x = static_cast<const bits *>(a.X) + t * a.x_stride;
     if (e < a.E) {
         const bits *r = static_cast<const bits *>(a.router) + (size_t)e * a.D;
         float sum = 0.f;
-        for (int d = lane; d < a.D; d += 64) sum = fmaf(E::get(x[d]), E::get(r[d]), sum);
+#pragma unroll 8
+        for (int d = lane * V; d < a.D; d += 64 * V) {   // (WIDE: D is a multiple of V)
+            const piece xv = *reinterpret_cast<const piece *>(x + d), rv = *reinterpret_cast<const piece *>(r + d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum = fmaf(E::get(xv[i]), E::get(rv[i]), sum);
+        }
         sum = wave_sum(sum);
         if (lane == 0) a.logits[t * a.E + e] = sum;
     }
-    const int d_pad = pad64(a.D);
-    for (int d = blockIdx.x * kRouterWaves * 64 + threadIdx.x; d < d_pad; d += gridDim.x * kRouterWaves * 64) {
-        float v = d < a.D ? E::get(x[d]) : 0.f;
+    constexpr int P = planes_of(TYPE);
+    for (int unit = blockIdx.x * kRouterWaves * 64 + threadIdx.x; unit < pad64(a.D) / 8; unit += gridDim.x * kRouterWaves * 64) {
+        const int d = unit * 8, kb = unit >> 3, quarter = (unit >> 1) & 3, half = unit & 1;
+        uint16_t out[P][8];
 #pragma unroll
-        for (int p = 0; p < planes_of(TYPE); ++p) a.x[((size_t)p * a.T + t) * d_pad + d] = cut(v);
+        for (int i = 0; i < 8; ++i) {
+            float v = d + i < a.D ? E::get(x[d + i]) : 0.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p) out[p][i] = cut(v);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            u32x4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = out[p][2 * i] | (unsigned)out[p][2 * i + 1] << 16;
+            a.x[(size_t)(((kb * P + p) * 2 + half) * 4 + quarter) * a.T + t] = o;
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Which tokens chose which expert, in the LDS: place[e][t] = rank of expert e among token t's, or 255.
-struct Chosen {
-    uint8_t place[kMaxE][kMaxTokens];
-    float p[kMaxTokens][kMaxTop];
-    uint16_t active[kMaxE];   // experts that some token chose, ascending
-    int n_active;
+// Which tokens chose which expert, in the LDS behind the workgroup's own: place[e][t] = rank of expert e among token t's, or 255.
+template <int NT> struct Chosen {
+    static constexpr int kTokens = 16 * NT;
+    uint8_t *place;     // [E][kTokens]
+    float *p;           // [T][top]
+    uint16_t *active;   // experts that some token chose, ascending
+    __device__ Chosen(char *lds, const MoeArgs &a)
+        : place(reinterpret_cast<uint8_t *>(lds)), p(reinterpret_cast<float *>(lds + a.E * kTokens)),
+          active(reinterpret_cast<uint16_t *>(p + a.T * a.top))
+    {
+    }
+    static size_t bytes(const MoeArgs &a) { return (size_t)a.E * kTokens + (size_t)a.T * a.top * sizeof(float) + (size_t)a.E * sizeof(uint16_t); }
+    __device__ int of(int e, int token) const { return place[e * kTokens + token]; }
 };
 
-// Bits that order as logits do: NaN above everything, -0 as +0.
+// Bits that order as logits do: NaN above everything, -0 as +0; none is 0.
 __device__ __forceinline__ unsigned order_key(float v)
 {
     const unsigned u = __float_as_uint(v + 0.f);
@@ -95,95 +124,102 @@ __device__ __forceinline__ unsigned order_key(float v)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ unsigned long long wave_max64(unsigned long long v)
+// The largest of a wavefront's values, the same in all lanes: maxima of 2, 4, 8, 16 neighbours, of rows of 16 and of halves, in lane 63.
+__device__ __forceinline__ unsigned wave_max(unsigned v)
 {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const unsigned long long o = ((unsigned long long)(unsigned)__shfl_xor((int)(v >> 32), d) << 32) | (unsigned)__shfl_xor((int)v, d);
-        v = v > o ? v : o;
-    }
-    return v;
+    auto step = [&](auto control) { return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xf, 0xf, false)); };
+    v = step(std::integral_constant<int, 0x111>{});   // row_shr 1
+    v = step(std::integral_constant<int, 0x112>{});
+    v = step(std::integral_constant<int, 0x114>{});
+    v = step(std::integral_constant<int, 0x118>{});
+    v = step(std::integral_constant<int, 0x142>{});   // row_bcast 15
+    v = step(std::integral_constant<int, 0x143>{});   // row_bcast 31
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // A wavefront finds a token's experts: top rounds of the largest of what is left; lane l holds experts l, l + 64, ...
-__device__ void choose_experts(const MoeArgs &a, Chosen &c, int t, int lane, bool write)
+template <int PER, int NT>
+__device__ void choose_experts(const MoeArgs &a, const Chosen<NT> &c, int t, int lane, bool write)
 {
-    constexpr int kPer = kMaxE / 64;
-    float l[kPer];
-    unsigned long long key[kPer];   // logit, then the lower expert first; 0: none (left)
-    float most = -INFINITY;
+    float l[PER];
+    unsigned key[PER];   // 0: none (left)
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int e = lane + 64 * i;
         l[i] = e < a.E ? a.logits[t * a.E + e] : -INFINITY;
-        key[i] = e < a.E ? ((unsigned long long)order_key(l[i]) << 32) | (unsigned)(kMaxE - e) : 0ull;
+        key[i] = e < a.E ? order_key(l[i]) : 0;
     }
-    float all = 0.f, chosen = 0.f;
+    float most = 0.f, all = 0.f, chosen = 0.f, mine = 0.f;
     for (int j = 0; j < a.top; ++j) {
-        unsigned long long best = 0;
+        unsigned best = key[0];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) best = best > key[i] ? best : key[i];
-        best = wave_max64(best);
-        const int e = kMaxE - (int)(unsigned)best;
+        for (int i = 1; i < PER; ++i) best = max(best, key[i]);
+        best = wave_max(best);
+        int e = -1;   // the lowest that has it
         float value = 0.f;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (key[i] == best) {
-                key[i] = 0;
-                value = l[i];
+        for (int i = 0; i < PER; ++i) {
+            const unsigned long long have = __ballot(key[i] == best);
+            if (e < 0 && have) {
+                const int at = __builtin_ctzll(have);
+                e = at + 64 * i;
+                value = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(l[i]), at));
+                if (lane == at) key[i] = 0;
             }
-        value = __shfl(value, e & 63);
+        }
         if (j == 0) {
             most = value;
+            if (!a.normalize) {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (lane + 64 * i < a.E) all += expf(l[i] - most);
-            all = wave_sum(all);
+                for (int i = 0; i < PER; ++i)
+                    if (lane + 64 * i < a.E) all += expf(l[i] - most);
+                all = wave_sum(all);
+            }
         }
         const float w = expf(value - most);
         chosen += w;
+        if (lane == j) mine = w;
         if (lane == 0) {
-            c.place[e][t] = (uint8_t)j;
-            c.p[t][j] = w;
+            c.place[e * c.kTokens + t] = (uint8_t)j;
             if (write) a.ids[t * a.top + j] = e;
         }
     }
-    const float total = a.normalize ? chosen : all;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // lane 0 wrote what the others read
     if (lane < a.top) {
-        const float p = c.p[t][lane] / total;
-        c.p[t][lane] = p;
+        const float p = mine / (a.normalize ? chosen : all);
+        c.p[t * a.top + lane] = p;
         if (write) a.p[t * a.top + lane] = p;
     }
 }
 
-// place[][] from the experts of each token (all threads), and the list of experts in use.
-__device__ void list_active(const MoeArgs &a, Chosen &c)
-{
-    if (threadIdx.x < 64) {   // one wavefront goes through the experts, 64 at a time
-        int n = 0;
-        for (int e0 = 0; e0 < a.E; e0 += 64) {
-            const int e = e0 + threadIdx.x;
-            bool any = false;
-            if (e < a.E)
-                for (int t = 0; t < a.T; ++t) any |= c.place[e][t] != 255;
-            const unsigned long long set = __ballot(any);
-            if (any) c.active[n + __popcll(set & ((1ull << threadIdx.x) - 1))] = (uint16_t)e;
-            n += __popcll(set);
-        }
-        if (threadIdx.x == 0) c.n_active = n;
-    }
-    __syncthreads();
-}
-
-__device__ __forceinline__ void clear_places(const MoeArgs &a, Chosen &c, int threads)
+template <int NT> __device__ __forceinline__ void clear_places(const MoeArgs &a, const Chosen<NT> &c)
 {
     unsigned *w = reinterpret_cast<unsigned *>(c.place);
-    for (int i = threadIdx.x; i < a.E * kMaxTokens / 4; i += threads) w[i] = 0xffffffffu;
+    for (int i = threadIdx.x; i < a.E * c.kTokens / 4; i += blockDim.x) w[i] = 0xffffffffu;
     __syncthreads();
 }
 
-// Sixteen 8-bit weights of a lane as two operands of the bf16 matrix instruction.
+// The list of experts in use; every wavefront counts them, the first one writes them down.
+template <int NT> __device__ int list_active(const MoeArgs &a, const Chosen<NT> &c)
+{
+    int n = 0;
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        const int e = e0 + lane;
+        bool any = false;
+        if (e < a.E) {
+            const u32x4 *w = reinterpret_cast<const u32x4 *>(c.place + e * c.kTokens);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) any |= (w[i][0] & w[i][1] & w[i][2] & w[i][3]) != 0xffffffffu;
+        }
+        const unsigned long long set = __ballot(any);
+        if (any && threadIdx.x < 64) c.active[n + __popcll(set & ((1ull << lane) - 1))] = (uint16_t)e;
+        n += __popcll(set);
+    }
+    __syncthreads();
+    return n;
+}
+
+// Sixteen 8-bit weights of a lane as two operands of the bf16 matrix instruction: 1.5 instructions a weight.
 __device__ __forceinline__ void widen(u32x4 w, bf16x8 out[2])
 {
 #pragma unroll
@@ -200,71 +236,112 @@ __device__ __forceinline__ void widen(u32x4 w, bf16x8 out[2])
     }
 }
 
+// A meeting of the workgroup that orders the LDS alone: loads on their way stay there.
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // ------------------------------------------------------------------------------------------------------------------
-// k_moe_up: h = silu(x gate) (x up) p for each token and expert it chose, in planes.  Every workgroup finds the experts by itself;
-// the first one writes them out.  Work is one expert x 16 columns of its gate and up, for all tokens; wavefronts share D.
+// k_moe_up: h = silu(x gate) (x up) p for each token and expert it chose, as operands.  Every workgroup finds the experts by itself;
+// the first one writes them out.  An item of work is one expert x 16 columns of its gate and up, for all tokens; wavefronts share D
+// and hold U blocks of it on the way: a block's registers are loaded again, for the round or the item to come, as soon as it is used.
 constexpr int kUpWaves = 8;
 
 template <int TYPE, int NT>
-__global__ void __launch_bounds__(kUpWaves * 64)
+__global__ void __launch_bounds__(kUpWaves * 64, NT == 1 ? 4 : 2)
 k_moe_up(const MoeArgs a)
 {
-    __shared__ Chosen c;
-    __shared__ f32x4 part[kUpWaves][2][NT][64];
-    constexpr int P = planes_of(TYPE), PH = h_planes_of(TYPE);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    clear_places(a, c, kUpWaves * 64);
-    for (int t = wave; t < a.T; t += kUpWaves) choose_experts(a, c, t, lane, blockIdx.x == 0);
+    constexpr int P = planes_of(TYPE), PH = h_planes_of(TYPE), U = P * NT == 1 ? 4 : P * NT <= 4 ? 2 : 1;
+    constexpr int kBuffers = NT == 1 ? 2 : 1;
+    __shared__ f32x4 part[kBuffers][kUpWaves][2][NT][64];
+    extern __shared__ u32x4 lds_behind[];
+    const Chosen<NT> c(reinterpret_cast<char *>(lds_behind), a);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    clear_places(a, c);
+    for (int t = wave; t < a.T; t += kUpWaves) {
+        if (a.E <= 64) choose_experts<1>(a, c, t, lane, blockIdx.x == 0);
+        else choose_experts<kMaxE / 64>(a, c, t, lane, blockIdx.x == 0);
+    }
     __syncthreads();
-    list_active(a, c);
+    const int k_blocks = pad64(a.D) / 64, cols = pad64(a.F) / 16, real_cols = blocks_of(a.F, kW8Cols);
+    const int items = list_active(a, c) * cols, rounds = blocks_of(k_blocks, kUpWaves * U);
+    const unsigned column = k_blocks * kW8Piece;
 
-    const int d_pad = pad64(a.D), f_pad = pad64(a.F);
-    const int k_blocks = d_pad / 64, cols = f_pad / 16, real_cols = blocks_of(a.F, kW8Cols);
-    const size_t matrix = (size_t)k_blocks * real_cols * kW8Piece;
-    for (int item = blockIdx.x; item < c.n_active * cols; item += gridDim.x) {
-        const int e = c.active[item / cols], nb = item % cols;
-        bool mine[NT];
+    struct Block {
+        u32x4 gate, up, x[P][2][NT];
+    } block[U];
+    // Block u of a round of an item; blocks that are not there (behind D, of padded columns, of no item) are left as they are
+    // and not multiplied.
+    auto there = [&](int item, int round, int u) {
+        return item < items && item % cols < real_cols && (round * U + u) * kUpWaves + wave < k_blocks;
+    };
+    auto load = [&](int item, int round, int u, Block &b) {
+        if (!there(item, round, u)) return;
+        const int e = __builtin_amdgcn_readfirstlane(c.active[item / cols]), kb = (round * U + u) * kUpWaves + wave;
+        const size_t at = ((size_t)e * real_cols + item % cols) * column + (size_t)kb * kW8Piece + lane * 16;
+        b.gate = *reinterpret_cast<const u32x4 *>(a.gate + at);
+        b.up = *reinterpret_cast<const u32x4 *>(a.up + at);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) mine[t] = 16 * t + (lane & 15) < a.T && c.place[e][16 * t + (lane & 15)] != 255;
+        for (int t = 0; t < NT; ++t) {
+            const int token = 16 * t + (lane & 15);
+            if (token < a.T && c.of(e, token) != 255) {   // the other columns are not used, whatever they hold
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) b.x[p][s][t] = a.x[(size_t)(((kb * P + p) * 2 + s) * 4 + (lane >> 4)) * a.T + token];
+            }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        block[u] = Block{};
+        load(blockIdx.x, 0, u, block[u]);
+    }
+    int buffer = 0;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
         f32x4 acc[2][NT] = {};
-        if (nb < real_cols) {
-            const size_t at = e * matrix + (size_t)nb * k_blocks * kW8Piece + lane * 16;
-            for (int kb = wave; kb < k_blocks; kb += kUpWaves) {
-                bf16x8 wg[2], wu[2];
-                widen(*reinterpret_cast<const u32x4 *>(a.gate + at + (size_t)kb * kW8Piece), wg);
-                widen(*reinterpret_cast<const u32x4 *>(a.up + at + (size_t)kb * kW8Piece), wu);
+        for (int round = 0; round < rounds; ++round) {
+            const bool last = round == rounds - 1;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+            for (int u = 0; u < U; ++u) {
+                Block &b = block[u];
+                if (there(item, round, u)) {
+                    bf16x8 wg[2], wu[2];
+                    widen(b.gate, wg);
+                    widen(b.up, wu);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        const uint16_t *x = a.x + ((size_t)p * a.T + 16 * t + (lane & 15)) * d_pad + kb * 64 + 16 * (lane >> 4);
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            u32x4 v = {};
-                            if (mine[t]) v = *reinterpret_cast<const u32x4 *>(x + 8 * s);
-                            const bf16x8 xf = __builtin_bit_cast(bf16x8, v);
-                            acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wg[s], xf, acc[0][t], 0, 0, 0);
-                            acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wu[s], xf, acc[1][t], 0, 0, 0);
-                        }
-                    }
+                        for (int p = 0; p < P; ++p)
+#pragma unroll
+                            for (int s = 0; s < 2; ++s) {
+                                const bf16x8 xf = __builtin_bit_cast(bf16x8, b.x[p][s][t]);
+                                acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wg[s], xf, acc[0][t], 0, 0, 0);
+                                acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wu[s], xf, acc[1][t], 0, 0, 0);
+                            }
                 }
+                load(last ? item + gridDim.x : item, last ? 0 : round + 1, u, b);
             }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            part[wave][0][t][lane] = acc[0][t];
-            part[wave][1][t][lane] = acc[1][t];
+            part[buffer][wave][0][t][lane] = acc[0][t];
+            part[buffer][wave][1][t][lane] = acc[1][t];
         }
-        __syncthreads();
+        meet();
         for (int i = threadIdx.x; i < NT * 64; i += kUpWaves * 64) {
+            const int e = c.active[item / cols], nb = item % cols;
             const int t = i >> 6, l = i & 63, token = 16 * t + (l & 15);
-            const int place = token < a.T ? c.place[e][token] : 255;
+            const int place = token < a.T ? c.of(e, token) : 255;
             if (place == 255) continue;
-            f32x4 g = part[0][0][t][l], u = part[0][1][t][l];
+            f32x4 g = part[buffer][0][0][t][l], u = part[buffer][0][1][t][l];
 #pragma unroll
             for (int w = 1; w < kUpWaves; ++w) {
-                g += part[w][0][t][l];
-                u += part[w][1][t][l];
+                g += part[buffer][w][0][t][l];
+                u += part[buffer][w][1][t][l];
             }
             const int f = nb * 16 + 4 * (l >> 4);
             uint16_t out[PH][4];
@@ -273,80 +350,114 @@ k_moe_up(const MoeArgs a)
                 float h = 0.f;
                 if (f + r < a.F) {
                     const float gv = g[r] * a.gate_scale[(size_t)e * a.F + f + r], uv = u[r] * a.up_scale[(size_t)e * a.F + f + r];
-                    h = gv / (1.f + expf(-gv)) * uv * c.p[token][place];
+                    h = gv / (1.f + expf(-gv)) * uv * c.p[token * a.top + place];
                 }
 #pragma unroll
                 for (int p = 0; p < PH; ++p) out[p][r] = p < PH - 1 ? cut(h) : Entry<TST_BF16>::put(h);   // the last one rounds
             }
+            const int kb = f >> 6, quarter = (f >> 4) & 3, half = (f >> 3) & 1;
 #pragma unroll
-            for (int p = 0; p < PH; ++p)
-                *reinterpret_cast<u32x2 *>(a.h + ((size_t)p * a.T * a.top + token * a.top + place) * f_pad + f) =
-                    u32x2{out[p][0] | (unsigned)out[p][1] << 16, out[p][2] | (unsigned)out[p][3] << 16};
+            for (int p = 0; p < PH; ++p) {
+                u32x4 *to = a.h + (size_t)(((kb * PH + p) * 2 + half) * 4 + quarter) * (a.T * a.top) + token * a.top + place;
+                reinterpret_cast<u32x2 *>(to)[(f >> 2) & 1] = u32x2{out[p][0] | (unsigned)out[p][1] << 16, out[p][2] | (unsigned)out[p][3] << 16};
+            }
         }
-        __syncthreads();
+        if (kBuffers == 1) meet();
+        else buffer ^= 1;   // what stands in the other one was read before the meeting
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// k_moe_down: 16 columns of Y for all tokens; the wavefronts share the rows of all experts in use, one after another.  Between
-// experts a wavefront scales its sums with the expert's channels and adds them to those of the token.
-constexpr int kDownWaves = 8;
+// k_moe_down: 16 columns of Y for all tokens; the wavefronts share the blocks of all experts in use, one expert behind another, U
+// of them on the way.  A block's sums are scaled with its expert's channels and added to those of the token.
+constexpr int down_waves(int nt) { return nt <= 2 ? 16 : 8; }   // as many as their registers let in
 
 template <int TYPE, int NT>
-__global__ void __launch_bounds__(kDownWaves * 64)
+__global__ void __launch_bounds__(down_waves(NT) * 64)
 k_moe_down(const MoeArgs a)
 {
     typedef Entry<TYPE> E;
-    __shared__ Chosen c;
+    constexpr int PH = h_planes_of(TYPE), U = NT == 1 ? (PH == 2 ? 3 : 2) : 1, kDownWaves = down_waves(NT);
+    typedef float scale4 __attribute__((ext_vector_type(4), aligned(4)));
     __shared__ f32x4 part[kDownWaves][NT][64];
-    constexpr int PH = h_planes_of(TYPE);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nb = blockIdx.x;
-    clear_places(a, c, kDownWaves * 64);
-    for (int i = threadIdx.x; i < a.T * a.top; i += kDownWaves * 64) c.place[a.ids[i]][i / a.top] = (uint8_t)(i % a.top);
+    extern __shared__ u32x4 lds_behind[];
+    const Chosen<NT> c(reinterpret_cast<char *>(lds_behind), a);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nb = blockIdx.x;
+    clear_places(a, c);
+    for (int i = threadIdx.x; i < a.T * a.top; i += kDownWaves * 64) c.place[a.ids[i] * c.kTokens + i / a.top] = (uint8_t)(i % a.top);
     __syncthreads();
-    list_active(a, c);
+    const int k_blocks = pad64(a.F) / 64, n_blocks = blocks_of(a.D, kW8Cols);
+    const int total = list_active(a, c) * k_blocks, share = blocks_of(total, kDownWaves);
+    const int begin = min(wave * share, total), end = min(begin + share, total);
 
-    const int f_pad = pad64(a.F), k_blocks = f_pad / 64, n_blocks = blocks_of(a.D, kW8Cols);
-    const int total = c.n_active * k_blocks, share = blocks_of(total, kDownWaves);
-    int at = min(wave * share, total);
-    const int end = min(at + share, total);
-    f32x4 sum[NT] = {};
-    while (at < end) {
-        const int e = c.active[at / k_blocks], kb0 = at % k_blocks, kb1 = min(k_blocks, kb0 + end - at);
-        at += kb1 - kb0;
-        int row[NT];   // of h, or -1
+    struct Block {
+        u32x4 w, h[PH][2][NT];
+        f32x4 scale;
+    } block[U];
+    int e = 0, kb = 0, row[NT];   // of the next block to be requested; row: of h, or -1
+    auto enter = [&](int nth) {
+        e = __builtin_amdgcn_readfirstlane(c.active[nth]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int token = 16 * t + (lane & 15);
-            const int place = token < a.T ? c.place[e][token] : 255;
+            const int place = token < a.T ? c.of(e, token) : 255;
             row[t] = place == 255 ? -1 : token * a.top + place;
         }
-        const char *w = a.down + ((size_t)e * n_blocks + nb) * k_blocks * kW8Piece + lane * 16;
-        f32x4 acc[NT] = {};
-        for (int kb = kb0; kb < kb1; ++kb) {
-            bf16x8 wd[2];
-            widen(*reinterpret_cast<const u32x4 *>(w + (size_t)kb * kW8Piece), wd);
+    };
+    const int d = nb * 16 + 4 * (lane >> 4);
+    const bool whole = nb * 16 + 16 <= a.D;
+    int next = begin;
+    auto load = [&](Block &b) {
+        if (next >= end) return;
+        b.w = *reinterpret_cast<const u32x4 *>(a.down + (((size_t)e * n_blocks + nb) * k_blocks + kb) * kW8Piece + lane * 16);
+        const float *scale = a.down_scale + (size_t)e * a.D;
+        if (whole) {
+            b.scale = *reinterpret_cast<const scale4 *>(scale + d);
+        } else {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int p = 0; p < PH; ++p) {
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        u32x4 v = {};
-                        if (row[t] >= 0)
-                            v = *reinterpret_cast<const u32x4 *>(a.h + ((size_t)p * a.T * a.top + row[t]) * f_pad + kb * 64 + 16 * (lane >> 4) + 8 * s);
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, v), acc[t], 0, 0, 0);
-                    }
-                }
-            }
+            for (int r = 0; r < 4; ++r) b.scale[r] = scale[min(d + r, a.D - 1)];
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = min(nb * 16 + 4 * (lane >> 4) + r, a.D - 1);
-            const float scale = a.down_scale[(size_t)e * a.D + d];
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (row[t] >= 0) sum[t][r] = fmaf(scale, acc[t][r], sum[t][r]);
+            for (int p = 0; p < PH; ++p)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    b.h[p][s][t] = u32x4{};
+                    if (row[t] >= 0) b.h[p][s][t] = a.h[(size_t)(((kb * PH + p) * 2 + s) * 4 + (lane >> 4)) * (a.T * a.top) + row[t]];
+                }
+        ++next;
+        if (++kb == k_blocks && next < end) {
+            kb = 0;
+            enter(next / k_blocks);
+        }
+    };
+    if (begin < end) {
+        kb = begin % k_blocks;
+        enter(begin / k_blocks);
+    }
+    f32x4 sum[NT] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(block[u]);
+    for (int at = begin; at < end; at += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            Block &b = block[u];
+            if (at + u >= end) break;
+            bf16x8 wd[2];
+            widen(b.w, wd);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f32x4 acc = {};
+#pragma unroll
+                for (int p = 0; p < PH; ++p)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, b.h[p][s][t]), acc, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[t][r] = fmaf(b.scale[r], acc[r], sum[t][r]);
+            }
+            load(b);
         }
     }
 #pragma unroll
@@ -361,8 +472,8 @@ k_moe_down(const MoeArgs a)
         typename E::bits *to = static_cast<typename E::bits *>(a.Y) + (size_t)token * a.D;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = nb * 16 + 4 * (l >> 4) + r;
-            if (d < a.D) to[d] = E::put(y[r]);
+            const int column = nb * 16 + 4 * (l >> 4) + r;
+            if (column < a.D) to[column] = E::put(y[r]);
         }
     }
 }
@@ -387,12 +498,15 @@ MoeSpace moe_space(const tst_moe_t &m, int T, int top)
 
 template <int TYPE, int NT> hipError_t launch_moe_nt(const MoeArgs &a, hipStream_t stream)
 {
-    k_moe_router<TYPE><<<dim3(blocks_of(a.E, kRouterWaves), a.T), kRouterWaves * 64, 0, stream>>>(a);
+    const dim3 router(blocks_of(a.E, kRouterWaves), a.T);
+    if (a.wide) k_moe_router<TYPE, true><<<router, kRouterWaves * 64, 0, stream>>>(a);
+    else k_moe_router<TYPE, false><<<router, kRouterWaves * 64, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    const int64_t items = (int64_t)(a.E < a.T * a.top ? a.E : a.T * a.top) * (pad64(a.F) / 16);
-    k_moe_up<TYPE, NT><<<(unsigned)(items < 1024 ? items : 1024), kUpWaves * 64, 0, stream>>>(a);
+    const size_t lds = Chosen<NT>::bytes(a);
+    const int64_t items = (int64_t)(a.E < a.T * a.top ? a.E : a.T * a.top) * (pad64(a.F) / 16), groups = 2 * (int64_t)compute_units();
+    k_moe_up<TYPE, NT><<<(unsigned)(items < groups ? items : groups), kUpWaves * 64, lds, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    k_moe_down<TYPE, NT><<<blocks_of(a.D, kW8Cols), kDownWaves * 64, 0, stream>>>(a);
+    k_moe_down<TYPE, NT><<<blocks_of(a.D, kW8Cols), down_waves(NT) * 64, lds, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -433,13 +547,15 @@ int tst_moe(const void *X, int64_t x_stride, const tst_moe_t *moe, int top_k, in
     if (!workspace || workspace_bytes < s.total) return TSTGEMM_EWORKSPACE;
     if (!tst::aligned(workspace, 256)) return TSTGEMM_EINVAL;
     char *ws = static_cast<char *>(workspace);
+    const int piece = (int)(16 / entry);
+    const bool wide = tst::aligned(X, 16) && tst::aligned(m.router, 16) && x_stride % piece == 0 && m.width % piece == 0;
     for (int64_t t0 = 0; t0 < T; t0 += tst::kMaxTokens) {
         const int n = (int)(T - t0 < tst::kMaxTokens ? T - t0 : tst::kMaxTokens);
         const tst::MoeArgs a{static_cast<const char *>(X) + t0 * x_stride * entry, x_stride, m.router, static_cast<const char *>(m.gate),
                              static_cast<const char *>(m.up), static_cast<const char *>(m.down), m.gate_scale, m.up_scale, m.down_scale,
                              static_cast<char *>(Y) + t0 * m.width * entry, ids + t0 * top_k, p + t0 * top_k, m.experts, m.width, m.inner, n,
-                             top_k, normalize != 0, reinterpret_cast<float *>(ws + s.logits), reinterpret_cast<uint16_t *>(ws + s.x),
-                             reinterpret_cast<uint16_t *>(ws + s.h)};
+                             top_k, normalize != 0, wide, reinterpret_cast<float *>(ws + s.logits), reinterpret_cast<tst::u32x4 *>(ws + s.x),
+                             reinterpret_cast<tst::u32x4 *>(ws + s.h)};
         const hipError_t e = tst::for_type(m.type, [&](auto type) {
             constexpr int TYPE = decltype(type)::value;
             hipStream_t st = static_cast<hipStream_t>(stream);
