@@ -33,6 +33,11 @@ struct MoeArgs {
     float *logits;   // [T][E]
     u32x4 *x;        // operands of X, zero behind D
     u32x4 *h;        // operands of h, a row for each token and expert it chose, zero behind F
+    int32_t *count;  // experts in use
+    int32_t *used;   // they, ascending
+    uint8_t *places; // [nth][16 NT] rank of the nth expert in use among a token's, or 255
+    float *partial;  // [split][T][D]
+    int splits;
 };
 
 constexpr int planes_of(int type) { return type == TST_F32 ? 3 : type == TST_F16 ? 2 : 1; }
@@ -267,7 +272,7 @@ k_moe_up(const MoeArgs a)
     }
     __syncthreads();
     const int k_blocks = pad64(a.D) / 64, cols = pad64(a.F) / 16, real_cols = blocks_of(a.F, kW8Cols);
-    const int items = list_active(a, c) * cols, rounds = blocks_of(k_blocks, kUpWaves * U);
+    const int n_active = list_active(a, c), items = n_active * cols, rounds = blocks_of(k_blocks, kUpWaves * U);
     const unsigned column = k_blocks * kW8Piece;
 
     struct Block {
@@ -299,6 +304,11 @@ k_moe_up(const MoeArgs a)
     for (int u = 0; u < U; ++u) {
         block[u] = Block{};
         load(blockIdx.x, 0, u, block[u]);
+    }
+    if (blockIdx.x == gridDim.x - 1) {   // for k_moe_down
+        if (threadIdx.x == 0) *a.count = n_active;
+        for (int i = threadIdx.x; i < n_active; i += kUpWaves * 64) a.used[i] = c.active[i];
+        for (int i = threadIdx.x; i < n_active * c.kTokens; i += kUpWaves * 64) a.places[i] = c.place[c.active[i / c.kTokens] * c.kTokens + i % c.kTokens];
     }
     int buffer = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
@@ -368,55 +378,43 @@ k_moe_up(const MoeArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// k_moe_down: 16 columns of Y for all tokens; the wavefronts share the blocks of all experts in use, one expert behind another, U
-// of them on the way.  A block's sums are scaled with its expert's channels and added to those of the token.
-constexpr int down_waves(int nt) { return nt <= 2 ? 16 : 8; }   // as many as their registers let in
+// k_moe_down: 64 columns of Y for all tokens.  The blocks of all experts in use, one expert behind another, are shared by the workgroups of
+// a split and their wavefronts, each with a run of them and U on the way.  Four pieces of weights use one operand of h, which
+// comes from the L2: with 16 columns the registers of h on its way left too few for the weights (86 MB of weights 41 us; now 19).
+// Between experts a wavefront scales its sums with the expert's channels and adds them to those of the token.
+constexpr int kDownCols = 4;   // pieces of 16
+constexpr int kDownWaves = 8;
 
 template <int TYPE, int NT>
-__global__ void __launch_bounds__(down_waves(NT) * 64)
+__global__ void __launch_bounds__(kDownWaves * 64, 2)
 k_moe_down(const MoeArgs a)
 {
     typedef Entry<TYPE> E;
-    constexpr int PH = h_planes_of(TYPE), U = NT == 1 ? (PH == 2 ? 3 : 2) : 1, kDownWaves = down_waves(NT);
-    typedef float scale4 __attribute__((ext_vector_type(4), aligned(4)));
-    __shared__ f32x4 part[kDownWaves][NT][64];
-    extern __shared__ u32x4 lds_behind[];
-    const Chosen<NT> c(reinterpret_cast<char *>(lds_behind), a);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nb = blockIdx.x;
-    clear_places(a, c);
-    for (int i = threadIdx.x; i < a.T * a.top; i += kDownWaves * 64) c.place[a.ids[i] * c.kTokens + i / a.top] = (uint8_t)(i % a.top);
-    __syncthreads();
+    constexpr int PH = h_planes_of(TYPE), U = NT == 1 ? 6 - PH : NT == 2 ? 2 : 1;
+    __shared__ f32x4 part[kDownWaves][kDownCols][NT][64];   // of the experts that a wavefront is done with
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int split = blockIdx.y, nb0 = blockIdx.x * kDownCols;
     const int k_blocks = pad64(a.F) / 64, n_blocks = blocks_of(a.D, kW8Cols);
-    const int total = list_active(a, c) * k_blocks, share = blocks_of(total, kDownWaves);
-    const int begin = min(wave * share, total), end = min(begin + share, total);
+    const int total = *a.count * k_blocks, share = blocks_of(total, kDownWaves * a.splits);
+    const int begin = min((split * kDownWaves + wave) * share, total), end = min(begin + share, total);
 
     struct Block {
-        u32x4 w, h[PH][2][NT];
-        f32x4 scale;
+        u32x4 w[kDownCols], h[PH][2][NT];
     } block[U];
-    int e = 0, kb = 0, row[NT];   // of the next block to be requested; row: of h, or -1
+    int e = 0, kb = 0, next = begin, row[NT];   // of the block to be requested next; row: of h, or -1
     auto enter = [&](int nth) {
-        e = __builtin_amdgcn_readfirstlane(c.active[nth]);
+        e = __builtin_amdgcn_readfirstlane(a.used[nth]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int token = 16 * t + (lane & 15);
-            const int place = token < a.T ? c.of(e, token) : 255;
+            const int token = 16 * t + (lane & 15), place = a.places[nth * 16 * NT + token];
             row[t] = place == 255 ? -1 : token * a.top + place;
         }
     };
-    const int d = nb * 16 + 4 * (lane >> 4);
-    const bool whole = nb * 16 + 16 <= a.D;
-    int next = begin;
     auto load = [&](Block &b) {
         if (next >= end) return;
-        b.w = *reinterpret_cast<const u32x4 *>(a.down + (((size_t)e * n_blocks + nb) * k_blocks + kb) * kW8Piece + lane * 16);
-        const float *scale = a.down_scale + (size_t)e * a.D;
-        if (whole) {
-            b.scale = *reinterpret_cast<const scale4 *>(scale + d);
-        } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) b.scale[r] = scale[min(d + r, a.D - 1)];
-        }
+        for (int j = 0; j < kDownCols; ++j)
+            b.w[j] = *reinterpret_cast<const u32x4 *>(a.down + (((size_t)e * n_blocks + min(nb0 + j, n_blocks - 1)) * k_blocks + kb) * kW8Piece + lane * 16);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -432,11 +430,35 @@ k_moe_down(const MoeArgs a)
             enter(next / k_blocks);
         }
     };
+    f32x4 acc[kDownCols][NT] = {};
+    int left = 0, nth = 0;   // the expert whose sums are in acc, and its blocks to come
     if (begin < end) {
+        nth = begin / k_blocks;
         kb = begin % k_blocks;
-        enter(begin / k_blocks);
+        left = k_blocks - kb;
+        enter(nth);
     }
-    f32x4 sum[NT] = {};
+    auto settle = [&]() {
+        const float *scale = a.down_scale + (size_t)a.used[nth] * a.D;
+#pragma unroll
+        for (int j = 0; j < kDownCols; ++j) {
+            float by[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) by[r] = scale[min((nb0 + j) * 16 + 4 * (lane >> 4) + r, a.D - 1)];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f32x4 v = part[wave][j][t][lane];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = fmaf(by[r], acc[j][t][r], v[r]);
+                part[wave][j][t][lane] = v;
+                acc[j][t] = f32x4{};
+            }
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kDownCols; ++j)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) part[wave][j][t][lane] = f32x4{};
 #pragma unroll
     for (int u = 0; u < U; ++u) load(block[u]);
     for (int at = begin; at < end; at += U) {
@@ -444,55 +466,89 @@ k_moe_down(const MoeArgs a)
         for (int u = 0; u < U; ++u) {
             Block &b = block[u];
             if (at + u >= end) break;
-            bf16x8 wd[2];
-            widen(b.w, wd);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f32x4 acc = {};
+            for (int j = 0; j < kDownCols; ++j) {
+                bf16x8 wd[2];
+                widen(b.w[j], wd);
 #pragma unroll
-                for (int p = 0; p < PH; ++p)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, b.h[p][s][t]), acc, 0, 0, 0);
+                    for (int p = 0; p < PH; ++p)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum[t][r] = fmaf(b.scale[r], acc[r], sum[t][r]);
+                        for (int s = 0; s < 2; ++s)
+                            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, b.h[p][s][t]), acc[j][t], 0, 0, 0);
             }
             load(b);
+            if (--left == 0) {
+                settle();
+                left = k_blocks;
+                ++nth;
+            }
         }
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) part[wave][t][lane] = sum[t];
+    if (begin < end && left != k_blocks) settle();   // an expert that others go on with
     __syncthreads();
-    for (int i = threadIdx.x; i < NT * 64; i += kDownWaves * 64) {
-        const int t = i >> 6, l = i & 63, token = 16 * t + (l & 15);
+    for (int i = threadIdx.x; i < kDownCols * NT * 64; i += kDownWaves * 64) {
+        const int l = i & 63, t = (i >> 6) % NT, j = (i >> 6) / NT, token = 16 * t + (l & 15);
         if (token >= a.T) continue;
-        f32x4 y = part[0][t][l];
+        f32x4 y = part[0][j][t][l];
 #pragma unroll
-        for (int w = 1; w < kDownWaves; ++w) y += part[w][t][l];
-        typename E::bits *to = static_cast<typename E::bits *>(a.Y) + (size_t)token * a.D;
+        for (int w = 1; w < kDownWaves; ++w) y += part[w][j][t][l];
+        const int d = (nb0 + j) * 16 + 4 * (l >> 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int column = nb * 16 + 4 * (l >> 4) + r;
-            if (column < a.D) to[column] = E::put(y[r]);
+            if (d + r >= a.D) continue;
+            if (a.splits == 1) static_cast<typename E::bits *>(a.Y)[(size_t)token * a.D + d + r] = E::put(y[r]);
+            else a.partial[((size_t)split * a.T + token) * a.D + d + r] = y[r];
         }
     }
 }
 
+// k_moe_join: the sums of the splits, in their order.
+constexpr int kJoinThreads = 256;
+
+template <int TYPE>
+__global__ void __launch_bounds__(kJoinThreads)
+k_moe_join(const MoeArgs a)
+{
+    typedef Entry<TYPE> E;
+    const int i = blockIdx.x * kJoinThreads + threadIdx.x, n = a.T * a.D;   // (T <= 64, D < 2^17)
+    if (i >= n) return;
+    float y = a.partial[i];
+#pragma unroll 16
+    for (int s = 1; s < a.splits; ++s) y += a.partial[(size_t)s * n + i];
+    static_cast<typename E::bits *>(a.Y)[i] = E::put(y);
+}
+
+// Workgroups that share the experts of a column tile, so that every compute unit has one; each has at least one block for a wavefront.
+constexpr int kMaxSplits = 16;
+int down_splits(int T, int D, int F, int top)
+{
+    const int tiles = blocks_of(D, 16 * kDownCols);
+    const int64_t wanted = blocks_of(compute_units(), tiles), blocks = (int64_t)blocks_of(F, 64) * (T < 4 ? top : 2 * top);
+    const int64_t useful = (blocks + kDownWaves - 1) / kDownWaves;
+    return (int)(wanted < useful ? (wanted < kMaxSplits ? wanted : kMaxSplits) : (useful < kMaxSplits ? useful : kMaxSplits));
+}
+
 struct MoeSpace {
-    size_t logits, x, h, total;
+    size_t logits, x, h, count, used, places, partial, total;
 };
 MoeSpace moe_space(const tst_moe_t &m, int T, int top)
 {
     MoeSpace s{};
     if (T > kMaxTokens) T = kMaxTokens;
-    size_t at = 0;
-    s.logits = at;
-    at += round256((size_t)T * m.experts * sizeof(float));
-    s.x = at;
-    at += round256((size_t)planes_of(m.type) * T * pad64(m.width) * 2);
-    s.h = at;
-    at += round256((size_t)h_planes_of(m.type) * T * top * pad64(m.inner) * 2);
-    s.total = at;
+    auto take = [&](size_t &at, size_t bytes) {
+        at = s.total;
+        s.total += round256(bytes);
+    };
+    const size_t in_use = (size_t)m.experts < (size_t)T * top ? m.experts : (size_t)T * top;
+    take(s.logits, (size_t)T * m.experts * sizeof(float));
+    take(s.x, (size_t)planes_of(m.type) * T * pad64(m.width) * 2);
+    take(s.h, (size_t)h_planes_of(m.type) * T * top * pad64(m.inner) * 2);
+    take(s.count, sizeof(int32_t));
+    take(s.used, in_use * sizeof(int32_t));
+    take(s.places, in_use * (size_t)((T + 63) / 64 * 64));
+    take(s.partial, (size_t)kMaxSplits * T * m.width * sizeof(float));
     return s;
 }
 
@@ -506,7 +562,11 @@ template <int TYPE, int NT> hipError_t launch_moe_nt(const MoeArgs &a, hipStream
     const int64_t items = (int64_t)(a.E < a.T * a.top ? a.E : a.T * a.top) * (pad64(a.F) / 16), groups = 2 * (int64_t)compute_units();
     k_moe_up<TYPE, NT><<<(unsigned)(items < groups ? items : groups), kUpWaves * 64, lds, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    k_moe_down<TYPE, NT><<<blocks_of(a.D, kW8Cols), down_waves(NT) * 64, lds, stream>>>(a);
+    k_moe_down<TYPE, NT><<<dim3(blocks_of(a.D, 16 * kDownCols), a.splits), kDownWaves * 64, 0, stream>>>(a);
+    if (a.splits > 1) {
+        if (hipError_t e = hipGetLastError()) return e;
+        k_moe_join<TYPE><<<blocks_of(a.T * a.D, kJoinThreads), kJoinThreads, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
@@ -555,7 +615,9 @@ int tst_moe(const void *X, int64_t x_stride, const tst_moe_t *moe, int top_k, in
                              static_cast<const char *>(m.up), static_cast<const char *>(m.down), m.gate_scale, m.up_scale, m.down_scale,
                              static_cast<char *>(Y) + t0 * m.width * entry, ids + t0 * top_k, p + t0 * top_k, m.experts, m.width, m.inner, n,
                              top_k, normalize != 0, wide, reinterpret_cast<float *>(ws + s.logits), reinterpret_cast<tst::u32x4 *>(ws + s.x),
-                             reinterpret_cast<tst::u32x4 *>(ws + s.h)};
+                             reinterpret_cast<tst::u32x4 *>(ws + s.h), reinterpret_cast<int32_t *>(ws + s.count), reinterpret_cast<int32_t *>(ws + s.used),
+                             reinterpret_cast<uint8_t *>(ws + s.places), reinterpret_cast<float *>(ws + s.partial),
+                             tst::down_splits(n, m.width, m.inner, top_k)};
         const hipError_t e = tst::for_type(m.type, [&](auto type) {
             constexpr int TYPE = decltype(type)::value;
             hipStream_t st = static_cast<hipStream_t>(stream);
