@@ -121,27 +121,6 @@ template <int NT> struct Chosen {
     __device__ int of(int e, int token) const { return place[e * kTokens + token]; }
 };
 
-// Bits that order as logits do: NaN above everything, -0 as +0; none is 0.
-__device__ __forceinline__ unsigned order_key(float v)
-{
-    const unsigned u = __float_as_uint(v + 0.f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// The largest of a wavefront's values, the same in all lanes: maxima of 2, 4, 8, 16 neighbours, of rows of 16 and of halves, in lane 63.
-__device__ __forceinline__ unsigned wave_max(unsigned v)
-{
-    auto step = [&](auto control) { return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xf, 0xf, false)); };
-    v = step(std::integral_constant<int, 0x111>{});   // row_shr 1
-    v = step(std::integral_constant<int, 0x112>{});
-    v = step(std::integral_constant<int, 0x114>{});
-    v = step(std::integral_constant<int, 0x118>{});
-    v = step(std::integral_constant<int, 0x142>{});   // row_bcast 15
-    v = step(std::integral_constant<int, 0x143>{});   // row_bcast 31
-    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
-}
-
 // A wavefront finds a token's experts: top rounds of the largest of what is left; lane l holds experts l, l + 64, ...
 template <int PER, int NT>
 __device__ void choose_experts(const MoeArgs &a, const Chosen<NT> &c, int t, int lane, bool write)
@@ -152,7 +131,7 @@ __device__ void choose_experts(const MoeArgs &a, const Chosen<NT> &c, int t, int
     for (int i = 0; i < PER; ++i) {
         const int e = lane + 64 * i;
         l[i] = e < a.E ? a.logits[t * a.E + e] : -INFINITY;
-        key[i] = e < a.E ? order_key(l[i]) : 0;
+        key[i] = e < a.E ? order_bits(l[i]) : 0;
     }
     float most = 0.f, all = 0.f, chosen = 0.f, mine = 0.f;
     for (int j = 0; j < a.top; ++j) {

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "tst_ops.h"
 
@@ -42,6 +43,29 @@ template <> struct Entry<TST_F16> {
     static __device__ __forceinline__ float get(bits b) { return (float)__builtin_bit_cast(_Float16, b); }
     static __device__ __forceinline__ bits put(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };
+
+// The largest of a wavefront's values, the same in all lanes: maxima of 2, 4, 8, 16 neighbours, of rows of 16 and of halves, in lane 63.
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+    auto step = [&](auto control) { return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, 0xf, 0xf, false)); };
+    v = step(std::integral_constant<int, 0x111>{});   // row_shr 1
+    v = step(std::integral_constant<int, 0x112>{});
+    v = step(std::integral_constant<int, 0x114>{});
+    v = step(std::integral_constant<int, 0x118>{});
+    v = step(std::integral_constant<int, 0x142>{});   // row_bcast 15
+    v = step(std::integral_constant<int, 0x143>{});   // row_bcast 31
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// Bits that order as floats do: NaN above everything, -0 as +0.  No float has 0.
+__device__ __forceinline__ unsigned order_bits(float v)
+{
+    const unsigned u = __float_as_uint(v + 0.f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// The float of bits that are not a NaN's.
+__device__ __forceinline__ float from_order_bits(unsigned b) { return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b); }
 
 int compute_units();   // (tstgemm_side.hip)
 

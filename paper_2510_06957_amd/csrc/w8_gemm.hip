@@ -11,13 +11,6 @@ namespace {
 // The row stays in the registers on the way if it fits (kQuantPieces pieces of 16 bytes for a thread), else it is read twice.
 constexpr int kQuantThreads = 256, kQuantPieces = 4;
 
-__device__ __forceinline__ unsigned wave_max(unsigned v)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, d));
-    return v;
-}
-
 // What a row's codes are made with, from the bits of its largest magnitude.
 struct Scaling {
     bool finite;

@@ -302,8 +302,12 @@ def logits(R, V, dtype, seed, columns=None):
     return z.cuda()[:, :V]
 
 
-def check_logprobs(Z, token, top):
-    z = f64(Z)
+def check_logprobs(Z, token, top, rows=slice(None)):
+    """rows: those looked at"""
+    out = tg.tst_logprobs(Z, None if token is None else token.cuda(), top=top)
+    of_token, entropy, ids, of_top = (o[rows] for o in out)
+    token = None if token is None else token[rows]
+    z = f64(Z[rows])
     R, V = z.shape
     with np.errstate(all="ignore"):
         d = z - z.max(1, keepdims=True)
@@ -312,7 +316,6 @@ def check_logprobs(Z, token, top):
         lp = d - log_sum
         spread = np.where(e > 0, e * -d, 0).sum(1) / e.sum(1)
     d_sum = (V / 256 + 40) * U
-    of_token, entropy, ids, of_top = tg.tst_logprobs(Z, None if token is None else token.cuda(), top=top)
     assert_within(entropy, log_sum[:, 0] + spread, d_sum * (2 + log_sum[:, 0] + 3 * spread), what="entropy")
     order = np.argsort(-z, axis=1, kind="stable")[:, :top]
     assert np.array_equal(ids.cpu().numpy(), order)
@@ -360,6 +363,27 @@ def test_logprobs_of_masked_rows_and_ties(V, dtype):
     Z[7] = Z[7].abs() + 60000                # far from zero (and infinite differences nowhere)
     Z[7] = Z[7].clamp(max=65000)
     check_logprobs(Z, torch.tensor([1, V - 1, 3, 4, 0, 3, 1, 2]), 9)
+
+
+@pytest.mark.parametrize("R", [10, 1030])   # rows in splits, and whole ones
+@pytest.mark.parametrize("V,top", [(5000, 1), (40007, 20), (70000, 64)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logprobs_of_rows_in_many_chunks(R, V, top, dtype):
+    """What a list of candidates can make of a row: values that rise, fall, tie everywhere, in runs, at the bound, only at the end."""
+    Z = torch.zeros((R, V), dtype=TYPES[dtype], device="cuda")
+    n = torch.arange(V, device="cuda")
+    Z[:10] = logits(10, V, dtype, 28)
+    Z[0] = (n / V * 20 - 10).to(TYPES[dtype])
+    Z[1] = (10 - n / V * 20).to(TYPES[dtype])
+    Z[2] = (n % 5).to(TYPES[dtype])
+    Z[3] = (n // (V // 7)).to(TYPES[dtype])
+    Z[4, :V - top - 3] = -float("inf")
+    Z[5, : V // 2] = torch.finfo(TYPES[dtype]).min
+    Z[6] = Z[6].round()
+    Z[7, 16384:16384 + 300 if V > 17000 else V] = 30.0
+    Z[8, ::64] = 25.0
+    Z[9, V - 1] = 60.0
+    check_logprobs(Z, torch.arange(R) % V, top, slice(0, 10))
 
 
 @pytest.mark.parametrize("V", [33, 2000, 70001])
