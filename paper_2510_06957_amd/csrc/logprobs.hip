@@ -1,10 +1,10 @@
 // Log probabilities of given tokens, entropy and the top alternatives of rows of logits (tst_logprobs).
 //
-// One pass over the logits.  A row, or a split of one where there are few rows, belongs to a workgroup, which takes it in chunks that its
-// threads hold in registers; a thread keeps a running maximum m, sum e^(z - m) and sum e^(z - m) (z - m).  The alternatives
-// come from the same registers: of the threads' maxima of a chunk, the n-th largest is a lower bound of the row's n-th largest
-// logit, so only what reaches it (seldom much more than n) goes into a list in the LDS, with its place; a member's rank is the number
-// of members before it.
+// One pass over the logits.  A row, or a split of one where there are few rows, belongs to a workgroup, whose wavefronts take it in chunks
+// that their lanes hold in registers, each for itself: nobody waits for anybody before the end.  A lane keeps a running maximum m,
+// sum e^(z - m) and sum e^(z - m) (z - m).  The alternatives come from the same registers: of the lanes' maxima of a chunk, the n-th
+// largest is a lower bound of the row's n-th largest logit, so only what reaches it (seldom much more than n) goes into a list in the
+// LDS, with its place; a member's rank is the number of members before it.
 #include "ops_internal.h"
 
 namespace tst {
@@ -30,18 +30,36 @@ __device__ __forceinline__ unsigned long long key_of(float v, int token) { retur
 __device__ __forceinline__ int token_of(unsigned long long key) { return (int)~(unsigned)key; }
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kVectors = 8, kFewVectors = 2;   // 16 bytes each, of a chunk for a thread: of whole rows, of splits
-// The list.  It is kept short; it has room for what is left of earlier chunks (at most `top`) and all that `top` threads hold of one.
-constexpr int kShort = 256, kList = TST_LOGPROBS_MAX_TOP + TST_LOGPROBS_MAX_TOP * kVectors * 8;
+constexpr int kVectors = 4, kFewVectors = 2;   // 16 bytes each, of a chunk for a lane: of whole rows, of splits
+constexpr int kMaxTop = TST_LOGPROBS_MAX_TOP;
+// A wavefront's list is kept under kShort.  Rising logits fill it with all that 64 lanes hold in one vector.
+constexpr int kShort = 192, kRoom = kMaxTop + 64 * 8;
 constexpr float kNan = __builtin_nanf("");
+typedef unsigned long long Key;
 
 struct Shared {
-    unsigned long long list[kList], sorted[TST_LOGPROBS_MAX_TOP];
-    __align__(16) float most[kThreads];
-    float sums[2][kWaves], bounds[kWaves];
-    int count, counts[kWaves];
-    float bound;
+    Key list[kWaves][kRoom], best[kWaves][kMaxTop], sorted[kMaxTop];
+    float sums[3][kWaves], lost[kWaves];
+    int counts[kWaves], flags[kWaves];
 };
+
+// The n largest of list[0 .. count), largest first, into sorted; 0 behind the last.  `threads` threads that have met, t of them this one.
+__device__ __forceinline__ void rank_keys(const Key *list, int count, Key *sorted, int n, int t, int threads)
+{
+    for (int i = t; i < count; i += threads) {
+        const Key mine = list[i];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < count; ++j) rank += list[j] > mine;   // (keys differ: each holds its token)
+        if (rank < n) sorted[rank] = mine;
+    }
+}
+
+__device__ __forceinline__ void order_wave()   // of a wavefront's own stores and reads in the LDS
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
 
 template <typename F> __device__ __forceinline__ float over_waves(float v, float *part, F f)
 {
@@ -55,84 +73,44 @@ template <typename F> __device__ __forceinline__ float over_waves(float v, float
     return v;
 }
 
-// The n largest keys of list[0 .. count), largest first, into sorted[]; 0 behind the last.  All threads; the list is as it was.
-__device__ void sort_top(Shared &s, int count, int n)
-{
-    __syncthreads();
-    if ((int)threadIdx.x < n) s.sorted[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < count; i += kThreads) {
-        const unsigned long long mine = s.list[i];
-        int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < count; ++j) rank += s.list[j] > mine;   // (keys differ: each holds its token)
-        if (rank < n) s.sorted[rank] = mine;
-    }
-    __syncthreads();
-}
-
-// The n-th largest of the threads' values (n <= kThreads).
-__device__ float nth_most(Shared &s, float mine, int n)
-{
-    __syncthreads();
-    s.most[threadIdx.x] = mine;
-    __syncthreads();
-    int above = 0, same = 0;
-#pragma unroll 4
-    for (int j = 0; j < kThreads; j += 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(s.most + j);
-        above += (v.x > mine) + (v.y > mine) + (v.z > mine) + (v.w > mine);
-        same += (v.x == mine) + (v.y == mine) + (v.z == mine) + (v.w == mine);
-    }
-    if (above < n && n <= above + same) s.bound = mine;   // every thread that gets here has the same value
-    __syncthreads();
-    return s.bound;
-}
-
-// A value that n of the threads' values reach at least, and seldom many more: of the n / 4-th largest of each wavefront the least.
-__device__ float reached_by(Shared &s, float mine, int n)
+// The n-th largest of the lanes' values (n <= 64).
+__device__ __forceinline__ float nth_of_lanes(float mine, int n)
 {
     unsigned left = order_bits(mine), least = 0;
-    for (int j = 0; j < n; j += kWaves) {
+    for (int j = 0; j < n; ++j) {
         least = wave_max(left);
         const unsigned long long have = __ballot(left == least);
         if ((int)(threadIdx.x & 63) == __builtin_ctzll(have)) left = 0;
     }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s.bounds[threadIdx.x >> 6] = from_order_bits(least);
-    __syncthreads();
-    float v = s.bounds[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) v = fminf(v, s.bounds[w]);
-    return v;
+    return from_order_bits(least);
 }
 
-// Alternatives of a row (split) that has NaN: n rounds over it.
-template <int TYPE> __device__ void sort_slowly(const LogArgs &a, const typename Entry<TYPE>::bits *z, int begin, int end, int n, Shared &s)
+// Alternatives of a row (split) that has NaN, or whose lists did not have the room: n rounds over it.
+template <int TYPE> __device__ void sort_slowly(const typename Entry<TYPE>::bits *z, int begin, int end, int n, Shared &s)
 {
     typedef Entry<TYPE> E;
-    unsigned long long last = ~0ull;
+    Key last = ~0ull;
     for (int j = 0; j < n; ++j) {
-        unsigned long long mine = 0;
+        Key mine = 0;
         for (int v = begin + threadIdx.x; v < end; v += kThreads) {
-            const unsigned long long key = key_of(E::get(z[v]), v);
+            const Key key = key_of(E::get(z[v]), v);
             if (key < last && key > mine) mine = key;
         }
         __syncthreads();
-        s.list[threadIdx.x] = mine;
+        s.list[0][threadIdx.x] = mine;
         __syncthreads();
         for (int half = kThreads / 2; half > 0; half /= 2) {
-            if ((int)threadIdx.x < half && s.list[threadIdx.x + half] > s.list[threadIdx.x]) s.list[threadIdx.x] = s.list[threadIdx.x + half];
+            if ((int)threadIdx.x < half && s.list[0][threadIdx.x + half] > s.list[0][threadIdx.x]) s.list[0][threadIdx.x] = s.list[0][threadIdx.x + half];
             __syncthreads();
         }
-        last = s.list[0];
+        last = s.list[0][0];
         if (threadIdx.x == 0) s.sorted[j] = last;
     }
     __syncthreads();
 }
 
 // The last step: results of a row from its state and its alternatives in sorted[].
-template <int TYPE> __device__ void finish(const LogArgs &a, int64_t r, float most, float sum, float weighted, const Shared &s)
+template <int TYPE> __device__ void finish(const LogArgs &a, int64_t r, float most, float sum, float weighted, const Key *sorted)
 {
     typedef Entry<TYPE> E;
     const typename E::bits *z = static_cast<const typename E::bits *>(a.z) + r * a.stride;
@@ -145,7 +123,7 @@ template <int TYPE> __device__ void finish(const LogArgs &a, int64_t r, float mo
         a.of_token[i] = token < 0 || token >= a.V ? kNan : E::get(z[token]) - most - log_sum;
     }
     if ((int)threadIdx.x < a.top) {
-        const int token = token_of(s.sorted[threadIdx.x]);
+        const int token = token_of(sorted[threadIdx.x]);
         a.top_ids[r * a.top + threadIdx.x] = token;
         a.of_top[r * a.top + threadIdx.x] = E::get(z[token]) - most - log_sum;
     }
@@ -157,33 +135,44 @@ k_logprobs(const LogArgs a)
 {
     typedef Entry<TYPE> E;
     typedef typename E::bits bits;
-    constexpr int V = 16 / sizeof(bits);
+    constexpr int V = 16 / sizeof(bits), kChunk = 64 * V * VECTORS;
     typedef bits piece __attribute__((ext_vector_type(V)));
     __shared__ Shared s;
     const int64_t r = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.y, begin = split * a.length, end = min(begin + a.length, a.V), n = min(a.top, end - begin);
     const bits *z = static_cast<const bits *>(a.z) + r * a.stride;
     const bits nothing = E::put(-INFINITY);
-    if (TOP && threadIdx.x == 0) s.count = 0;
+    const float lowest = TYPE == TST_F16 ? -65504.f : TYPE == TST_BF16 ? -0x1.fep127f : -0x1.fffffep127f;   // of the type
 
-    float most = -INFINITY, sum = 0.f, weighted = 0.f;   // of the thread
-    float bound = -INFINITY;                             // n logits at least reach it (or all there were)
-    float lost = -INFINITY;                              // some that are equal to this are not in the list ...
-    bool any_lost = false;                               // ... if this is set
-    bool first = true;
-    for (int v0 = begin; v0 < end; v0 += kThreads * V * VECTORS) {
-        piece x[VECTORS];
-        auto place = [&](int i) { return v0 + (i * kThreads + (int)threadIdx.x) * V; };
+    float most = -INFINITY, sum = 0.f, weighted = 0.f;   // of the lane
+    // Of the wavefront: n of its logits at least reach the bound (or all it has had); what is larger than `lost` and belongs to
+    // its n largest is in the list, what is equal to it may not be, if any is lost.
+    float bound = -INFINITY, lost = -INFINITY;
+    bool any_lost = false, slow = false;
+    int count = 0;   // of the list
+    Key *const list = s.list[wave];
+
+    auto load = [&](int v0, piece (&to)[VECTORS]) {
+        if (a.wide && v0 + kChunk <= end) {
 #pragma unroll
-        for (int i = 0; i < VECTORS; ++i) {
-            const int v = place(i);
-            if (a.wide && v + V <= end) {
-                x[i] = *reinterpret_cast<const piece *>(z + v);
-            } else {
+            for (int i = 0; i < VECTORS; ++i) to[i] = *reinterpret_cast<const piece *>(z + v0 + (i * 64 + lane) * V);
+        } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) x[i][j] = v + j < end ? z[v + j] : nothing;
-            }
+            for (int i = 0; i < VECTORS; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const int v = v0 + (i * 64 + lane) * V + j;
+                    to[i][j] = v < end ? z[v] : nothing;
+                }
         }
+    };
+    piece x[VECTORS], next[VECTORS];
+    int v0 = begin + wave * kChunk;
+    if (v0 < end) load(v0, x);
+    for (; v0 < end; v0 += kWaves * kChunk) {
+        if (v0 + kWaves * kChunk < end) load(v0 + kWaves * kChunk, next);
+        __builtin_amdgcn_sched_barrier(0);   // or the compiler moves the loads behind the work that hides them
         float of_vector[VECTORS], here = -INFINITY;
 #pragma unroll
         for (int i = 0; i < VECTORS; ++i) {
@@ -209,69 +198,111 @@ k_logprobs(const LogArgs a)
                 weighted = fmaf(f, fmaxf(d, -150.f), weighted);   // e^-150 is 0 here; -infinity would make 0 times it NaN
             }
         if constexpr (TOP) {
-            // Few threads reach the bound of earlier chunks: what they have goes into the list.  Else a bound of this one's.
-            if (first || __syncthreads_count(here >= bound) > n) bound = fmaxf(bound, reached_by(s, here, n));
-            first = false;
-            // Few vectors reach the bound; they are read again, from the L2, rather than looked for in the registers.
+            // Few lanes reach the bound of earlier chunks: what they have goes into the list.  Else a bound of this one's.
+            const bool first = v0 == begin + wave * kChunk;
+            const int reach = first ? 64 : __popcll(__ballot(here >= bound));
+            if (reach > n) bound = fmaxf(bound, nth_of_lanes(here, n));
             auto collect = [&](bool strict) {
-                if (here < bound) return;
 #pragma unroll
-                for (int i = 0; i < VECTORS; ++i)
-                    if (of_vector[i] >= bound)
-                        for (int j = 0, v = place(i); j < V && v < end; ++j, ++v) {
-                            const float y = E::get(z[v]);
-                            if (strict ? y > bound : y >= bound) {
-                                const int at = atomicAdd(&s.count, 1);
-                                if (at < kList) s.list[at] = key_of(y, v);
-                            }
-                        }
+                for (int i = 0; i < VECTORS; ++i) {
+                    if (__ballot(of_vector[i] >= bound) == 0) continue;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float y = E::get(x[i][j]);
+                        const int v = v0 + (i * 64 + lane) * V + j;
+                        const bool take = (strict ? y > bound : y >= bound) && v < end;
+                        const unsigned long long set = __ballot(take);
+                        const int at = count + __popcll(set & ((1ull << lane) - 1));
+                        if (take && at < kRoom) list[at] = key_of(y, v);
+                        count += __popcll(set);
+                    }
+                }
             };
-            const int held = s.count;
-            __syncthreads();
-            collect(false);
-            __syncthreads();
-            if (s.count > kShort) {
-                // Too many: logits that tie at the bound (masked ones above all), a bound too low, or much from earlier chunks.  The list
-                // keeps its `n` largest, and of this chunk all that pass the n-th largest of the threads' maxima; fewer than n threads
-                // have any.  What is equal to it is lost for now.
-                sort_top(s, held, n);
-                if ((int)threadIdx.x < n) s.list[threadIdx.x] = s.sorted[threadIdx.x];
-                if (threadIdx.x == 0) s.count = min(held, n);
-                bound = fmaxf(bound, nth_most(s, here, n));   // (meets)
-                collect(true);
-                __syncthreads();
-                if (!any_lost || bound > lost) lost = bound;
-                any_lost = true;
+            if (reach > 0) {
+                const bool masked = bound <= lowest;   // most of the chunk is: none of that goes into the list
+                const int held = count;
+                collect(masked);
+                if (masked) {
+                    lost = bound;
+                    any_lost = true;
+                }
+                if (count > kShort) {
+                    // Too many: logits that tie at the bound, rising ones, or much from earlier chunks.  The list keeps its n largest,
+                    // and of this chunk what passes the bound; what is equal to it is lost for now.
+                    order_wave();
+                    rank_keys(list, held, s.best[wave], n, lane, 64);
+                    order_wave();
+                    count = min(held, n);
+                    if (lane < count) list[lane] = s.best[wave][lane];
+                    bound = fmaxf(bound, nth_of_lanes(here, n));
+                    collect(true);
+                    if (!any_lost || bound > lost) lost = bound;
+                    any_lost = true;
+                    if (count > kRoom) {
+                        slow = true;
+                        count = 0;
+                    }
+                }
             }
         }
+#pragma unroll
+        for (int i = 0; i < VECTORS; ++i) x[i] = next[i];
     }
     const float all = over_waves(most, s.sums[0], [](float x, float y) { return fmaxf(x, y); });
     const float d = most - all, f = most > -INFINITY ? __builtin_amdgcn_exp2f(d * 1.44269504f) : 0.f;
     const bool spoilt = sum != sum;
     weighted = f > 0.f ? (weighted + d * sum) * f : 0.f;
     sum = spoilt ? kNan : f > 0.f ? sum * f : 0.f;
-    __syncthreads();
-    sum = over_waves(sum, s.sums[0], [](float x, float y) { return x + y; });
-    weighted = over_waves(weighted, s.sums[1], [](float x, float y) { return x + y; });
     if constexpr (TOP) {
-        if (sum != sum) {
-            sort_slowly<TYPE>(a, z, begin, end, n, s);
+        order_wave();
+        if (lane < n) s.best[wave][lane] = 0;
+        order_wave();
+        rank_keys(list, count, s.best[wave], n, lane, 64);
+        if (lane == 0) {
+            s.lost[wave] = lost;
+            s.flags[wave] = (any_lost ? 1 : 0) | (slow ? 2 : 0);
+        }
+    }
+    sum = over_waves(sum, s.sums[1], [](float x, float y) { return x + y; });
+    weighted = over_waves(weighted, s.sums[2], [](float x, float y) { return x + y; });
+    if constexpr (TOP) {
+        int flags = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            flags |= s.flags[w];
+            if (s.flags[w] & 1) lost = fmaxf(lost, s.lost[w]);
+        }
+        if (sum != sum || (flags & 2)) {
+            sort_slowly<TYPE>(z, begin, end, n, s);
         } else {
-            sort_top(s, s.count, n);
+            // the wavefronts' n largest behind one another
+            __syncthreads();
+            Key *const together = s.list[0];
+            if ((int)threadIdx.x < n) s.sorted[threadIdx.x] = 0;
+            if (lane < n) together[wave * n + lane] = s.best[wave][lane];
+            __syncthreads();
+            const Key mine = (int)threadIdx.x < kWaves * n ? together[threadIdx.x] : 0;
+            if (mine) {
+                int rank = 0;
+#pragma unroll 4
+                for (int j = 0; j < kWaves * n; ++j) rank += together[j] > mine;
+                if (rank < n) s.sorted[rank] = mine;
+            }
+            __syncthreads();
             // What was lost counts if fewer than n lie above it: then the lowest tokens with that logit follow them.
-            if (any_lost) {
+            if (flags & 1) {
                 const unsigned edge = order_bits(lost);
                 int found = __syncthreads_count((int)threadIdx.x < n && (unsigned)(s.sorted[threadIdx.x] >> 32) > edge);
-                for (int v0 = begin; v0 < end && found < n; v0 += kThreads) {
-                    const int v = v0 + threadIdx.x;
+                for (int t0 = begin; t0 < end && found < n; t0 += kThreads) {
+                    const int v = t0 + threadIdx.x;
                     const bool tie = v < end && E::get(z[v]) == lost;
                     const unsigned long long set = __ballot(tie);
                     __syncthreads();
-                    if ((threadIdx.x & 63) == 0) s.counts[threadIdx.x >> 6] = __popcll(set);
+                    if (lane == 0) s.counts[wave] = __popcll(set);
                     __syncthreads();
-                    int before = found + __popcll(set & ((1ull << (threadIdx.x & 63)) - 1));
+                    int before = found + __popcll(set & ((1ull << lane) - 1));
                     for (int w = 0; w < kWaves; ++w) {
-                        if (w < (int)(threadIdx.x >> 6)) before += s.counts[w];
+                        if (w < wave) before += s.counts[w];
                         found += s.counts[w];
                     }
                     if (tie && before < n) s.sorted[before] = key_of(lost, v);
@@ -281,7 +312,7 @@ k_logprobs(const LogArgs a)
         }
     }
     if (a.splits == 1) {
-        finish<TYPE>(a, r, all, sum, weighted, s);
+        finish<TYPE>(a, r, all, sum, weighted, s.sorted);
         return;
     }
     const int64_t part = r * a.splits + split;
@@ -291,15 +322,18 @@ k_logprobs(const LogArgs a)
 
 // k_logprobs_join: a row from its splits.  Each brings its alternatives in order: of the first ceil(top / splits) of each, the top-th
 // largest is a bound again, and only what reaches it is sorted.
+constexpr int kMaxSplits = 32;
+
 template <int TYPE>
 __global__ void __launch_bounds__(kThreads)
 k_logprobs_join(const LogArgs a)
 {
-    __shared__ Shared s;
+    __shared__ Key list[kMaxSplits * kMaxTop], sorted[kMaxTop];
+    __shared__ int count;
     const int64_t r = blockIdx.x;
     const int lane = threadIdx.x & 63;
     float most = -INFINITY, sum = 0.f, weighted = 0.f;
-    if (lane < a.splits) {   // (every wavefront for itself; at most 32 splits)
+    if (lane < a.splits) {   // (every wavefront for itself)
         const float4 v = a.states[r * a.splits + lane];
         most = v.x;
         sum = v.y;
@@ -317,25 +351,28 @@ k_logprobs_join(const LogArgs a)
         weighted += __shfl_xor(weighted, d);
     }
     if (a.top > 0) {
-        const unsigned long long *keys = a.keys + r * a.splits * a.top;
+        const Key *keys = a.keys + r * a.splits * a.top;
         const int heads = blocks_of(a.top, a.splits), n = heads * a.splits;   // (below top + splits)
-        if ((int)threadIdx.x < n) s.list[threadIdx.x] = keys[threadIdx.x / heads * a.top + threadIdx.x % heads];
-        sort_top(s, n, a.top);
-        const unsigned long long bound = s.sorted[a.top - 1];   // 0: some splits hold fewer
-        if (threadIdx.x == 0) s.count = 0;
+        if ((int)threadIdx.x < n) list[threadIdx.x] = keys[threadIdx.x / heads * a.top + threadIdx.x % heads];
+        if ((int)threadIdx.x < a.top) sorted[threadIdx.x] = 0;
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+        rank_keys(list, n, sorted, a.top, threadIdx.x, kThreads);
+        __syncthreads();
+        const Key bound = sorted[a.top - 1];   // 0: some splits hold fewer
         __syncthreads();
         for (int i = threadIdx.x; i < a.splits * a.top; i += kThreads) {
-            const unsigned long long key = keys[i];
-            if (key && key >= bound) s.list[atomicAdd(&s.count, 1)] = key;
+            const Key key = keys[i];
+            if (key && key >= bound) list[atomicAdd(&count, 1)] = key;   // (in any order: they are sorted)
         }
         __syncthreads();
-        sort_top(s, s.count, a.top);
+        rank_keys(list, count, sorted, a.top, threadIdx.x, kThreads);
+        __syncthreads();
     }
-    finish<TYPE>(a, r, all, sum, weighted, s);
+    finish<TYPE>(a, r, all, sum, weighted, sorted);
 }
 
-// Splits of a row: while there are fewer than two workgroups for a compute unit, of a chunk at least.
-constexpr int kMaxSplits = 32;
+// Splits of a row: while there are fewer than two workgroups for a compute unit, of a chunk for each wavefront at least.
 int splits_of(int R, int V, int type)
 {
     const int64_t least = (int64_t)kThreads * kFewVectors * (16 / type_bytes(type));
