@@ -146,10 +146,10 @@ k_logprobs(const LogArgs a)
     const float lowest = TYPE == TST_F16 ? -65504.f : TYPE == TST_BF16 ? -0x1.fep127f : -0x1.fffffep127f;   // of the type
 
     float most = -INFINITY, sum = 0.f, weighted = 0.f;   // of the lane
-    // Of the wavefront: n of its logits at least reach the bound (or all it has had); what is larger than `lost` and belongs to
-    // its n largest is in the list, what is equal to it may not be, if any is lost.
+    // Of the wavefront: n of its logits at least reach the bound (or all it has had); closed: the list has n that do.  What is larger
+    // than `lost` and belongs to its n largest is in the list, what is equal to it may not be, if any is lost.
     float bound = -INFINITY, lost = -INFINITY;
-    bool any_lost = false, slow = false;
+    bool closed = false, any_lost = false, slow = false;
     int count = 0;   // of the list
     Key *const list = s.list[wave];
 
@@ -198,10 +198,6 @@ k_logprobs(const LogArgs a)
                 weighted = fmaf(f, fmaxf(d, -150.f), weighted);   // e^-150 is 0 here; -infinity would make 0 times it NaN
             }
         if constexpr (TOP) {
-            // Few lanes reach the bound of earlier chunks: what they have goes into the list.  Else a bound of this one's.
-            const bool first = v0 == begin + wave * kChunk;
-            const int reach = first ? 64 : __popcll(__ballot(here >= bound));
-            if (reach > n) bound = fmaxf(bound, nth_of_lanes(here, n));
             auto collect = [&](bool strict) {
 #pragma unroll
                 for (int i = 0; i < VECTORS; ++i) {
@@ -212,35 +208,57 @@ k_logprobs(const LogArgs a)
                         const int v = v0 + (i * 64 + lane) * V + j;
                         const bool take = (strict ? y > bound : y >= bound) && v < end;
                         const unsigned long long set = __ballot(take);
+                        if (set == 0) continue;
                         const int at = count + __popcll(set & ((1ull << lane) - 1));
                         if (take && at < kRoom) list[at] = key_of(y, v);
                         count += __popcll(set);
                     }
                 }
             };
+            auto keep_largest = [&](int of) {   // of the list's first
+                order_wave();
+                rank_keys(list, of, s.best[wave], n, lane, 64);
+                order_wave();
+                count = min(of, n);
+                if (lane < count) list[lane] = s.best[wave][lane];
+            };
+            // Few lanes reach what the list holds: that goes into it.  Else what n lanes of this chunk reach is a better bound.
+            const int reach = closed ? __popcll(__ballot(here > bound)) : 64;
+            if (reach > n) {
+                const float better = nth_of_lanes(here, n);
+                if (!closed || better > bound) {
+                    bound = fmaxf(bound, better);
+                    closed = false;
+                }
+            }
             if (reach > 0) {
-                const bool masked = bound <= lowest;   // most of the chunk is: none of that goes into the list
+                const bool masked = bound <= lowest && !closed;   // most of the chunk is: none of that goes into the list
                 const int held = count;
-                collect(masked);
+                collect(closed || masked);
                 if (masked) {
                     lost = bound;
                     any_lost = true;
                 }
                 if (count > kShort) {
-                    // Too many: logits that tie at the bound, rising ones, or much from earlier chunks.  The list keeps its n largest,
-                    // and of this chunk what passes the bound; what is equal to it is lost for now.
-                    order_wave();
-                    rank_keys(list, held, s.best[wave], n, lane, 64);
-                    order_wave();
-                    count = min(held, n);
-                    if (lane < count) list[lane] = s.best[wave][lane];
+                    // Too many: logits that tie at the bound, or rising ones.  Of this chunk the list takes what passes the n-th largest
+                    // of the lanes' maxima; what is equal to it is lost for now.
+                    keep_largest(held);
                     bound = fmaxf(bound, nth_of_lanes(here, n));
+                    closed = false;
                     collect(true);
                     if (!any_lost || bound > lost) lost = bound;
                     any_lost = true;
                     if (count > kRoom) {
                         slow = true;
                         count = 0;
+                    }
+                }
+                if (count > n + 16 || (count >= n && !closed)) {
+                    keep_largest(count);
+                    const float nth = from_order_bits((unsigned)(s.best[wave][n - 1] >> 32));
+                    if (nth >= bound) {
+                        bound = nth;
+                        closed = true;   // what comes later in the row and is equal to it comes behind it
                     }
                 }
             }
