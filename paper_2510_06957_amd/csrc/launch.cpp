@@ -6,17 +6,14 @@
 // device, a shape that does not fit, a dispatch or function mode, a call that the library refuses -- and the caller goes the long
 // way, which refuses what it refuses with the message that belongs to it.  An error of the GPU, which kernels of the call may have
 // gone before, is raised here: nothing is launched twice.
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <ATen/ops/empty.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPFunctions.h>
-#include <c10/hip/HIPStream.h>
+#include "launch_internal.h"
 
 #include "tstgemm.h"
 
 namespace {
+
+using launch::int_attr;
+using launch::WithoutGil;
 
 typedef int (*Gemm)(const float *, const void *, const float *, float *, int, int, int, void *);
 typedef int (*Prelu)(const float *, const void *, const float *, const float *, int, float *, int, int, int, void *);
@@ -26,20 +23,6 @@ Gemm g_entry[kEntries];
 Prelu g_prelu;
 PyObject *g_error;   // TstgemmError
 PyObject *s_raw, *s_n, *s_device_index, *s_cuda_stream;
-
-// An attribute that is an int; false (no error set) if it is not there or something else.
-bool int_attr(PyObject *o, PyObject *name, unsigned long long *out)
-{
-    PyObject *v = PyObject_GetAttr(o, name);
-    const bool ok = v != nullptr && PyLong_CheckExact(v);
-    if (ok) *out = PyLong_AsUnsignedLongLong(v);
-    Py_XDECREF(v);
-    if (PyErr_Occurred()) {
-        PyErr_Clear();
-        return false;
-    }
-    return ok;
-}
 
 // A float32 tensor with memory of its own on device `dev`, contiguous, of torch's own class.
 const at::Tensor *plain(PyObject *o, int dev)
@@ -52,13 +35,8 @@ const at::Tensor *plain(PyObject *o, int dev)
     return &t;
 }
 
-struct WithoutGil {
-    PyThreadState *state = PyEval_SaveThread();
-    ~WithoutGil() { PyEval_RestoreThread(state); }
-};
-
 // launch(entry, X, t, b, Y, stream, alpha) -> Y or None
-PyObject *launch(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+PyObject *launch_product(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     if (n_args != 7) {
         PyErr_SetString(PyExc_TypeError, "launch(entry, X, t, b, Y, stream, alpha)");
@@ -67,8 +45,8 @@ PyObject *launch(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     try {
         const long entry = PyLong_AsLong(a[0]);
         unsigned long long raw = 0, n = 0, index = 0, stream = 0;
-        if (entry < 0 || entry >= kEntries || g_prelu == nullptr || at::impl::PythonTorchFunctionTLS::stack_len() > 0 ||
-            c10::impl::TorchDispatchModeTLS::any_modes_set() || !int_attr(a[2], s_raw, &raw) || !int_attr(a[2], s_n, &n) ||
+        if (entry < 0 || entry >= kEntries || g_prelu == nullptr || launch::modes_set() ||
+            !int_attr(a[2], s_raw, &raw) || !int_attr(a[2], s_n, &n) ||
             !int_attr(a[2], s_device_index, &index))
             Py_RETURN_NONE;
         const at::Tensor *x = plain(a[1], (int)index);
@@ -143,7 +121,7 @@ PyObject *bind(PyObject *, PyObject *args)
 }
 
 PyMethodDef methods[] = {
-    {"launch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(launch)), METH_FASTCALL, nullptr},
+    {"launch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(launch_product)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -156,7 +134,8 @@ PyMODINIT_FUNC PyInit__launch()
     s_n = PyUnicode_InternFromString("N");
     s_device_index = PyUnicode_InternFromString("device_index");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    PyObject *module = PyModule_Create(&module_def);
+    PyObject *module = launch::ops_init() ? PyModule_Create(&module_def) : nullptr;
+    if (module != nullptr && PyModule_AddFunctions(module, launch::ops_methods) < 0) Py_CLEAR(module);
     // what it reads of a tensor is laid out as in the torch it was built for
     if (module != nullptr && PyModule_AddStringConstant(module, "torch_version", BUILT_FOR_TORCH) < 0) Py_CLEAR(module);
     return module;

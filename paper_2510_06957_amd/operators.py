@@ -8,6 +8,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 
+from . import binding
 from .binding import TstgemmError, _launch_stream, _load
 
 TST_F32, TST_BF16, TST_F16 = 0, 1, 2
@@ -25,16 +26,23 @@ _SIGNATURES = {
     "tst_logprobs": [_vp, _ci, _i64, _vp, _ci, _ci, _ci, _vp, _vp, _vp, _vp, _ci, _ci, _vp, _sz, _vp],
 }
 _lib = None
+_native = None   # the native half (csrc/launch_ops.cpp): calls with plain tensors that bring nothing but their operands
 
 
 def _ops():
-    global _lib
+    global _lib, _native
     if _lib is None:
         lib = _load()
         for name, args in _SIGNATURES.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, ctypes.c_int
         _lib = lib
+        if binding._launch is not None:   # built, and for this torch
+            from . import _launch as native
+            native.bind_ops(*(ctypes.cast(getattr(lib, name), _vp).value for name in (
+                "tst_w8_gemm", "tst_w8_linear_workspace_bytes", "tst_w8_linear", "tst_moe_workspace_bytes", "tst_moe",
+                "tst_logprobs_workspace_bytes", "tst_logprobs")), TstgemmError)
+            _native = native
     return _lib
 
 
@@ -171,6 +179,10 @@ def tst_quantize(X, Q=None, scale=None, stream=None):
 def tst_w8_gemm(Q, scale, w: W8, b=None, Y=None, dtype=None, stream=None):
     """Y = (Q W) scale[:, None] w.scale + b: Q int8 [M, K] with rows on 16-byte borders (as tst_quantize leaves them), scale float32
     [M], w from tst_w8_pack, b float32 [N] or None.  dtype of Y: float32 unless another or Y itself is given."""
+    if _native is not None and Y is None and stream is None:
+        done = _native.w8_gemm(Q, scale, w, b, dtype)
+        if done is not None:
+            return done
     import torch
     M, K, stride = _rows(Q, "Q", torch.int8)
     dev = Q.get_device()
@@ -190,6 +202,10 @@ def tst_w8_gemm(Q, scale, w: W8, b=None, Y=None, dtype=None, stream=None):
 
 def tst_w8_linear(X, w: W8, b=None, Y=None, workspace=None, stream=None):
     """tst_w8_gemm() of tst_quantize(X): X [M, K] float32, bfloat16 or float16, Y of the same type."""
+    if _native is not None and Y is None and workspace is None and stream is None:
+        done = _native.w8_linear(X, w, b)
+        if done is not None:
+            return done
     M, K, stride = _rows(X, "X")
     kind, dev = _type(X.dtype, "X"), X.get_device()
     b_ptr = _layer(w, b, dev)
@@ -215,6 +231,7 @@ class Moe:
         self.E, self.D, self.F, self.dtype, self.device_index = E, D, F, dtype, device_index
         self._tensors, self._struct = tensors, struct   # the struct holds the tensors' addresses
         self._ref = ctypes.byref(struct)
+        self._raw = ctypes.addressof(struct)   # for the native half
 
 
 def tst_moe_pack(router, gate, gate_scale, up, up_scale, down, down_scale, stream=None) -> Moe:
@@ -248,6 +265,10 @@ def tst_moe_pack(router, gate, gate_scale, up, up_scale, down, down_scale, strea
 def tst_moe(X, moe: Moe, top_k: int, normalize=True, Y=None, ids=None, p=None, workspace=None, stream=None):
     """The layer for tokens X [T, D] of the router's type: (Y [T, D], ids int32 [T, top_k], p float32 [T, top_k]).  normalize: the
     chosen experts' weights add up to one, else they are those of the softmax over all experts."""
+    if _native is not None and Y is None and ids is None and p is None and workspace is None and stream is None:
+        done = _native.moe(X, moe, top_k, normalize)
+        if done is not None:
+            return done
     import torch
     T, D, stride = _rows(X, "X", moe.dtype)
     dev = X.get_device()
@@ -267,6 +288,10 @@ def tst_moe(X, moe: Moe, top_k: int, normalize=True, Y=None, ids=None, p=None, w
 def tst_logprobs(logits, tokens=None, top=0, workspace=None, stream=None):
     """Log probabilities in rows of logits [R, V] float32, bfloat16 or float16: (of_token, entropy [R], top_ids int32 [R, top],
     of_top [R, top]).  tokens: int32 or int64 [R] or [R, C]; of_token has their shape, [R, 0] without any."""
+    if _native is not None and workspace is None and stream is None:
+        done = _native.logprobs(logits, tokens, top)
+        if done is not None:
+            return done
     import torch
     R, V, stride = _rows(logits, "logits")
     kind, dev = _type(logits.dtype, "logits"), logits.get_device()
