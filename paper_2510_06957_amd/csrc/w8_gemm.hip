@@ -8,8 +8,8 @@ namespace {
 // ------------------------------------------------------------------------------------------------------------------
 // k_quantize: one workgroup per row; the row's largest magnitude, then its codes.  Magnitudes are compared as integers: of
 // non-negative floats the bits order as the values do, with infinity and NaN above every number.
-// The row stays in the registers on the way if it fits (kQuantPieces pieces of 16 bytes for a thread), else it is read twice.
-constexpr int kQuantThreads = 256, kQuantPieces = 4;
+// The row stays in the registers on the way if it fits (64 bytes for a thread), else it is read twice.
+constexpr int kQuantBytes = 64;
 
 // What a row's codes are made with, from the bits of its largest magnitude.
 struct Scaling {
@@ -25,40 +25,34 @@ struct Scaling {
     __device__ __forceinline__ unsigned code(float x) const { return finite ? (unsigned)(int)rintf(x * factor) & 0xffu : 0u; }
 };
 
-// WIDE: rows of X on 16-byte borders, rows of Q on borders of a piece's codes
-template <int TYPE, bool WIDE>
-__global__ void __launch_bounds__(kQuantThreads)
+// WIDE: rows of X on 16-byte borders, rows of Q on borders of a piece's codes, K a multiple of a piece; else an entry at a time.
+template <int TYPE, bool WIDE, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 k_quantize(const typename Entry<TYPE>::bits *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int K)
 {
     typedef Entry<TYPE> E;
     typedef typename E::bits bits;
-    constexpr int V = 16 / sizeof(bits);
+    constexpr int V = WIDE ? 16 / sizeof(bits) : 1, kPieces = kQuantBytes / sizeof(bits) / V;
     typedef bits piece __attribute__((ext_vector_type(V)));
-    __shared__ unsigned most[kQuantThreads / 64];
+    __shared__ unsigned most[THREADS / 64];
     const int64_t m = blockIdx.x;
     const bits *x = X + m * x_stride;
     int8_t *q = Q + m * q_stride;
-    piece v[kQuantPieces];
+    piece v[kPieces];
     auto load = [&](int k0) {
 #pragma unroll
-        for (int p = 0; p < kQuantPieces; ++p) {
-            const int k = k0 + (p * kQuantThreads + threadIdx.x) * V;
+        for (int p = 0; p < kPieces; ++p) {
+            const int k = k0 + (p * THREADS + threadIdx.x) * V;
             v[p] = piece{};
-            if (WIDE && k + V <= K) {
-                v[p] = *reinterpret_cast<const piece *>(x + k);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (k + i < K) v[p][i] = x[k + i];
-            }
+            if (k < K) v[p] = *reinterpret_cast<const piece *>(x + k);
         }
     };
-    constexpr int kRound = kQuantPieces * kQuantThreads * V;
+    constexpr int kRound = kPieces * THREADS * V;
     unsigned a = 0;
     for (int k0 = 0; k0 < K; k0 += kRound) {
         load(k0);
 #pragma unroll
-        for (int p = 0; p < kQuantPieces; ++p)
+        for (int p = 0; p < kPieces; ++p)
 #pragma unroll
             for (int i = 0; i < V; ++i) a = max(a, __float_as_uint(E::get(v[p][i])) & 0x7fffffffu);
     }
@@ -66,24 +60,23 @@ k_quantize(const typename Entry<TYPE>::bits *X, int64_t x_stride, int8_t *Q, int
     if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = a;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kQuantThreads / 64; ++w) a = max(a, most[w]);
+    for (int w = 0; w < THREADS / 64; ++w) a = max(a, most[w]);
     const Scaling by(a);
     if (threadIdx.x == 0) scale[m] = by.scale;
     for (int k0 = 0; k0 < K; k0 += kRound) {
         if (K > kRound) load(k0);
 #pragma unroll
-        for (int p = 0; p < kQuantPieces; ++p) {
-            const int k = k0 + (p * kQuantThreads + threadIdx.x) * V;
-            unsigned out[V / 4] = {};
+        for (int p = 0; p < kPieces; ++p) {
+            const int k = k0 + (p * THREADS + threadIdx.x) * V;
+            if (k >= K) continue;
+            if constexpr (V == 1) {
+                q[k] = (int8_t)by.code(E::get(v[p][0]));
+            } else {
+                unsigned out[V / 4] = {};
 #pragma unroll
-            for (int i = 0; i < V; ++i) out[i / 4] |= by.code(E::get(v[p][i])) << (8 * (i % 4));
-            if (WIDE && k + V <= K) {
+                for (int i = 0; i < V; ++i) out[i / 4] |= by.code(E::get(v[p][i])) << (8 * (i % 4));
                 if constexpr (V == 8) *reinterpret_cast<u32x2 *>(q + k) = u32x2{out[0], out[1]};
                 else *reinterpret_cast<unsigned *>(q + k) = out[0];
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (k + i < K) q[k + i] = (int8_t)(out[i / 4] >> (8 * (i % 4)));
             }
         }
     }
@@ -530,9 +523,14 @@ hipError_t launch_quantize(const void *X, int type, int64_t x_stride, int8_t *Q,
     return for_type(type, [&](auto t) {
         typedef typename Entry<decltype(t)::value>::bits bits;
         constexpr int T = decltype(t)::value, V = 16 / sizeof(bits);
-        const bool wide = aligned(X, 16) && x_stride % V == 0 && aligned(Q, V) && q_stride % V == 0;
-        if (wide) k_quantize<T, true><<<M, kQuantThreads, 0, stream>>>(static_cast<const bits *>(X), x_stride, Q, q_stride, scale, K);
-        else k_quantize<T, false><<<M, kQuantThreads, 0, stream>>>(static_cast<const bits *>(X), x_stride, Q, q_stride, scale, K);
+        const bool wide = aligned(X, 16) && K % V == 0 && x_stride % V == 0 && aligned(Q, V) && q_stride % V == 0;
+        const bits *x = static_cast<const bits *>(X);
+        // few rows get more threads each (1 x 16385 fp16 5 us in place of 20)
+        const bool few = M < compute_units();
+        if (wide && few) k_quantize<T, true, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
+        else if (wide) k_quantize<T, true, 256><<<M, 256, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
+        else if (few) k_quantize<T, false, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
+        else k_quantize<T, false, 256><<<M, 256, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
         return hipGetLastError();
     });
 }
