@@ -501,12 +501,16 @@ k_moe_join(const MoeArgs a)
 
 // Workgroups that share the experts of a column tile, so that every compute unit has one; each has at least one block for a wavefront.
 constexpr int kMaxSplits = 16;
+int most_splits(int D)
+{
+    const int wanted = blocks_of(compute_units(), blocks_of(D, 16 * kDownCols));
+    return wanted < kMaxSplits ? wanted : kMaxSplits;
+}
 int down_splits(int T, int D, int F, int top)
 {
-    const int tiles = blocks_of(D, 16 * kDownCols);
-    const int64_t wanted = blocks_of(compute_units(), tiles), blocks = (int64_t)blocks_of(F, 64) * (T < 4 ? top : 2 * top);
+    const int64_t blocks = (int64_t)blocks_of(F, 64) * (T < 4 ? top : 2 * top);   // (experts in use are not known here)
     const int64_t useful = (blocks + kDownWaves - 1) / kDownWaves;
-    return (int)(wanted < useful ? (wanted < kMaxSplits ? wanted : kMaxSplits) : (useful < kMaxSplits ? useful : kMaxSplits));
+    return useful < most_splits(D) ? (int)useful : most_splits(D);
 }
 
 struct MoeSpace {
@@ -527,7 +531,7 @@ MoeSpace moe_space(const tst_moe_t &m, int T, int top)
     take(s.count, sizeof(int32_t));
     take(s.used, in_use * sizeof(int32_t));
     take(s.places, in_use * (size_t)((T + 63) / 64 * 64));
-    take(s.partial, (size_t)kMaxSplits * T * m.width * sizeof(float));
+    take(s.partial, most_splits(m.width) > 1 ? (size_t)most_splits(m.width) * T * m.width * sizeof(float) : 0);
     return s;
 }
 

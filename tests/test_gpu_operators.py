@@ -241,7 +241,7 @@ def moe_reference(X, w, k, normalize, dtype):
 
 
 MOE = [(1, 1, 1, 1, 1), (1, 2, 1, 64, 64), (1, 8, 2, 256, 512), (2, 5, 5, 70, 33), (5, 12, 3, 153, 129), (16, 16, 4, 128, 64),
-       (17, 7, 2, 200, 100), (33, 70, 6, 96, 48), (64, 4, 1, 64, 130), (70, 130, 8, 65, 31), (3, 512, 16, 40, 20)]
+       (17, 7, 2, 200, 100), (33, 70, 6, 96, 48), (64, 4, 1, 64, 130), (70, 130, 8, 65, 31), (3, 512, 16, 40, 20), (60, 512, 2, 33, 17), (2, 3, 2, 17000, 16), (1, 4, 2, 64, 5000)]
 
 
 @pytest.mark.parametrize("T,E,k,D,F", MOE)
@@ -467,6 +467,61 @@ def test_no_tokens():
     out = tg.tst_logprobs(e((0, 50), device="cuda"), e((0, 2), dtype=torch.int64, device="cuda"), top=3)
     assert [tuple(o.shape) for o in out] == [(0, 2), (0,), (0, 3), (0, 3)]
     torch.cuda.synchronize()
+
+
+def test_plain_calls_go_through_the_native_half():
+    """... and give what the long way gives, which takes over whatever is not plain."""
+    from paper_2510_06957_amd import operators
+    W, t, b, w = layer(700, 300, 51)
+    bd, X = torch.from_numpy(b).cuda(), tokens(6, 700, "f16", 52, 720)
+    Q, s = tg.tst_quantize(X)
+    moe, x = packed(experts(9, 128, 96, "bf16", 53)), tokens(5, 128, "bf16", 54, 131)
+    z, token = logits(4, 3000, "f32", 55, 3004), torch.tensor([[5, 2999], [7, 1], [0, 0], [2, -1]], dtype=torch.int32, device="cuda")
+    native = operators._native
+    assert native is not None
+    here = torch.cuda.current_stream()
+    for fast, slow in ((native.w8_linear(X, w, bd), tg.tst_w8_linear(X, w, bd, stream=here)), (native.w8_linear(X, w, None), tg.tst_w8_linear(X, w, stream=here)),
+                       (native.w8_gemm(Q, s, w, bd, torch.bfloat16), tg.tst_w8_gemm(Q, s, w, bd, dtype=torch.bfloat16, stream=here)),
+                       (native.w8_gemm(Q, s, w, None, None), tg.tst_w8_gemm(Q, s, w, stream=here)),
+                       (native.moe(x, moe, 3, True), tg.tst_moe(x, moe, 3, stream=here)), (native.moe(x, moe, 9, False), tg.tst_moe(x, moe, 9, False, stream=here)),
+                       (native.logprobs(z, token, 7), tg.tst_logprobs(z, token, 7, stream=here)), (native.logprobs(z, None, 0), tg.tst_logprobs(z, stream=here)),
+                       (native.logprobs(z, token[:, 0].contiguous().long(), 1), tg.tst_logprobs(z, token[:, 0].contiguous().long(), 1, stream=here))):
+        assert fast is not None
+        for a, c in zip(as_list(fast), as_list(slow)):
+            assert a.dtype == c.dtype and a.shape == c.shape and torch.equal(torch.nan_to_num(a.float(), 77), torch.nan_to_num(c.float(), 77))
+    for none in (native.w8_linear(X.double(), w, bd), native.w8_linear(X.t(), w, bd), native.w8_linear(X[:, :600], w, bd), native.w8_linear(X, moe, bd),
+                 native.w8_linear(X, w, s), native.w8_linear(X.cpu(), w, bd), native.w8_linear(None, w, bd), native.w8_gemm(Q, s, w, bd, torch.int8),
+                 native.w8_gemm(Q, s[:3], w, bd, None), native.w8_gemm(Q, s, w, bd, "f32"), native.w8_gemm(X, s, w, bd, None),
+                 native.w8_gemm(Q.contiguous(), s, w, bd, None), native.moe(x.float(), moe, 3, True), native.moe(x, w, 3, True), native.moe(x, moe, 10, True),
+                 native.moe(x, moe, 3.0, True), native.moe(x, moe, 3, 1), native.logprobs(z, token.float(), 7), native.logprobs(z, token[:3], 7),
+                 native.logprobs(z, token, 65), native.logprobs(z, token.t(), 7), native.logprobs(z[0], None, 1)):
+        assert none is None
+    with pytest.raises(TypeError):
+        native.moe(x, moe)
+    with torch.utils._python_dispatch.TorchDispatchMode():
+        assert native.w8_linear(X, w, bd) is None
+
+
+def test_large_strides():
+    """Rows far apart, up to what the product takes; and offsets that pass 32 bits."""
+    W, t, b, w = layer(96, 40, 56)
+    far = torch.empty(700 * (1 << 22), dtype=torch.int8, device="cuda")          # 2.9 GB
+    rows = far.view(700, 1 << 22)[:, :96]
+    Q = torch.from_numpy(rng(57).integers(-128, 128, (700, 96)).astype(np.int8)).cuda()
+    s = torch.ones(700, device="cuda")
+    rows.copy_(Q)
+    near = torch.zeros((700, 96), dtype=torch.int8, device="cuda").copy_(Q)
+    for M in (1, 5, 40, 200, 700):
+        assert torch.equal(tg.tst_w8_gemm(rows[:M], s[:M], w), tg.tst_w8_gemm(near[:M], s[:M], w))
+    with pytest.raises(tg.TstgemmError):
+        tg.tst_w8_gemm(far[:(1 << 23) + 32].view(2, (1 << 22) + 16)[:, :96], s[:2], w)
+    x = far.view(torch.bfloat16).view(700, 1 << 21)[:, :96]
+    x.copy_(Q.bfloat16())
+    y = near.bfloat16()
+    assert torch.equal(tg.tst_w8_linear(x, w), tg.tst_w8_linear(y, w))
+    assert all(torch.equal(a, c) for a, c in zip(tg.tst_logprobs(x, top=3), tg.tst_logprobs(y, top=3)))
+    moe = packed(experts(5, 96, 32, "bf16", 58))
+    assert all(torch.equal(a, c) for a, c in zip(tg.tst_moe(x[632:], moe, 2), tg.tst_moe(y[632:], moe, 2)))
 
 
 def test_given_results_and_workspaces():

@@ -115,3 +115,17 @@ def test_the_binding_refuses_what_is_not_on_a_gpu():
         tg.tst_w8_pack(x.to(torch.int8), torch.ones(64))
     with pytest.raises(ValueError):
         tg.tst_logprobs(x)
+
+
+def test_the_native_half_hands_back_what_is_not_on_a_gpu():
+    import torch
+    operators._ops()
+    native = operators._native
+    assert native is not None
+    x = torch.zeros((2, 64))
+    w = tg.W8(64, 32, 1, torch.zeros(2048, dtype=torch.uint8), torch.ones(32))
+    assert native.w8_linear(x, w, None) is None and native.w8_gemm(x.to(torch.int8), torch.ones(2), w, None, None) is None
+    assert native.moe(x, None, 2, True) is None and native.logprobs(x, None, 1) is None
+    for call in (lambda: native.w8_linear(x), lambda: native.w8_gemm(x), lambda: native.moe(x), lambda: native.logprobs(x)):
+        with pytest.raises(TypeError):
+            call()
