@@ -5,8 +5,8 @@
 // mantissas off (x = p0 + p1 + p2, p0 the upper 16 bits of x, p1 those of x - p0, ...): one plane holds a bf16 entry, two an fp16
 // entry, three an fp32 entry, all exactly, so that products are exact and only the fp32 sums round.
 //
-// The tokens are the columns of a matrix instruction (16 at a time) and the weights its rows: up to 16 tokens cost the matrix cores the same, and
-// a token that has not chosen an expert is a column that is not used (first product) or zero (second).
+// The tokens that chose an expert are the columns of a matrix instruction, 16 at a time, and the weights its rows: up to 16 tokens cost
+// the matrix cores the same.  Columns without a token hold anything and are not used; a column's values stay in it.
 #include "ops_internal.h"
 
 namespace tst {
@@ -35,7 +35,7 @@ struct MoeArgs {
     u32x4 *h;        // operands of h, a row for each token and expert it chose, zero behind F
     int32_t *count;  // experts in use
     int32_t *used;   // they, ascending
-    uint8_t *places; // [nth][16 NT] rank of the nth expert in use among a token's, or 255
+    uint16_t *members;   // [nth][16 NT] of the nth expert in use, as in Chosen
     float *partial;  // [split][T][D]
     int splits;
 };
@@ -106,19 +106,24 @@ k_moe_router(const MoeArgs a)
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Which tokens chose which expert, in the LDS behind the workgroup's own: place[e][t] = rank of expert e among token t's, or 255.
+// Which tokens chose which expert, in the LDS behind the workgroup's own: the members of expert e, their tokens ascending, stand in
+// of(e, 0), of(e, 1), ... as token | rank of e among the token's << 8, and kNobody behind the last.
+constexpr unsigned kNobody = 0xffff;
+__device__ __forceinline__ int token_of(unsigned member) { return member & 0xff; }
+__device__ __forceinline__ int rank_of(unsigned member) { return member >> 8; }
+
 template <int NT> struct Chosen {
     static constexpr int kTokens = 16 * NT;
-    uint8_t *place;     // [E][kTokens]
+    uint16_t *members;  // [E][kTokens]; while they are chosen, entry t is token t's
     float *p;           // [T][top]
     uint16_t *active;   // experts that some token chose, ascending
     __device__ Chosen(char *lds, const MoeArgs &a)
-        : place(reinterpret_cast<uint8_t *>(lds)), p(reinterpret_cast<float *>(lds + a.E * kTokens)),
+        : members(reinterpret_cast<uint16_t *>(lds)), p(reinterpret_cast<float *>(members + a.E * kTokens)),
           active(reinterpret_cast<uint16_t *>(p + a.T * a.top))
     {
     }
-    static size_t bytes(const MoeArgs &a) { return (size_t)a.E * kTokens + (size_t)a.T * a.top * sizeof(float) + (size_t)a.E * sizeof(uint16_t); }
-    __device__ int of(int e, int token) const { return place[e * kTokens + token]; }
+    static size_t bytes(const MoeArgs &a) { return (size_t)a.E * kTokens * sizeof(uint16_t) + (size_t)a.T * a.top * sizeof(float) + (size_t)a.E * sizeof(uint16_t); }
+    __device__ unsigned of(int e, int i) const { return members[e * kTokens + i]; }
 };
 
 // A wavefront finds a token's experts: top rounds of the largest of what is left; lane l holds experts l, l + 64, ...
@@ -164,7 +169,7 @@ __device__ void choose_experts(const MoeArgs &a, const Chosen<NT> &c, int t, int
         chosen += w;
         if (lane == j) mine = w;
         if (lane == 0) {
-            c.place[e * c.kTokens + t] = (uint8_t)j;
+            c.members[e * c.kTokens + t] = (uint16_t)(t | j << 8);
             if (write) a.ids[t * a.top + j] = e;
         }
     }
@@ -175,29 +180,37 @@ __device__ void choose_experts(const MoeArgs &a, const Chosen<NT> &c, int t, int
     }
 }
 
-template <int NT> __device__ __forceinline__ void clear_places(const MoeArgs &a, const Chosen<NT> &c)
+template <int NT> __device__ __forceinline__ void clear_members(const MoeArgs &a, const Chosen<NT> &c)
 {
-    unsigned *w = reinterpret_cast<unsigned *>(c.place);
-    for (int i = threadIdx.x; i < a.E * c.kTokens / 4; i += blockDim.x) w[i] = 0xffffffffu;
+    unsigned *w = reinterpret_cast<unsigned *>(c.members);
+    for (int i = threadIdx.x; i < a.E * c.kTokens / 2; i += blockDim.x) w[i] = 0xffffffffu;
     __syncthreads();
 }
 
-// The list of experts in use; every wavefront counts them, the first one writes them down.
+// The list of experts in use, which every wavefront counts and the first one writes down, and each expert's members moved together.
 template <int NT> __device__ int list_active(const MoeArgs &a, const Chosen<NT> &c)
 {
     int n = 0;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     for (int e0 = 0; e0 < a.E; e0 += 64) {
         const int e = e0 + lane;
         bool any = false;
         if (e < a.E) {
-            const u32x4 *w = reinterpret_cast<const u32x4 *>(c.place + e * c.kTokens);
+            const u32x4 *w = reinterpret_cast<const u32x4 *>(c.members + e * c.kTokens);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) any |= (w[i][0] & w[i][1] & w[i][2] & w[i][3]) != 0xffffffffu;
+            for (int i = 0; i < 2 * NT; ++i) any |= (w[i][0] & w[i][1] & w[i][2] & w[i][3]) != 0xffffffffu;
         }
         const unsigned long long set = __ballot(any);
-        if (any && threadIdx.x < 64) c.active[n + __popcll(set & ((1ull << lane) - 1))] = (uint16_t)e;
+        if (any && wave == 0) c.active[n + __popcll(set & ((1ull << lane) - 1))] = (uint16_t)e;
         n += __popcll(set);
+    }
+    __syncthreads();
+    for (int i = wave; i < n; i += waves) {
+        uint16_t *row = c.members + c.active[i] * c.kTokens;
+        const unsigned m = lane < c.kTokens ? row[lane] : kNobody;
+        const unsigned long long set = __ballot(m != kNobody);
+        if (m != kNobody) row[__popcll(set & ((1ull << lane) - 1))] = (uint16_t)m;   // (all have read; never behind where it stood)
+        if (lane < c.kTokens && lane >= __popcll(set)) row[lane] = kNobody;
     }
     __syncthreads();
     return n;
@@ -244,7 +257,7 @@ k_moe_up(const MoeArgs a)
     extern __shared__ u32x4 lds_behind[];
     const Chosen<NT> c(reinterpret_cast<char *>(lds_behind), a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    clear_places(a, c);
+    clear_members(a, c);
     for (int t = wave; t < a.T; t += kUpWaves) {
         if (a.E <= 64) choose_experts<1>(a, c, t, lane, blockIdx.x == 0);
         else choose_experts<kMaxE / 64>(a, c, t, lane, blockIdx.x == 0);
@@ -270,12 +283,12 @@ k_moe_up(const MoeArgs a)
         b.up = *reinterpret_cast<const u32x4 *>(a.up + at);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int token = 16 * t + (lane & 15);
-            if (token < a.T && c.of(e, token) != 255) {   // the other columns are not used, whatever they hold
+            const unsigned m = c.of(e, 16 * t + (lane & 15));
+            if (m != kNobody) {   // the other columns are not used, whatever they hold
 #pragma unroll
                 for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) b.x[p][s][t] = a.x[(size_t)(((kb * P + p) * 2 + s) * 4 + (lane >> 4)) * a.T + token];
+                    for (int s = 0; s < 2; ++s) b.x[p][s][t] = a.x[(size_t)(((kb * P + p) * 2 + s) * 4 + (lane >> 4)) * a.T + token_of(m)];
             }
         }
     };
@@ -287,11 +300,15 @@ k_moe_up(const MoeArgs a)
     if (blockIdx.x == gridDim.x - 1) {   // for k_moe_down
         if (threadIdx.x == 0) *a.count = n_active;
         for (int i = threadIdx.x; i < n_active; i += kUpWaves * 64) a.used[i] = c.active[i];
-        for (int i = threadIdx.x; i < n_active * c.kTokens; i += kUpWaves * 64) a.places[i] = c.place[c.active[i / c.kTokens] * c.kTokens + i % c.kTokens];
+        for (int i = threadIdx.x; i < n_active * c.kTokens; i += kUpWaves * 64) a.members[i] = (uint16_t)c.of(c.active[i / c.kTokens], i % c.kTokens);
     }
     int buffer = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         f32x4 acc[2][NT] = {};
+        int tiles = 1;   // of 16 members
+#pragma unroll
+        for (int t = 1; t < NT; ++t)
+            if (__builtin_amdgcn_readfirstlane((int)c.of(c.active[item / cols], 16 * t)) != (int)kNobody) tiles = t + 1;
         for (int round = 0; round < rounds; ++round) {
             const bool last = round == rounds - 1;
 #pragma unroll
@@ -302,7 +319,8 @@ k_moe_up(const MoeArgs a)
                     widen(b.gate, wg);
                     widen(b.up, wu);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t) {
+                        if (t >= tiles) break;
 #pragma unroll
                         for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -311,21 +329,24 @@ k_moe_up(const MoeArgs a)
                                 acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wg[s], xf, acc[0][t], 0, 0, 0);
                                 acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wu[s], xf, acc[1][t], 0, 0, 0);
                             }
+                    }
                 }
                 load(last ? item + gridDim.x : item, last ? 0 : round + 1, u, b);
             }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            if (t >= tiles) break;
             part[buffer][wave][0][t][lane] = acc[0][t];
             part[buffer][wave][1][t][lane] = acc[1][t];
         }
         meet();
-        for (int i = threadIdx.x; i < NT * 64; i += kUpWaves * 64) {
+        for (int i = threadIdx.x; i < tiles * 64; i += kUpWaves * 64) {
             const int e = c.active[item / cols], nb = item % cols;
-            const int t = i >> 6, l = i & 63, token = 16 * t + (l & 15);
-            const int place = token < a.T ? c.of(e, token) : 255;
-            if (place == 255) continue;
+            const int t = i >> 6, l = i & 63;
+            const unsigned m = c.of(e, 16 * t + (l & 15));
+            if (m == kNobody) continue;
+            const int row = token_of(m) * a.top + rank_of(m);
             f32x4 g = part[buffer][0][0][t][l], u = part[buffer][0][1][t][l];
 #pragma unroll
             for (int w = 1; w < kUpWaves; ++w) {
@@ -339,7 +360,7 @@ k_moe_up(const MoeArgs a)
                 float h = 0.f;
                 if (f + r < a.F) {
                     const float gv = g[r] * a.gate_scale[(size_t)e * a.F + f + r], uv = u[r] * a.up_scale[(size_t)e * a.F + f + r];
-                    h = gv / (1.f + expf(-gv)) * uv * c.p[token * a.top + place];
+                    h = gv / (1.f + expf(-gv)) * uv * c.p[row];
                 }
 #pragma unroll
                 for (int p = 0; p < PH; ++p) out[p][r] = p < PH - 1 ? cut(h) : Entry<TST_BF16>::put(h);   // the last one rounds
@@ -347,7 +368,7 @@ k_moe_up(const MoeArgs a)
             const int kb = f >> 6, quarter = (f >> 4) & 3, half = (f >> 3) & 1;
 #pragma unroll
             for (int p = 0; p < PH; ++p) {
-                u32x4 *to = a.h + (size_t)(((kb * PH + p) * 2 + half) * 4 + quarter) * (a.T * a.top) + token * a.top + place;
+                u32x4 *to = a.h + (size_t)(((kb * PH + p) * 2 + half) * 4 + quarter) * (a.T * a.top) + row;
                 reinterpret_cast<u32x2 *>(to)[(f >> 2) & 1] = u32x2{out[p][0] | (unsigned)out[p][1] << 16, out[p][2] | (unsigned)out[p][3] << 16};
             }
         }
@@ -385,8 +406,8 @@ k_moe_down(const MoeArgs a)
         e = __builtin_amdgcn_readfirstlane(a.used[nth]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int token = 16 * t + (lane & 15), place = a.places[nth * 16 * NT + token];
-            row[t] = place == 255 ? -1 : token * a.top + place;
+            const unsigned m = a.members[nth * 16 * NT + 16 * t + (lane & 15)];
+            row[t] = m == kNobody ? -1 : token_of(m) * a.top + rank_of(m);
         }
     };
     auto load = [&](Block &b) {
@@ -400,7 +421,6 @@ k_moe_down(const MoeArgs a)
             for (int p = 0; p < PH; ++p)
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    b.h[p][s][t] = u32x4{};
                     if (row[t] >= 0) b.h[p][s][t] = a.h[(size_t)(((kb * PH + p) * 2 + s) * 4 + (lane >> 4)) * (a.T * a.top) + row[t]];
                 }
         ++next;
@@ -410,12 +430,19 @@ k_moe_down(const MoeArgs a)
         }
     };
     f32x4 acc[kDownCols][NT] = {};
-    int left = 0, nth = 0;   // the expert whose sums are in acc, and its blocks to come
+    int left = 0, nth = 0, tiles = 1;   // the expert whose sums are in acc: its blocks to come, its tiles of 16 members
+    auto count_tiles = [&]() {
+        tiles = 1;
+#pragma unroll
+        for (int t = 1; t < NT; ++t)
+            if (a.members[(nth * NT + t) * 16] != kNobody) tiles = t + 1;
+    };
     if (begin < end) {
         nth = begin / k_blocks;
         kb = begin % k_blocks;
         left = k_blocks - kb;
         enter(nth);
+        count_tiles();
     }
     auto settle = [&]() {
         const float *scale = a.down_scale + (size_t)a.used[nth] * a.D;
@@ -426,10 +453,13 @@ k_moe_down(const MoeArgs a)
             for (int r = 0; r < 4; ++r) by[r] = scale[min((nb0 + j) * 16 + 4 * (lane >> 4) + r, a.D - 1)];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                f32x4 v = part[wave][j][t][lane];
+                if (t >= tiles) break;
+                const unsigned m = a.members[nth * 16 * NT + 16 * t + (lane & 15)];
+                if (m != kNobody) {
+                    f32x4 &v = part[wave][j][token_of(m) >> 4][(lane & 48) | (token_of(m) & 15)];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = fmaf(by[r], acc[j][t][r], v[r]);
-                part[wave][j][t][lane] = v;
+                    for (int r = 0; r < 4; ++r) v[r] = fmaf(by[r], acc[j][t][r], v[r]);
+                }
                 acc[j][t] = f32x4{};
             }
         }
@@ -450,18 +480,23 @@ k_moe_down(const MoeArgs a)
                 bf16x8 wd[2];
                 widen(b.w[j], wd);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    if (t >= tiles) break;
 #pragma unroll
                     for (int p = 0; p < PH; ++p)
 #pragma unroll
                         for (int s = 0; s < 2; ++s)
                             acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, b.h[p][s][t]), acc[j][t], 0, 0, 0);
+                }
             }
             load(b);
             if (--left == 0) {
                 settle();
                 left = k_blocks;
-                ++nth;
+                if (at + u + 1 < end) {
+                    ++nth;
+                    count_tiles();
+                }
             }
         }
     }
@@ -514,7 +549,7 @@ int down_splits(int T, int D, int F, int top)
 }
 
 struct MoeSpace {
-    size_t logits, x, h, count, used, places, partial, total;
+    size_t logits, x, h, count, used, members, partial, total;
 };
 MoeSpace moe_space(const tst_moe_t &m, int T, int top)
 {
@@ -530,7 +565,7 @@ MoeSpace moe_space(const tst_moe_t &m, int T, int top)
     take(s.h, (size_t)h_planes_of(m.type) * T * top * pad64(m.inner) * 2);
     take(s.count, sizeof(int32_t));
     take(s.used, in_use * sizeof(int32_t));
-    take(s.places, in_use * (size_t)((T + 63) / 64 * 64));
+    take(s.members, in_use * kMaxTokens * sizeof(uint16_t));
     take(s.partial, most_splits(m.width) > 1 ? (size_t)most_splits(m.width) * T * m.width * sizeof(float) : 0);
     return s;
 }
@@ -599,7 +634,7 @@ int tst_moe(const void *X, int64_t x_stride, const tst_moe_t *moe, int top_k, in
                              static_cast<char *>(Y) + t0 * m.width * entry, ids + t0 * top_k, p + t0 * top_k, m.experts, m.width, m.inner, n,
                              top_k, normalize != 0, wide, reinterpret_cast<float *>(ws + s.logits), reinterpret_cast<tst::u32x4 *>(ws + s.x),
                              reinterpret_cast<tst::u32x4 *>(ws + s.h), reinterpret_cast<int32_t *>(ws + s.count), reinterpret_cast<int32_t *>(ws + s.used),
-                             reinterpret_cast<uint8_t *>(ws + s.places), reinterpret_cast<float *>(ws + s.partial),
+                             reinterpret_cast<uint16_t *>(ws + s.members), reinterpret_cast<float *>(ws + s.partial),
                              tst::down_splits(n, m.width, m.inner, top_k)};
         const hipError_t e = tst::for_type(m.type, [&](auto type) {
             constexpr int TYPE = decltype(type)::value;
