@@ -248,12 +248,13 @@ __device__ __forceinline__ void meet()
 constexpr int kUpWaves = 8;
 
 template <int TYPE, int NT>
-__global__ void __launch_bounds__(kUpWaves * 64, NT == 1 ? 4 : 2)
+__global__ void __launch_bounds__(kUpWaves * 64, NT == 1 || planes_of(TYPE) == 1 ? 4 : 2)
 k_moe_up(const MoeArgs a)
 {
-    constexpr int P = planes_of(TYPE), PH = h_planes_of(TYPE), U = P * NT == 1 ? 4 : P * NT <= 4 ? 2 : 1;
-    constexpr int kBuffers = NT == 1 ? 2 : 1;
-    __shared__ f32x4 part[kBuffers][kUpWaves][2][NT][64];
+    constexpr int P = planes_of(TYPE), PH = h_planes_of(TYPE);
+    constexpr int AHEAD = NT == 1 ? 1 : 2;   // tiles of members whose X is requested ahead; few experts have more
+    constexpr int U = NT == 1 ? (P == 1 ? 4 : 2) : NT == 4 && P == 1 ? 2 : 3;
+    __shared__ f32x4 part[2][kUpWaves][2][64];
     extern __shared__ u32x4 lds_behind[];
     const Chosen<NT> c(reinterpret_cast<char *>(lds_behind), a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -268,13 +269,14 @@ k_moe_up(const MoeArgs a)
     const unsigned column = k_blocks * kW8Piece;
 
     struct Block {
-        u32x4 gate, up, x[P][2][NT];
+        u32x4 gate, up, x[P][2][AHEAD];
     } block[U];
     // Block u of a round of an item; blocks that are not there (behind D, of padded columns, of no item) are left as they are
     // and not multiplied.
     auto there = [&](int item, int round, int u) {
         return item < items && item % cols < real_cols && (round * U + u) * kUpWaves + wave < k_blocks;
     };
+    auto operand = [&](int kb, int p, int s, unsigned m) { return a.x[(size_t)(((kb * P + p) * 2 + s) * 4 + (lane >> 4)) * a.T + token_of(m)]; };
     auto load = [&](int item, int round, int u, Block &b) {
         if (!there(item, round, u)) return;
         const int e = __builtin_amdgcn_readfirstlane(c.active[item / cols]), kb = (round * U + u) * kUpWaves + wave;
@@ -282,14 +284,13 @@ k_moe_up(const MoeArgs a)
         b.gate = *reinterpret_cast<const u32x4 *>(a.gate + at);
         b.up = *reinterpret_cast<const u32x4 *>(a.up + at);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < AHEAD; ++t) {
             const unsigned m = c.of(e, 16 * t + (lane & 15));
-            if (m != kNobody) {   // the other columns are not used, whatever they hold
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) b.x[p][s][t] = a.x[(size_t)(((kb * P + p) * 2 + s) * 4 + (lane >> 4)) * a.T + token_of(m)];
-            }
+                for (int s = 0; s < 2; ++s)
+                    if (m != kNobody) b.x[p][s][t] = operand(kb, p, s, m);   // the other columns are not used, whatever they hold
         }
     };
 #pragma unroll
@@ -302,6 +303,37 @@ k_moe_up(const MoeArgs a)
         for (int i = threadIdx.x; i < n_active; i += kUpWaves * 64) a.used[i] = c.active[i];
         for (int i = threadIdx.x; i < n_active * c.kTokens; i += kUpWaves * 64) a.members[i] = (uint16_t)c.of(c.active[i / c.kTokens], i % c.kTokens);
     }
+    // h of a tile of members and an item, from the sums of the wavefronts.
+    auto finish = [&](int item, int t, int buffer) {
+        const int e = c.active[item / cols], nb = item % cols;
+        const unsigned m = c.of(e, 16 * t + (lane & 15));
+        if (m == kNobody) return;
+        const int row = token_of(m) * a.top + rank_of(m);
+        f32x4 g = part[buffer][0][0][lane], u = part[buffer][0][1][lane];
+#pragma unroll
+        for (int w = 1; w < kUpWaves; ++w) {
+            g += part[buffer][w][0][lane];
+            u += part[buffer][w][1][lane];
+        }
+        const int f = nb * 16 + 4 * (lane >> 4);
+        uint16_t out[PH][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float h = 0.f;
+            if (f + r < a.F) {
+                const float gv = g[r] * a.gate_scale[(size_t)e * a.F + f + r], uv = u[r] * a.up_scale[(size_t)e * a.F + f + r];
+                h = gv / (1.f + expf(-gv)) * uv * c.p[row];
+            }
+#pragma unroll
+            for (int p = 0; p < PH; ++p) out[p][r] = p < PH - 1 ? cut(h) : Entry<TST_BF16>::put(h);   // the last one rounds
+        }
+        const int kb = f >> 6, quarter = (f >> 4) & 3, half = (f >> 3) & 1;
+#pragma unroll
+        for (int p = 0; p < PH; ++p) {
+            u32x4 *to = a.h + (size_t)(((kb * PH + p) * 2 + half) * 4 + quarter) * (a.T * a.top) + row;
+            reinterpret_cast<u32x2 *>(to)[(f >> 2) & 1] = u32x2{out[p][0] | (unsigned)out[p][1] << 16, out[p][2] | (unsigned)out[p][3] << 16};
+        }
+    };
     int buffer = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         f32x4 acc[2][NT] = {};
@@ -321,11 +353,15 @@ k_moe_up(const MoeArgs a)
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         if (t >= tiles) break;
+                        const unsigned m = t < AHEAD ? 0 : c.of(c.active[item / cols], 16 * t + (lane & 15));
 #pragma unroll
                         for (int p = 0; p < P; ++p)
 #pragma unroll
                             for (int s = 0; s < 2; ++s) {
-                                const bf16x8 xf = __builtin_bit_cast(bf16x8, b.x[p][s][t]);
+                                u32x4 x = {};
+                                if (t < AHEAD) x = b.x[p][s][t < AHEAD ? t : 0];
+                                else if (m != kNobody) x = operand((round * U + u) * kUpWaves + wave, p, s, m);
+                                const bf16x8 xf = __builtin_bit_cast(bf16x8, x);
                                 acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wg[s], xf, acc[0][t], 0, 0, 0);
                                 acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wu[s], xf, acc[1][t], 0, 0, 0);
                             }
@@ -335,45 +371,14 @@ k_moe_up(const MoeArgs a)
             }
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (t >= tiles) break;
-            part[buffer][wave][0][t][lane] = acc[0][t];
-            part[buffer][wave][1][t][lane] = acc[1][t];
+        for (int t = 0; t < NT; ++t) {   // a tile of members after another, through two buffers: what stands in one was read before the
+            if (t >= tiles) break;       // meeting that lets the other be read
+            part[buffer][wave][0][lane] = acc[0][t];
+            part[buffer][wave][1][lane] = acc[1][t];
+            meet();
+            if (wave == 0) finish(item, t, buffer);
+            buffer ^= 1;
         }
-        meet();
-        for (int i = threadIdx.x; i < tiles * 64; i += kUpWaves * 64) {
-            const int e = c.active[item / cols], nb = item % cols;
-            const int t = i >> 6, l = i & 63;
-            const unsigned m = c.of(e, 16 * t + (l & 15));
-            if (m == kNobody) continue;
-            const int row = token_of(m) * a.top + rank_of(m);
-            f32x4 g = part[buffer][0][0][t][l], u = part[buffer][0][1][t][l];
-#pragma unroll
-            for (int w = 1; w < kUpWaves; ++w) {
-                g += part[buffer][w][0][t][l];
-                u += part[buffer][w][1][t][l];
-            }
-            const int f = nb * 16 + 4 * (l >> 4);
-            uint16_t out[PH][4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float h = 0.f;
-                if (f + r < a.F) {
-                    const float gv = g[r] * a.gate_scale[(size_t)e * a.F + f + r], uv = u[r] * a.up_scale[(size_t)e * a.F + f + r];
-                    h = gv / (1.f + expf(-gv)) * uv * c.p[row];
-                }
-#pragma unroll
-                for (int p = 0; p < PH; ++p) out[p][r] = p < PH - 1 ? cut(h) : Entry<TST_BF16>::put(h);   // the last one rounds
-            }
-            const int kb = f >> 6, quarter = (f >> 4) & 3, half = (f >> 3) & 1;
-#pragma unroll
-            for (int p = 0; p < PH; ++p) {
-                u32x4 *to = a.h + (size_t)(((kb * PH + p) * 2 + half) * 4 + quarter) * (a.T * a.top) + row;
-                reinterpret_cast<u32x2 *>(to)[(f >> 2) & 1] = u32x2{out[p][0] | (unsigned)out[p][1] << 16, out[p][2] | (unsigned)out[p][3] << 16};
-            }
-        }
-        if (kBuffers == 1) meet();
-        else buffer ^= 1;   // what stands in the other one was read before the meeting
     }
 }
 
@@ -390,7 +395,8 @@ __global__ void __launch_bounds__(kDownWaves * 64, 2)
 k_moe_down(const MoeArgs a)
 {
     typedef Entry<TYPE> E;
-    constexpr int PH = h_planes_of(TYPE), U = NT == 1 ? 6 - PH : NT == 2 ? 2 : 1;
+    constexpr int PH = h_planes_of(TYPE), U = NT == 1 ? 6 - PH : 2;
+    constexpr int AHEAD = NT > 1 && PH == 2 ? 2 : 1;   // tiles of members whose h is requested ahead; few experts have more
     __shared__ f32x4 part[kDownWaves][kDownCols][NT][64];   // of the experts that a wavefront is done with
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.y, nb0 = blockIdx.x * kDownCols;
@@ -399,30 +405,32 @@ k_moe_down(const MoeArgs a)
     const int begin = min((split * kDownWaves + wave) * share, total), end = min(begin + share, total);
 
     struct Block {
-        u32x4 w[kDownCols], h[PH][2][NT];
+        u32x4 w[kDownCols], h[PH][2][AHEAD];
+        int kb;
     } block[U];
-    int e = 0, kb = 0, next = begin, row[NT];   // of the block to be requested next; row: of h, or -1
+    int e = 0, kb = 0, next = begin, row[AHEAD];   // of the block to be requested next; row: of h, or -1
     auto enter = [&](int nth) {
         e = __builtin_amdgcn_readfirstlane(a.used[nth]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < AHEAD; ++t) {
             const unsigned m = a.members[nth * 16 * NT + 16 * t + (lane & 15)];
             row[t] = m == kNobody ? -1 : token_of(m) * a.top + rank_of(m);
         }
     };
+    auto operand = [&](int kb, int p, int s, int row) { return a.h[(size_t)(((kb * PH + p) * 2 + s) * 4 + (lane >> 4)) * (a.T * a.top) + row]; };
     auto load = [&](Block &b) {
         if (next >= end) return;
 #pragma unroll
         for (int j = 0; j < kDownCols; ++j)
             b.w[j] = *reinterpret_cast<const u32x4 *>(a.down + (((size_t)e * n_blocks + min(nb0 + j, n_blocks - 1)) * k_blocks + kb) * kW8Piece + lane * 16);
+        b.kb = kb;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < AHEAD; ++t)
 #pragma unroll
             for (int p = 0; p < PH; ++p)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (row[t] >= 0) b.h[p][s][t] = a.h[(size_t)(((kb * PH + p) * 2 + s) * 4 + (lane >> 4)) * (a.T * a.top) + row[t]];
-                }
+                for (int s = 0; s < 2; ++s)
+                    if (row[t] >= 0) b.h[p][s][t] = operand(kb, p, s, row[t]);
         ++next;
         if (++kb == k_blocks && next < end) {
             kb = 0;
@@ -475,19 +483,24 @@ k_moe_down(const MoeArgs a)
         for (int u = 0; u < U; ++u) {
             Block &b = block[u];
             if (at + u >= end) break;
+            bf16x8 wd[kDownCols][2];
 #pragma unroll
-            for (int j = 0; j < kDownCols; ++j) {
-                bf16x8 wd[2];
-                widen(b.w[j], wd);
+            for (int j = 0; j < kDownCols; ++j) widen(b.w[j], wd[j]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (t >= tiles) break;
+            for (int t = 0; t < NT; ++t) {
+                if (t >= tiles) break;
+                const unsigned m = t < AHEAD ? 0 : a.members[nth * 16 * NT + 16 * t + (lane & 15)];
 #pragma unroll
-                    for (int p = 0; p < PH; ++p)
+                for (int p = 0; p < PH; ++p)
 #pragma unroll
-                        for (int s = 0; s < 2; ++s)
-                            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[s], __builtin_bit_cast(bf16x8, b.h[p][s][t]), acc[j][t], 0, 0, 0);
-                }
+                    for (int s = 0; s < 2; ++s) {
+                        u32x4 h = {};
+                        if (t < AHEAD) h = b.h[p][s][t < AHEAD ? t : 0];
+                        else if (m != kNobody) h = operand(b.kb, p, s, token_of(m) * a.top + rank_of(m));
+#pragma unroll
+                        for (int j = 0; j < kDownCols; ++j)
+                            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wd[j][s], __builtin_bit_cast(bf16x8, h), acc[j][t], 0, 0, 0);
+                    }
             }
             load(b);
             if (--left == 0) {
