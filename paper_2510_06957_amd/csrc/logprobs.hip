@@ -5,6 +5,9 @@
 // sum e^(z - m) and sum e^(z - m) (z - m).  The alternatives come from the same registers: of the lanes' maxima of a chunk, the n-th
 // largest is a lower bound of the row's n-th largest logit, so only what reaches it (seldom much more than n) goes into a list in the
 // LDS, with its place; a member's rank is the number of members before it.
+//
+// Bound by memory and, about as much, by the exponentials: 1024 x 131072 bf16 with one alternative 55 us, 4.9 TB/s, with 20 of them 85.  Few
+// rows are bound by latency: 1 x 131072 with 20 alternatives 10.9 us and 5.7 for joining the splits.
 #include "ops_internal.h"
 
 namespace tst {

@@ -7,7 +7,8 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------------------------
 // k_quantize: one workgroup per row; the row's largest magnitude, then its codes.  Magnitudes are compared as integers: of
-// non-negative floats the bits order as the values do, with infinity and NaN above every number.
+// non-negative floats the bits order as the values do, with infinity and NaN above every number.  Bound by memory for many rows (2048 x
+// 4096 bf16 7.0 us, 3.6 TB/s read and written), by latency for few (37 x 2053 fp16 4.6 us).
 // The row stays in the registers on the way if it fits (64 bytes for a thread), else it is read twice.
 constexpr int kQuantBytes = 64;
 
@@ -154,7 +155,7 @@ __device__ __forceinline__ i32x4 load16(__amdgpu_buffer_rsrc_t from, unsigned la
 // part of the LDS that belongs to the wavefront: an operand wants row l % 16 in lane l, and loads whose neighbouring lanes lie in different
 // rows take the address unit a cycle for each lane (64 x 16384 x 4096: 35 us in place of 18), so 8 lanes load 128 bytes of a row together.
 // Chunk c of 8 of a row stands in slot (row % 16) ^ c, which makes both the writes (8 chunks of a row together) and the reads (16 rows
-// of a chunk together) free of bank conflicts.
+// of a chunk together) free of bank conflicts.  64 x 16384 x 4096 16.4 us (67 MB of weights at 4.1 TB/s), 256 x 4096 x 4096 11.6.
 constexpr int kRowsWaves = 8, kRowsThreads = kRowsWaves * 64, kStepK = 128;
 
 template <int TYPE, int MT, int NT>
@@ -350,7 +351,9 @@ k_w8_few(const GemmArgs a, const typename Entry<TYPE>::bits *X, int64_t x_stride
 // ------------------------------------------------------------------------------------------------------------------
 // k_w8_tiles: 256 columns x 16 MF rows of Y for a workgroup of four wavefronts, 64 columns x all its rows each.  What a wavefront
 // takes of W nobody else in the workgroup needs, so it goes from memory straight into the registers (a piece of the packed form is an
-// operand of the matrix instruction); X goes through the LDS, 128 of K at a time in two buffers, in slots as in k_w8_rows.
+// operand of the matrix instruction); X goes through the LDS, 128 of K at a time in two buffers, in slots as in k_w8_rows.  Bound by what a
+// compute unit can load: 48 KiB a step for 256 x 128 results.  4096 x 8192 x 8192 217 us, 2.53 POP/s (a library's product of this size 236;
+// instructions of 32 x 32 x 32 9 % slower; a tile of 256 x 256 does not fit the registers), 2048 x 4096 x 4096 38 us.
 constexpr int kTileThreads = 256, kTileCols = 256;
 
 template <int TYPE, int MF>
