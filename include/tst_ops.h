@@ -34,7 +34,7 @@ extern "C" {
  * it is NaN in that row and nowhere else.
  * X: DEVICE, M rows of K entries of `type` (TST_*), x_stride entries apart (>= K).  Q: DEVICE, M rows of K bytes, q_stride
  * bytes apart (>= K); only the K bytes of a row are written.  tst_w8_gemm() wants rows on 16-byte borders.  scale: DEVICE, M.
- * M >= 0, K >= 1.  Errors: EINVAL, EHIP.
+ * M >= 0, 1 <= K <= 2^30.  Errors: EINVAL, EHIP.
  */
 int tst_quantize(const void *X, int type, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int M, int K, void *stream);
 
@@ -112,7 +112,7 @@ int tst_moe(const void *X, int64_t x_stride, const tst_moe_t *moe, int top_k, in
  * probabilities are NaN; a token outside 0 .. V-1 has NaN.
  * logits: DEVICE, R rows of V entries of `type`, stride entries apart (>= V).  tokens: DEVICE, R x C, int32 (token_bytes 4) or int64
  * (8); C = 0 for none.  of_token: R x C fp32; entropy: R fp32 or NULL; top_ids: R x top int32; of_top: R x top fp32.
- * R >= 0, V >= 1, 0 <= top <= min(V, 64), 0 <= C <= 64.
+ * R >= 0, 1 <= V <= 2^30, 0 <= top <= min(V, 64), 0 <= C <= 64.
  * workspace: DEVICE, 256-byte aligned, at least tst_logprobs_workspace_bytes() (0 for many rows).
  * Errors: EINVAL, EWORKSPACE, EHIP.
  */

@@ -419,7 +419,7 @@ extern "C" {
 
 int tst_logprobs_workspace_bytes(int R, int V, int top, size_t *bytes)
 {
-    if (!bytes || R < 0 || V < 1 || top < 0 || top > V || top > TST_LOGPROBS_MAX_TOP) return TSTGEMM_EINVAL;
+    if (!bytes || R < 0 || V < 1 || V > 1 << 30 || top < 0 || top > V || top > TST_LOGPROBS_MAX_TOP) return TSTGEMM_EINVAL;
     *bytes = R > 0 && tst::splits_of(R, V, TST_F32) > 1 ? tst::log_space(R, top).total : 0;   // (fp32 rows are split first)
     return TSTGEMM_OK;
 }

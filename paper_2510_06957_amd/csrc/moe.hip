@@ -60,7 +60,7 @@ __device__ __forceinline__ float wave_sum(float v)
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// k_moe_router: a wavefront per (token, expert) for the logits, and the operands of X.  Bound by latency: 4.9 us for 16 tokens and 64 experts
+// k_moe_router: a wavefront per (token, expert) for the logits, and workgroups behind these for the operands of X.  Bound by latency: 4.9 us for 16 tokens and 64 experts
 // of width 2048.
 constexpr int kRouterWaves = 4;
 
@@ -74,7 +74,9 @@ k_moe_router(const MoeArgs a)
     typedef bits piece __attribute__((ext_vector_type(V)));
     const int t = blockIdx.y, lane = threadIdx.x & 63, e = blockIdx.x * kRouterWaves + (threadIdx.x >> 6);
     const bits *x = static_cast<const bits *>(a.X) + t * a.x_stride;
-    if (e < a.E) {
+    const int logit_groups = blocks_of(a.E, kRouterWaves);
+    if ((int)blockIdx.x < logit_groups) {
+        if (e >= a.E) return;
         const bits *r = static_cast<const bits *>(a.router) + (size_t)e * a.D;
         float sum = 0.f;
 #pragma unroll 8
@@ -85,9 +87,11 @@ k_moe_router(const MoeArgs a)
         }
         sum = wave_sum(sum);
         if (lane == 0) a.logits[t * a.E + e] = sum;
+        return;
     }
     constexpr int P = planes_of(TYPE);
-    for (int unit = blockIdx.x * kRouterWaves * 64 + threadIdx.x; unit < pad64(a.D) / 8; unit += gridDim.x * kRouterWaves * 64) {
+    const int unit = ((int)blockIdx.x - logit_groups) * kRouterWaves * 64 + threadIdx.x;
+    if (unit < pad64(a.D) / 8) {
         const int d = unit * 8, kb = unit >> 3, quarter = (unit >> 1) & 3, half = unit & 1;
         uint16_t out[P][8];
 #pragma unroll
@@ -589,7 +593,7 @@ MoeSpace moe_space(const tst_moe_t &m, int T, int top)
 
 template <int TYPE, int NT> hipError_t launch_moe_nt(const MoeArgs &a, hipStream_t stream)
 {
-    const dim3 router(blocks_of(a.E, kRouterWaves), a.T);
+    const dim3 router(blocks_of(a.E, kRouterWaves) + blocks_of(pad64(a.D) / 8, kRouterWaves * 64), a.T);
     if (a.wide) k_moe_router<TYPE, true><<<router, kRouterWaves * 64, 0, stream>>>(a);
     else k_moe_router<TYPE, false><<<router, kRouterWaves * 64, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;

@@ -573,7 +573,7 @@ extern "C" {
 
 int tst_quantize(const void *X, int type, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int M, int K, void *stream)
 {
-    if (!tst::type_ok(type) || M < 0 || K < 1 || x_stride < K || q_stride < K) return TSTGEMM_EINVAL;
+    if (!tst::type_ok(type) || M < 0 || K < 1 || K > 1 << 30 || x_stride < K || q_stride < K) return TSTGEMM_EINVAL;
     if (M == 0) return TSTGEMM_OK;
     if (!X || !Q || !scale || !tst::aligned(X, tst::type_bytes(type)) || !tst::aligned(scale, 4)) return TSTGEMM_EINVAL;
     return tst::status(tst::launch_quantize(X, type, x_stride, Q, q_stride, scale, M, K, static_cast<hipStream_t>(stream)));

@@ -94,6 +94,18 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _shared(stream, operands, results):
+    """A call on a stream that was given: operands are in use there until it is done, what it made may be looked at on the current one."""
+    import torch
+    if stream is not None:
+        here = torch.cuda.current_stream()
+        for t in operands:
+            if t is not None:
+                t.record_stream(stream)
+        for t in results:
+            t.record_stream(here)
+
+
 def _workspace(bytes_, given, stream, dev):
     """(tensor to keep until the call is enqueued, address, bytes)"""
     import torch
@@ -121,6 +133,8 @@ class W8:
     """8-bit weights in their device form (tst_w8_pack) with the scale of each output channel."""
 
     def __init__(self, K, N, count, packed, scale):
+        if packed.numel() != count * _bytes("tst_w8_bytes", K, N) or scale.numel() != count * N:
+            raise ValueError("packed and scale must be those of count matrices K x N")
         self.K, self.N, self.count, self.packed, self.scale = K, N, count, packed, scale
 
 
@@ -138,6 +152,7 @@ def _pack(W, what, stream):
     with _on(stream):
         packed = torch.empty(count * size, dtype=torch.uint8, device=dev)
     _call("tst_w8_pack", W.data_ptr(), count, K, N, packed.data_ptr(), _launch_stream(stream, dev))
+    _shared(stream, (W,), (packed,))
     return count, K, N, packed, dev
 
 
@@ -173,6 +188,7 @@ def tst_quantize(X, Q=None, scale=None, stream=None):
     _, _, q_stride = _rows(Q, "Q", torch.int8)
     scale = _result(scale, "scale", torch.float32, (M,), stream, dev)
     _call("tst_quantize", X.data_ptr(), kind, stride, Q.data_ptr(), q_stride, scale.data_ptr(), M, K, _launch_stream(stream, dev))
+    _shared(stream, (X, Q, scale), (Q, scale))
     return Q, scale
 
 
@@ -197,6 +213,7 @@ def tst_w8_gemm(Q, scale, w: W8, b=None, Y=None, dtype=None, stream=None):
     Y = _result(Y, "Y", dtype, (M, w.N), stream, dev)
     _call("tst_w8_gemm", Q.data_ptr(), stride, s_ptr, w.packed.data_ptr(), w.scale.data_ptr(), b_ptr, Y.data_ptr(), kind, M, K, w.N,
           _launch_stream(stream, dev))
+    _shared(stream, (Q, scale, w.packed, w.scale, b, Y), (Y,))
     return Y
 
 
@@ -215,6 +232,7 @@ def tst_w8_linear(X, w: W8, b=None, Y=None, workspace=None, stream=None):
     keep, ws, n = _workspace(_bytes("tst_w8_linear_workspace_bytes", M, K), workspace, stream, dev)
     _call("tst_w8_linear", X.data_ptr(), kind, stride, w.packed.data_ptr(), w.scale.data_ptr(), b_ptr, Y.data_ptr(), M, K, w.N, ws, n,
           _launch_stream(stream, dev))
+    _shared(stream, (X, w.packed, w.scale, b, Y, keep), (Y,))
     return Y
 
 
@@ -282,6 +300,7 @@ def tst_moe(X, moe: Moe, top_k: int, normalize=True, Y=None, ids=None, p=None, w
     keep, ws, n = _workspace(size, workspace, stream, dev)
     _call("tst_moe", X.data_ptr(), stride, moe._ref, top_k, int(bool(normalize)), Y.data_ptr(), ids.data_ptr(), p.data_ptr(), T, ws, n,
           _launch_stream(stream, dev))
+    _shared(stream, (X, *moe._tensors, Y, ids, p, keep), (Y, ids, p))
     return Y, ids, p
 
 
@@ -312,4 +331,5 @@ def tst_logprobs(logits, tokens=None, top=0, workspace=None, stream=None):
     keep, ws, n = _workspace(size, workspace, stream, dev)
     _call("tst_logprobs", logits.data_ptr(), kind, stride, t_ptr, t_bytes, C, top, of_token.data_ptr(), entropy.data_ptr(),
           ids.data_ptr(), of_top.data_ptr(), R, V, ws, n, _launch_stream(stream, dev))
+    _shared(stream, (logits, tokens, keep), (of_token, entropy, ids, of_top))
     return of_token, entropy, ids, of_top

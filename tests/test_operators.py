@@ -57,7 +57,7 @@ def test_refusals():
     for args in ((None, 1, 4, 4, a), (a, 1, 4, 4, None), (a, 0, 4, 4, a), (a, 1, 0, 4, a), (a, 1, 131072, 4, a), (a, 1, 4, 4, a + 8)):
         assert lib.tst_w8_pack(*args, None) == EINVAL
     ok = [a, 0, 64, a, 64, a, 2, 64, None]     # X, type, stride, Q, stride, scale, M, K, stream
-    for i, v in ((0, None), (0, a + 2), (1, 3), (1, -1), (2, 63), (3, None), (4, 63), (5, None), (6, -1), (7, 0)):
+    for i, v in ((0, None), (0, a + 2), (1, 3), (1, -1), (2, 63), (3, None), (4, 63), (5, None), (6, -1), (7, 0), (7, 2 ** 30 + 1)):
         assert lib.tst_quantize(*ok[:i], v, *ok[i + 1:]) == EINVAL, i
     ok = [a, 64, a, a, a, None, a, 1, 2, 64, 32, None]   # Q, stride, scale, packed, w_scale, b, Y, type, M, K, N, stream
     for i, v in ((0, None), (0, a + 8), (1, 63), (1, 72), (2, None), (3, None), (3, a + 8), (4, None), (6, None), (6, a + 1), (7, 3), (8, -1),
@@ -96,7 +96,7 @@ def test_refusals_of_moe():
 def test_refusals_of_logprobs():
     lib = operators._ops()
     a, n = 1 << 20, ctypes.c_size_t()
-    for args in ((-1, 50, 3), (2, 0, 0), (2, 50, -1), (2, 50, 51), (2, 500, 65)):
+    for args in ((-1, 50, 3), (2, 0, 0), (2, 2 ** 30 + 1, 3), (2, 50, -1), (2, 50, 51), (2, 500, 65)):
         assert lib.tst_logprobs_workspace_bytes(*args, ctypes.byref(n)) == EINVAL
     ok = [a, 1, 50, a, 8, 1, 3, a, a, a, a, 2, 50, a, 1 << 30, None]
     # logits, type, stride, tokens, bytes, C, top, of_token, entropy, top_ids, of_top, R, V, workspace, bytes, stream
@@ -124,6 +124,9 @@ def test_the_native_half_hands_back_what_is_not_on_a_gpu():
     assert native is not None
     x = torch.zeros((2, 64))
     w = tg.W8(64, 32, 1, torch.zeros(2048, dtype=torch.uint8), torch.ones(32))
+    for wrong in ((64, 33, torch.ones(33)), (128, 32, torch.ones(32)), (64, 32, torch.ones(31))):
+        with pytest.raises(ValueError):
+            tg.W8(wrong[0], wrong[1], 1, torch.zeros(2048, dtype=torch.uint8), wrong[2])
     assert native.w8_linear(x, w, None) is None and native.w8_gemm(x.to(torch.int8), torch.ones(2), w, None, None) is None
     assert native.moe(x, None, 2, True) is None and native.logprobs(x, None, 1) is None
     for call in (lambda: native.w8_linear(x), lambda: native.w8_gemm(x), lambda: native.moe(x), lambda: native.logprobs(x)):
