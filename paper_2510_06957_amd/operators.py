@@ -110,7 +110,7 @@ def _workspace(bytes_, given, stream, dev):
     """(tensor to keep until the call is enqueued, address, bytes)"""
     import torch
     if given is not None:
-        if not (given.is_cuda and given.is_contiguous() and given.get_device() == dev):
+        if not (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.get_device() == dev):
             raise ValueError("workspace must be a contiguous CUDA tensor on the operands' device")
         return given, given.data_ptr(), given.numel() * given.element_size()
     if bytes_ == 0:
@@ -160,7 +160,7 @@ def tst_w8_pack(W, scale, stream=None) -> W8:
     """Weights of a layer in 8 bits: W int8 [K, N], scale float32 [N] (of each output channel), both on the GPU.  A ternary matrix
     is a case of them: torch.from_numpy(tcsc_to_dense(t)).cuda()."""
     import torch
-    if W.dim() != 2:
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
         raise ValueError("W must be a contiguous int8 CUDA tensor [K, N]")
     count, K, N, packed, dev = _pack(W, "W", stream)
     _dense(scale, "scale", torch.float32, (N,), dev)
@@ -183,7 +183,7 @@ def tst_quantize(X, Q=None, scale=None, stream=None):
     if Q is None:
         with _on(stream):
             Q = torch.empty((M, (K + 63) // 64 * 64), dtype=torch.int8, device=dev)[:, :K]
-    elif not (Q.is_cuda and Q.get_device() == dev and tuple(Q.shape) == (M, K)):
+    elif not (isinstance(Q, torch.Tensor) and Q.is_cuda and Q.get_device() == dev and tuple(Q.shape) == (M, K)):
         raise ValueError("Q must be an int8 CUDA matrix of X's shape on X's device")
     _, _, q_stride = _rows(Q, "Q", torch.int8)
     scale = _result(scale, "scale", torch.float32, (M,), stream, dev)
@@ -256,14 +256,14 @@ def tst_moe_pack(router, gate, gate_scale, up, up_scale, down, down_scale, strea
     """router [E, D] float32, bfloat16 or float16 (the type of the tokens to come); gate, up int8 [E, D, F] with scales float32
     [E, F]; down int8 [E, F, D] with scales float32 [E, D]."""
     import torch
-    kind = _type(router.dtype, "router")
     n, D, stride = _rows(router, "router")
+    kind = _type(router.dtype, "router")
     if n > 1 and stride != D:
         raise ValueError("router must be contiguous")
     dev = router.get_device()
     E, packed, F = n, [], None
     for what, W, S in (("gate", gate, gate_scale), ("up", up, up_scale), ("down", down, down_scale)):
-        if W.dim() != 3 or W.shape[0] != E or (F is not None and W.shape[1:] != ((F, D) if what == "down" else (D, F))):
+        if not isinstance(W, torch.Tensor) or W.dim() != 3 or W.shape[0] != E or (F is not None and W.shape[1:] != ((F, D) if what == "down" else (D, F))):
             raise ValueError("gate and up must be [E, D, F], down [E, F, D]")
         _, rows, cols, p, on = _pack(W, what, stream)
         if what == "gate":
@@ -288,6 +288,8 @@ def tst_moe(X, moe: Moe, top_k: int, normalize=True, Y=None, ids=None, p=None, w
         if done is not None:
             return done
     import torch
+    if not isinstance(moe, Moe):
+        raise ValueError("moe must be what tst_moe_pack gives")
     T, D, stride = _rows(X, "X", moe.dtype)
     dev = X.get_device()
     if D != moe.D or dev != moe.device_index:
@@ -317,7 +319,7 @@ def tst_logprobs(logits, tokens=None, top=0, workspace=None, stream=None):
     if tokens is None:
         shape, t_ptr, t_bytes = (R, 0), None, 8
     else:
-        if tokens.dtype not in (torch.int32, torch.int64) or tokens.dim() not in (1, 2) or tokens.shape[0] != R:
+        if not isinstance(tokens, torch.Tensor) or tokens.dtype not in (torch.int32, torch.int64) or tokens.dim() not in (1, 2) or tokens.shape[0] != R:
             raise ValueError("tokens must be int32 or int64, [R] or [R, C]")
         shape = tuple(tokens.shape)
         t_ptr, t_bytes = _dense(tokens, "tokens", tokens.dtype, shape, dev), tokens.element_size()

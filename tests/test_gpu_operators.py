@@ -554,6 +554,9 @@ def test_refusals_on_the_gpu():
                  lambda: tg.tst_w8_gemm(off[:, 1:65], s, w), lambda: tg.tst_w8_gemm(off.view(-1)[:2 * 72].view(2, 72)[:, :64], s, w),
                  lambda: tg.tst_w8_gemm(Q, s[:1], w), lambda: tg.tst_w8_gemm(Q.float(), s, w), lambda: tg.tst_w8_gemm(Q, s, w, dtype=torch.int32),
                  lambda: tg.tst_w8_pack(torch.zeros((4, 4), device="cuda"), s), lambda: tg.tst_quantize(X, Q[:1]),
+                 lambda: tg.tst_w8_pack(np.zeros((4, 4), np.int8), s), lambda: tg.tst_w8_linear(X, moe), lambda: tg.tst_quantize(X, Q.cpu().numpy()),
+                 lambda: tg.tst_w8_linear(X, w, workspace=4096), lambda: tg.tst_moe(x, w, 2), lambda: tg.tst_logprobs(X, [1, 2]),
+                 lambda: tg.tst_moe_pack(np.zeros((2, 4)), *[None] * 6), lambda: tg.tst_moe_pack(x, *[np.zeros((2, 64, 4), np.int8), None] * 3),
                  lambda: tg.tst_moe(X, moe, 2), lambda: tg.tst_moe(x[:, :60], moe, 2), lambda: tg.tst_logprobs(X[0]),
                  lambda: tg.tst_logprobs(X, torch.zeros(3, dtype=torch.int64, device="cuda")),
                  lambda: tg.tst_logprobs(X, torch.zeros(2, dtype=torch.int16, device="cuda")), lambda: tg.tst_logprobs(X.cpu())):
