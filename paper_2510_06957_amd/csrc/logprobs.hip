@@ -92,12 +92,12 @@ __device__ __forceinline__ float nth_of_lanes(float mine, int n)
 template <int TYPE> __device__ void sort_slowly(const typename Entry<TYPE>::bits *z, int begin, int end, int n, Shared &s)
 {
     typedef Entry<TYPE> E;
-    Key last = ~0ull;
+    Key last = 0;
     for (int j = 0; j < n; ++j) {
         Key mine = 0;
         for (int v = begin + threadIdx.x; v < end; v += kThreads) {
             const Key key = key_of(E::get(z[v]), v);
-            if (key < last && key > mine) mine = key;
+            if ((j == 0 || key < last) && key > mine) mine = key;   // (a NaN at token 0 has the largest key there is)
         }
         __syncthreads();
         s.list[0][threadIdx.x] = mine;
@@ -126,9 +126,9 @@ template <int TYPE> __device__ void finish(const LogArgs &a, int64_t r, float mo
         a.of_token[i] = token < 0 || token >= a.V ? kNan : E::get(z[token]) - most - log_sum;
     }
     if ((int)threadIdx.x < a.top) {
-        const int token = token_of(sorted[threadIdx.x]);
+        const int token = token_of(sorted[threadIdx.x]);   // of the row, there being as many keys as alternatives (top <= V); -1 of no key
         a.top_ids[r * a.top + threadIdx.x] = token;
-        a.of_top[r * a.top + threadIdx.x] = E::get(z[token]) - most - log_sum;
+        a.of_top[r * a.top + threadIdx.x] = token < 0 ? kNan : E::get(z[token]) - most - log_sum;
     }
 }
 

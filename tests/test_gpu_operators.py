@@ -402,6 +402,30 @@ def test_logprobs_of_rows_without_a_distribution(V):
     assert torch.equal(ids[5], clean[2][5]) and torch.equal(entropy[5], clean[1][5]) and torch.equal(of_top[5], clean[3][5])
 
 
+@pytest.mark.parametrize("R", [7, 1100])   # rows in splits where they are long, and whole ones
+@pytest.mark.parametrize("V", [1, 2, 5, 33, 64, 3000, 70001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_logprobs_alternatives_of_rows_with_nan(V, R, dtype):
+    """A NaN counts as largest wherever it stands, ties go to the lowest token, and a row has as many alternatives as are asked for: all
+    of them where top is V."""
+    Z = torch.zeros((R, V), dtype=TYPES[dtype], device="cuda")
+    Z[:7] = logits(7, V, dtype, 29)
+    Z[0, 0] = float("nan")
+    Z[1] = float("nan")
+    Z[2, 0] = Z[2, V // 2] = Z[2, V - 1] = float("nan")
+    Z[3, ::2] = float("nan")
+    Z[4, 0], Z[4, V - 1] = float("nan"), float("inf")
+    Z[5] = -float("inf")
+    Z[5, 0] = float("nan")
+    Z[6, V // 2] = -float("nan")
+    z = f64(Z[:7])
+    order = np.lexsort((np.broadcast_to(np.arange(V), z.shape), -np.nan_to_num(z, nan=0.0), ~np.isnan(z)))
+    for top in {1, min(V, 5), min(V, 64)}:
+        of_token, entropy, ids, of_top = (o[:7].cpu() for o in tg.tst_logprobs(Z, torch.zeros(R, dtype=torch.int64, device="cuda"), top=top))
+        assert np.array_equal(ids.numpy(), order[:, :top])
+        assert torch.isnan(of_token).all() and torch.isnan(entropy).all() and torch.isnan(of_top).all()
+
+
 def test_logprobs_of_tokens_outside_the_vocabulary():
     Z = logits(3, 500, "bf16", 27)
     t = torch.tensor([[-1, 4], [500, 499], [2 ** 40, -2 ** 40]], device="cuda")
