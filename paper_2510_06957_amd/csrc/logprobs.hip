@@ -437,22 +437,33 @@ int tst_logprobs(const void *logits, int type, int64_t stride, const void *token
     if (need && !tst::aligned(workspace, 256)) return TSTGEMM_EINVAL;
     const int per = (int)(16 / entry), splits = tst::splits_of(R, V, type);
     const int length = tst::blocks_of(tst::blocks_of(V, splits), per) * per;   // splits begin on borders of vectors
-    const tst::LogArgs a{logits, stride, tokens, token_bytes, C, top, of_token, entropy, top_ids, of_top, V,
-                         tst::aligned(logits, 16) && stride % per == 0, tst::blocks_of(V, length), length, static_cast<float4 *>(workspace),
-                         reinterpret_cast<unsigned long long *>(static_cast<char *>(workspace) + tst::log_space(R, top).keys)};
+    tst::LogArgs a{logits, stride, tokens, token_bytes, C, top, of_token, entropy, top_ids, of_top, V,
+                   tst::aligned(logits, 16) && stride % per == 0, tst::blocks_of(V, length), length, static_cast<float4 *>(workspace),
+                   reinterpret_cast<unsigned long long *>(static_cast<char *>(workspace) + tst::log_space(R, top).keys)};
     return tst::status(tst::for_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
         hipStream_t st = static_cast<hipStream_t>(stream);
-        const dim3 grid(R, a.splits);
-        if (top > 0 && a.splits == 1) tst::k_logprobs<T, true, tst::kVectors><<<grid, tst::kThreads, 0, st>>>(a);
-        else if (top > 0) tst::k_logprobs<T, true, tst::kFewVectors><<<grid, tst::kThreads, 0, st>>>(a);
-        else if (a.splits == 1) tst::k_logprobs<T, false, tst::kVectors><<<grid, tst::kThreads, 0, st>>>(a);
-        else tst::k_logprobs<T, false, tst::kFewVectors><<<grid, tst::kThreads, 0, st>>>(a);
-        if (a.splits > 1) {
+        for (int64_t r = 0;;) {   // (rows of which there are many are not split)
+            const int rows = (int)(R - r < tst::kLaunchRows ? R - r : tst::kLaunchRows);
+            const dim3 grid(rows, a.splits);
+            if (top > 0 && a.splits == 1) tst::k_logprobs<T, true, tst::kVectors><<<grid, tst::kThreads, 0, st>>>(a);
+            else if (top > 0) tst::k_logprobs<T, true, tst::kFewVectors><<<grid, tst::kThreads, 0, st>>>(a);
+            else if (a.splits == 1) tst::k_logprobs<T, false, tst::kVectors><<<grid, tst::kThreads, 0, st>>>(a);
+            else tst::k_logprobs<T, false, tst::kFewVectors><<<grid, tst::kThreads, 0, st>>>(a);
+            if (a.splits > 1) {
+                if (hipError_t e = hipGetLastError()) return e;
+                tst::k_logprobs_join<T><<<rows, tst::kThreads, 0, st>>>(a);
+            }
             if (hipError_t e = hipGetLastError()) return e;
-            tst::k_logprobs_join<T><<<R, tst::kThreads, 0, st>>>(a);
+            r += rows;
+            if (r == R) return hipSuccess;
+            a.z = static_cast<const char *>(a.z) + rows * stride * (int64_t)entry;
+            if (C) a.tokens = static_cast<const char *>(a.tokens) + (int64_t)rows * C * token_bytes;
+            if (C) a.of_token += (int64_t)rows * C;
+            if (a.entropy) a.entropy += rows;
+            if (top) a.top_ids += (int64_t)rows * top;
+            if (top) a.of_top += (int64_t)rows * top;
         }
-        return hipGetLastError();
     }));
 }
 

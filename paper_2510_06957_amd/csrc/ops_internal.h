@@ -69,6 +69,10 @@ __device__ __forceinline__ float from_order_bits(unsigned b) { return __uint_as_
 
 int compute_units();   // (tstgemm_side.hip)
 
+// A dimension of a grid has fewer than 2^32 threads, and a launch with more goes through with what is left of their number in 32 bits: kernels
+// with a workgroup of 256 for a row are launched for so many rows at a time.
+constexpr int kLaunchRows = 1 << 22;
+
 inline int status(hipError_t e) { return e == hipSuccess ? TSTGEMM_OK : TSTGEMM_EHIP; }
 
 // call(std::integral_constant<int, type>) for a run-time type

@@ -531,9 +531,14 @@ hipError_t launch_quantize(const void *X, int type, int64_t x_stride, int8_t *Q,
         // few rows get more threads each (1 x 16385 fp16 5 us in place of 20)
         const bool few = M < compute_units();
         if (wide && few) k_quantize<T, true, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
-        else if (wide) k_quantize<T, true, 256><<<M, 256, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
         else if (few) k_quantize<T, false, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
-        else k_quantize<T, false, 256><<<M, 256, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
+        else
+            for (int64_t m = 0; m < M; m += kLaunchRows) {
+                const int rows = (int)(M - m < kLaunchRows ? M - m : kLaunchRows);
+                if (wide) k_quantize<T, true, 256><<<rows, 256, 0, stream>>>(x + m * x_stride, x_stride, Q + m * q_stride, q_stride, scale + m, K);
+                else k_quantize<T, false, 256><<<rows, 256, 0, stream>>>(x + m * x_stride, x_stride, Q + m * q_stride, q_stride, scale + m, K);
+                if (hipError_t e = hipGetLastError()) return e;
+            }
         return hipGetLastError();
     });
 }

@@ -526,6 +526,23 @@ def test_plain_calls_go_through_the_native_half():
         assert native.w8_linear(X, w, bd) is None
 
 
+def test_more_rows_than_a_launch_takes():
+    """2^24 workgroups of 256 have more threads than a grid counts."""
+    M = (1 << 24) + 3
+    r = torch.Generator(device="cuda").manual_seed(60)
+    x = torch.randn((M, 2), generator=r, device="cuda")
+    Q, s = tg.tst_quantize(x)
+    token = torch.randint(0, 2, (M,), generator=r, device="cuda")
+    of_token, entropy, ids, of_top = tg.tst_logprobs(x, token, top=2)
+    lp = x.double().log_softmax(1)
+    assert torch.equal(s, x.abs().amax(1) / torch.full_like(s, 127))
+    assert torch.equal(Q.abs().amax(1), torch.full((M,), 127, dtype=torch.int8, device="cuda"))
+    assert ((Q.float() * s[:, None] - x).abs() <= 0.501 * s[:, None]).all()
+    assert torch.equal(ids, torch.sort(x, dim=1, descending=True, stable=True).indices.int())
+    for got, want in ((of_token, lp.gather(1, token[:, None])[:, 0]), (entropy, -(lp.exp() * lp).sum(1)), (of_top, lp.gather(1, ids.long()))):
+        assert ((got - want).abs() <= 50 * U * (1 + want.abs())).all()
+
+
 def test_large_strides():
     """Rows far apart, up to what the product takes; and offsets that pass 32 bits."""
     W, t, b, w = layer(96, 40, 56)
