@@ -17,7 +17,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // Geometry of packed 8-bit weights (tst_w8_pack): pieces of 16 columns x 64 rows.
 constexpr int kW8Cols = 16, kW8Rows = 64, kW8Piece = kW8Cols * kW8Rows;
-inline __host__ __device__ int blocks_of(int n, int size) { return (n + size - 1) / size; }
+inline __host__ __device__ int blocks_of(int n, int size) { return n / size + (n % size != 0); }   // (n + size may pass 2^31)
 inline size_t w8_bytes(int K, int N) { return (size_t)blocks_of(K, kW8Rows) * blocks_of(N, kW8Cols) * kW8Piece; }
 constexpr int kW8MaxK = 131071;   // 131072 * (-128 * -128) = 2^31
 

@@ -71,6 +71,16 @@ def test_refusals():
     assert lib.tst_w8_linear_workspace_bytes(-1, 4, ctypes.byref(n)) == EINVAL
 
 
+def test_bytes_of_as_many_columns_as_there_can_be():
+    for K, N, want in ((1, 2 ** 31 - 1, 2 ** 37), (131071, 2 ** 31 - 1, 2 ** 48)):
+        assert operators._bytes("tst_w8_bytes", K, N) == want
+
+
+def test_workspace_of_as_many_rows_as_there_can_be():
+    for R in (2 ** 31 - 1, 2 ** 31 - 600, 1 << 24):
+        assert operators._bytes("tst_logprobs_workspace_bytes", R, 1 << 20, 20) == 0
+
+
 def test_refusals_of_moe():
     lib = operators._ops()
     a, n = 1 << 20, ctypes.c_size_t()
