@@ -44,7 +44,7 @@ int tst_quantize(const void *X, int type, int64_t x_stride, int8_t *Q, int64_t q
  * tst_w8_bytes: bytes of one K x N matrix (a multiple of 1024).  K <= 131071, so that a sum of K products of codes, -128 included,
  * fits 32 bits.
  * tst_w8_pack: W: DEVICE, `count` matrices of K x N int8, row-major, one behind another; packed: DEVICE, count * tst_w8_bytes(),
- * 16-byte aligned, fully overwritten.  Errors: EINVAL, EHIP.
+ * 16-byte aligned, fully overwritten, below 64 GiB a matrix.  Errors: EINVAL, ETOOBIG, EHIP.
  */
 int tst_w8_bytes(int K, int N, size_t *bytes);
 int tst_w8_pack(const int8_t *W, int count, int K, int N, void *packed, void *stream);
@@ -55,7 +55,7 @@ int tst_w8_pack(const int8_t *W, int count, int K, int N, void *packed, void *st
  * Q: DEVICE, M rows of K codes, q_stride bytes apart; Q 16-byte aligned and q_stride a multiple of 16, at most 4 MiB (or M = 1).
  * What lies between K and the next 16-byte border of a row is read and does not matter; nothing behind that border is read.
  * scale: DEVICE, M.  packed: DEVICE, tst_w8_pack() of W.  w_scale: DEVICE, N.  b: DEVICE, N, or NULL.  Y: DEVICE, M x N of y_type,
- * row-major, aligned to its type.  0 <= M <= 1048560.  Errors: EINVAL, EHIP.
+ * row-major, aligned to its type.  0 <= M <= 1048560, N < 2^27 - 15.  Errors: EINVAL, EHIP.
  */
 int tst_w8_gemm(const int8_t *Q, int64_t q_stride, const float *scale, const void *packed, const float *w_scale, const float *b,
                 void *Y, int y_type, int M, int K, int N, void *stream);

@@ -556,10 +556,12 @@ hipError_t launch_few(const GemmArgs &a, const void *X, int64_t x_stride, hipStr
 
 // the most rows that a grid's second dimension holds with the smallest tile, and bytes between rows whose offsets in a tile fit 31 bits
 constexpr int kMaxRows = 65535 * 16, kMaxStride = 1 << 22;
+// the most columns: k_w8_rows and k_w8_few have 512 threads for 16 of them, and a dimension of a grid fewer than 2^32
+constexpr int kMaxColumns = (1 << 27) - 16;
 
 int check_gemm(const void *X, const void *packed, const float *w_scale, const void *Y, int type, int M, int K, int N)
 {
-    if (!type_ok(type) || M < 0 || M > kMaxRows || K < 1 || K > kW8MaxK || N < 1 || N > INT32_MAX - 64) return TSTGEMM_EINVAL;
+    if (!type_ok(type) || M < 0 || M > kMaxRows || K < 1 || K > kW8MaxK || N < 1 || N > kMaxColumns) return TSTGEMM_EINVAL;
     if (M > 0 && (!X || !packed || !w_scale || !Y || !aligned(packed, 16) || !aligned(Y, type_bytes(type)))) return TSTGEMM_EINVAL;
     return TSTGEMM_OK;
 }
@@ -595,7 +597,7 @@ int tst_w8_pack(const int8_t *W, int count, int K, int N, void *packed, void *st
 {
     if (!W || !packed || count < 1 || count > 65535 || K < 1 || K > tst::kW8MaxK || N < 1 || !tst::aligned(packed, 16)) return TSTGEMM_EINVAL;
     const int k_blocks = tst::blocks_of(K, tst::kW8Rows), n_blocks = tst::blocks_of(N, tst::kW8Cols);
-    if ((int64_t)k_blocks * n_blocks > INT32_MAX) return TSTGEMM_ETOOBIG;
+    if ((int64_t)k_blocks * n_blocks * 64 > UINT32_MAX) return TSTGEMM_ETOOBIG;   // threads of a dimension of the grid
     tst::k_w8_pack<<<dim3(k_blocks * n_blocks, count), 64, 0, static_cast<hipStream_t>(stream)>>>(W, static_cast<char *>(packed), K, N,
                                                                                                  k_blocks, n_blocks);
     return tst::status(hipGetLastError());

@@ -71,6 +71,18 @@ def test_refusals():
     assert lib.tst_w8_linear_workspace_bytes(-1, 4, ctypes.byref(n)) == EINVAL
 
 
+def test_sizes_that_no_grid_counts_are_refused():
+    """A dimension of a grid has fewer than 2^32 threads."""
+    lib = operators._ops()
+    a = 1 << 20
+    for K, N in ((64, 1 << 30), (131071, 1 << 19), (1, 2 ** 31 - 1)):
+        assert lib.tst_w8_pack(a, 1, K, N, a, None) == -6
+    for N in ((1 << 27) - 15, 1 << 27, 2 ** 31 - 100):
+        assert lib.tst_w8_gemm(a, 64, a, a, a, None, a, 1, 2, 64, N, None) == EINVAL
+        assert lib.tst_w8_linear(a, 1, 64, a, a, None, a, 2, 64, N, a, 1 << 30, None) == EINVAL
+    assert lib.tst_w8_gemm(a, 64, a, a, a, None, a, 1, 0, 64, (1 << 27) - 16, None) == 0   # no rows: nothing to do
+
+
 def test_bytes_of_as_many_columns_as_there_can_be():
     for K, N, want in ((1, 2 ** 31 - 1, 2 ** 37), (131071, 2 ** 31 - 1, 2 ** 48)):
         assert operators._bytes("tst_w8_bytes", K, N) == want
