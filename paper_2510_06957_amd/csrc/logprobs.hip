@@ -58,12 +58,6 @@ __device__ __forceinline__ void rank_keys(const Key *list, int count, Key *sorte
     }
 }
 
-__device__ __forceinline__ void order_wave()   // of a wavefront's own stores and reads in the LDS
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-}
-
 template <typename F> __device__ __forceinline__ float over_waves(float v, float *part, F f)
 {
 #pragma unroll

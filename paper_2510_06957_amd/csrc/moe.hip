@@ -460,6 +460,7 @@ k_moe_down(const MoeArgs a)
         count_tiles();
     }
     auto settle = [&]() {
+        order_wave();   // a token's sums were written by the lane that had its column before
         const float *scale = a.down_scale + (size_t)a.used[nth] * a.D;
 #pragma unroll
         for (int j = 0; j < kDownCols; ++j) {

@@ -57,6 +57,14 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
     return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 
+// Orders a wavefront's own stores and reads in the LDS, which its lanes exchange without a meeting of the workgroup: the LDS takes them as
+// they come, the compiler would be free to move them.
+__device__ __forceinline__ void order_wave()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Bits that order as floats do: NaN above everything, -0 as +0.  No float has 0.
 __device__ __forceinline__ unsigned order_bits(float v)
 {

@@ -192,15 +192,11 @@ k_w8_rows(const GemmArgs a)
             stage[((row >> 4) * 8 + c) * 16 + ((row & 15) ^ c)] = xr[p];
         }
     };
-    auto order = [&]() {   // of the wavefront's own stores and reads; the LDS takes them in this order
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-        __builtin_amdgcn_wave_barrier();
-    };
     load_x(wave);
     load_w(wave, wr);
     for (int step = wave; step < steps; step += kRowsWaves) {
         store_x();
-        order();
+        order_wave();
         load_x(step + kRowsWaves);   // behind the last step: X reads as 0
         load_w(step + kRowsWaves, wn);
         __builtin_amdgcn_sched_barrier(0);   // or the compiler moves the loads to where they are used
@@ -213,7 +209,7 @@ k_w8_rows(const GemmArgs a)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[t][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wr[s][j], xf, acc[t][j], 0, 0, 0);
             }
-        order();
+        order_wave();
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll

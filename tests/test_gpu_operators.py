@@ -264,6 +264,27 @@ def test_moe(T, E, k, D, F, dtype):
     assert torch.equal(again[0], Y) and torch.equal(again[2], got_p)
 
 
+@pytest.mark.parametrize("T,E,k,D,F,most", [(64, 1, 1, 70, 50, 64), (64, 4, 4, 530, 90, 64), (50, 4, 3, 130, 333, 33), (40, 2, 1, 65, 700, 17),
+                                            (101, 3, 3, 100, 40, 64), (60, 9, 6, 201, 150, 33)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_moe_of_experts_with_many_members(T, E, k, D, F, most, dtype):
+    """Experts whose tokens fill all four tiles of 16, some of them in part; `most`: members that some expert has at least in 64 tokens."""
+    w = experts(E, D, F, dtype, 61)
+    for seed in range(62, 162):
+        X = tokens(T, D, dtype, seed, D + 5)
+        if clear_choice(X, w, k):
+            break
+    assert clear_choice(X, w, k)
+    want, ids, p, bound, d_p = moe_reference(X, w, k, True, dtype)
+    assert np.bincount(ids[:64].ravel()).max() >= most
+    moe = packed(w)
+    Y, got_ids, got_p = tg.tst_moe(X, moe, k)
+    assert np.array_equal(got_ids.cpu().numpy(), ids)
+    assert_within(got_p, p, d_p, what="p")
+    assert_within(Y, want, bound, dtype, "Y")
+    assert torch.equal(tg.tst_moe(X, moe, k)[0], Y)
+
+
 def test_moe_ties_go_to_the_lowest_expert():
     r = rng(13)
     rows = r.standard_normal((3, 80))
