@@ -1,6 +1,7 @@
 // Layers in 8 bits: quantisation of tokens, the packed form of the weights, and the product
 //   Y[m][n] = scale[m] w_scale[n] sum_k Q[m][k] W[k][n] + b[n].
 #include "ops_internal.h"
+#include "w8_choice.h"
 
 namespace tst {
 namespace {
@@ -156,7 +157,7 @@ __device__ __forceinline__ i32x4 load16(__amdgpu_buffer_rsrc_t from, unsigned la
 // rows take the address unit a cycle for each lane (64 x 16384 x 4096: 35 us in place of 18), so 8 lanes load 128 bytes of a row together.
 // Chunk c of 8 of a row stands in slot (row % 16) ^ c, which makes both the writes (8 chunks of a row together) and the reads (16 rows
 // of a chunk together) free of bank conflicts.  64 x 16384 x 4096 16.4 us (67 MB of weights at 4.1 TB/s), 256 x 4096 x 4096 11.6.
-constexpr int kRowsWaves = 8, kRowsThreads = kRowsWaves * 64, kStepK = 128;
+constexpr int kRowsWaves = 8, kRowsThreads = kRowsWaves * 64;
 
 template <int TYPE, int MT, int NT>
 __global__ void __launch_bounds__(kRowsThreads, 2)
@@ -462,38 +463,9 @@ k_w8_tiles(const GemmArgs a, int m_tiles, int n_tiles)
     }
 }
 
-// Which kernel and tile.  All of them are bound by what a compute unit can load (about 65 GB/s each, over all sizes measured), so the
-// choice is the one for which the busiest compute unit loads least: rounds of workgroups x bytes of a workgroup, and for k_w8_rows the
-// sums that its wavefronts exchange.  Measured with K = N = 4096 (us): 256 rows 11.8 with 64 x 64 tiles of k_w8_rows, 23 with k_w8_tiles<4>,
-// 31 with k_w8_tiles<8>; 512 rows 20 / 24 / 31; 1024 rows 36 / 24 / 32; 2048 rows 70 / 38 / 36; 4096 rows 61 with k_w8_tiles<8>, 72
-// with <4>.  64 x 16384 x 4096: 17.3 with 32 x 32 tiles of k_w8_rows, 18.3 with 64 x 16, 26 with 64 x 64.
-struct GemmTile {
-    bool rows;
-    int mt, nt;   // 16 mt rows x 16 nt columns
-};
-constexpr GemmTile kGemmTiles[] = {{true, 1, 1}, {true, 1, 2}, {true, 2, 2}, {true, 4, 2}, {true, 4, 4}, {false, 4, 16}, {false, 8, 16}};
-
-GemmTile choose_tile(int M, int K, int N)
-{
-    const double compute_units = tst::compute_units(), steps = blocks_of(K, kStepK);
-    GemmTile best = kGemmTiles[0];
-    double least = 1e300;
-    for (const GemmTile &t : kGemmTiles) {
-        const double groups = (double)blocks_of(M, 16 * t.mt) * blocks_of(N, 16 * t.nt);
-        const double rounds = groups > compute_units ? (double)(int64_t)((groups + compute_units - 1) / compute_units) : 1;
-        const double x_rows = M < 16 * t.mt ? M : 16 * t.mt;
-        const double bytes = rounds * (steps * kStepK * (x_rows + 16 * t.nt) + (t.rows ? 20e3 + 6e3 * t.mt * t.nt : 0));
-        if (bytes < least) {
-            least = bytes;
-            best = t;
-        }
-    }
-    return best;
-}
-
 hipError_t launch_gemm(const GemmArgs &a, int y_type, hipStream_t stream)
 {
-    const GemmTile tile = choose_tile(a.M, a.K, a.N);
+    const GemmTile tile = choose_tile(a.M, a.K, a.N, compute_units());
     const int m = blocks_of(a.M, 16 * tile.mt), n = blocks_of(a.N, 16 * tile.nt);
     return for_type(y_type, [&](auto type) {
         constexpr int T = decltype(type)::value;

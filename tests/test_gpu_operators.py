@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2510_06957_amd as tg
+from w8_tiles import FAR, TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -124,6 +125,38 @@ def test_w8_gemm(M, K, N, dtype):
         assert_within(Y, *product(Q[:, :K].numpy(), s, W, t, bias), dtype, f"{M}x{K}x{N}")
     again = tg.tst_w8_gemm(Qd, sd, w, torch.from_numpy(b).cuda(), dtype=TYPES[dtype])
     assert torch.equal(again, Y)
+
+
+@pytest.mark.parametrize("tile,M,K,N", [("%s-%d-%d" % tile, *s) for tile, shapes in TILES.items() for s in shapes])
+def test_w8_gemm_on_every_tile(tile, M, K, N):
+    W, t, b, w = layer(K, N, 63)
+    q = rng(64, M, K).integers(-128, 128, (M, K)).astype(np.int8)
+    Q = torch.full((M, (K + 15) // 16 * 16 + 16), -77, dtype=torch.int8)
+    Q[:, :K] = torch.from_numpy(q)
+    s = (rng(65, M).random(M) / 100).astype(np.float32)
+    Qd, sd, bd = Q.cuda()[:, :K], torch.from_numpy(s).cuda(), torch.from_numpy(b).cuda()
+    want, bound = product(q, s, W, t, b)
+    for dtype in TYPES:
+        Y = tg.tst_w8_gemm(Qd, sd, w, bd, dtype=TYPES[dtype])
+        assert_within(Y, want, bound, dtype, f"{tile} {M}x{K}x{N}")
+        assert torch.equal(tg.tst_w8_gemm(Qd, sd, w, bd, dtype=TYPES[dtype]), Y)
+    odd = torch.empty(M * N + 1, device="cuda")[1:].view(M, N)   # off the border of wider stores
+    tg.tst_w8_gemm(Qd, sd, w, Y=odd)
+    assert_within(odd, *product(q, s, W, t, None), "f32", f"{tile} {M}x{K}x{N}")
+
+
+@pytest.mark.parametrize("M,K,N", FAR.values())
+def test_w8_gemm_of_rows_far_apart_on_every_tile(M, K, N):
+    """Rows 4 MiB apart, the most there may be: offsets in a tile of 128 rows come to 2^29."""
+    W, t, b, w = layer(K, N, 66)
+    near = torch.zeros((M, (K + 15) // 16 * 16), dtype=torch.int8, device="cuda")
+    near[:, :K] = torch.from_numpy(rng(67, M, K).integers(-128, 128, (M, K)).astype(np.int8))
+    far = torch.empty((M, 1 << 22), dtype=torch.int8, device="cuda")
+    far[:, :K] = near[:, :K]
+    s = torch.ones(M, device="cuda")
+    Y = tg.tst_w8_gemm(far[:, :K], s, w)
+    assert torch.equal(Y, tg.tst_w8_gemm(near[:, :K], s, w))
+    assert_within(Y, *product(near[:, :K].cpu().numpy(), s.cpu().numpy(), W, t, None))
 
 
 @pytest.mark.parametrize("M,K,N", [(1, 131071, 3), (20, 131071, 5), (70, 131071, 33), (300, 131071, 260)])

@@ -39,6 +39,26 @@ def test_w8_bytes(K, N, want):
     assert operators._bytes("tst_w8_bytes", K, N) == want
 
 
+def test_the_gpu_tests_take_every_tile_of_the_8_bit_product(tmp_path):
+    """The rule itself, compiled for the host: a change of it may not leave a kernel without a test."""
+    from w8_tiles import FAR, TILES
+    src = tmp_path / "choice.cpp"
+    src.write_text('#include "w8_choice.h"\n#include <cstdio>\nint main()\n{\n'
+                   '    for (const auto &t : tst::kGemmTiles) std::printf("%s %d %d\\n", t.rows ? "rows" : "tiles", t.mt, t.nt);\n'
+                   '    int M, K, N;\n'
+                   '    while (std::scanf("%d%d%d", &M, &K, &N) == 3) {\n'
+                   '        const auto t = tst::choose_tile(M, K, N, 256);\n'
+                   '        std::printf("%s %d %d\\n", t.rows ? "rows" : "tiles", t.mt, t.nt);\n    }\n}\n')
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", f"-I{ROOT / 'paper_2510_06957_amd' / 'csrc'}", str(src), "-o", str(tmp_path / "choice")], check=True)
+    shapes = [(tile, s) for tile, all_ in TILES.items() for s in all_] + list(FAR.items())
+    out = subprocess.run([str(tmp_path / "choice")], input="\n".join("%d %d %d" % s for _, s in shapes), text=True, capture_output=True, check=True).stdout
+    tiles = [(k, int(m), int(n)) for k, m, n in (line.split() for line in out.splitlines())]
+    there, chosen = tiles[:len(TILES)], tiles[len(TILES):]
+    assert set(there) == set(TILES) and len(chosen) == len(shapes)
+    for (tile, shape), got in zip(shapes, chosen):
+        assert got == tile, shape
+
+
 def moe_struct(**change):
     fields = dict(struct_size=ctypes.sizeof(operators._MoeStruct), type=1, experts=8, width=64, inner=64)
     fields.update({n: 4096 for n in ("router", "gate", "up", "down", "gate_scale", "up_scale", "down_scale")})
