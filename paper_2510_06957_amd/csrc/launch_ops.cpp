@@ -21,6 +21,7 @@ decltype(&tst_moe) g_moe;
 decltype(&tst_logprobs_workspace_bytes) g_logprobs_bytes;
 decltype(&tst_logprobs) g_logprobs;
 PyObject *g_error;   // TstgemmError
+PyObject *g_w8_class, *g_moe_class;   // W8 and Moe
 PyObject *s_K, *s_N, *s_count, *s_packed, *s_scale, *s_raw, *s_device_index;
 
 // A tensor of torch's own class with memory of its own on the current device.
@@ -68,10 +69,13 @@ struct Layer {
     Layer(PyObject *w, PyObject *bias, int dev)
     {
         unsigned long long count = 0;
-        if (!int_attr(w, s_count, &count) || count != 1 || !int_attr(w, s_K, &K) || !int_attr(w, s_N, &N)) return;
+        if ((PyObject *)Py_TYPE(w) != g_w8_class || !int_attr(w, s_count, &count) || count != 1 || !int_attr(w, s_K, &K) || !int_attr(w, s_N, &N) || K < 1 ||
+            K > INT_MAX - 64 || N < 1 || N > INT_MAX - 16)
+            return;
+        const int64_t bytes = ((int64_t)K + 63) / 64 * 64 * (((int64_t)N + 15) / 16 * 16);   // tst_w8_bytes()
         PyObject *p = PyObject_GetAttr(w, s_packed), *s = PyObject_GetAttr(w, s_scale);   // (w keeps them)
         const at::Tensor *pt = p ? dense(p, dev, at::kByte) : nullptr, *st = s ? dense(s, dev, at::kFloat) : nullptr;
-        if (pt && st && st->numel() == (int64_t)N) {
+        if (pt && st && pt->numel() == bytes && st->numel() == (int64_t)N) {
             packed = pt->data_ptr();
             scale = static_cast<const float *>(st->data_ptr());
             ok = true;
@@ -162,7 +166,7 @@ PyObject *moe(PyObject *, PyObject *const *a, Py_ssize_t n)
         unsigned long long raw = 0, index = 0;
         int64_t stride = 0;
         const at::Tensor *x = rows(a[0], dev, &stride);
-        if (x == nullptr || !int_attr(a[1], s_raw, &raw) || !int_attr(a[1], s_device_index, &index) || raw == 0 || (int)index != dev ||
+        if (x == nullptr || (PyObject *)Py_TYPE(a[1]) != g_moe_class || !int_attr(a[1], s_raw, &raw) || !int_attr(a[1], s_device_index, &index) || raw == 0 || (int)index != dev ||
             !PyLong_CheckExact(a[2]) || !PyBool_Check(a[3]))
             Py_RETURN_NONE;
         const tst_moe_t *m = reinterpret_cast<const tst_moe_t *>(raw);
@@ -236,12 +240,12 @@ PyObject *logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind_ops(addresses of the seven in the loaded library, TstgemmError)
+// bind_ops(addresses of the seven in the loaded library, TstgemmError, W8, Moe)
 PyObject *bind_ops(PyObject *, PyObject *args)
 {
     unsigned long long p[7];
-    PyObject *error;
-    if (!PyArg_ParseTuple(args, "KKKKKKKO", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &error)) return nullptr;
+    PyObject *error, *w8, *moe_class;
+    if (!PyArg_ParseTuple(args, "KKKKKKKOOO", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &error, &w8, &moe_class)) return nullptr;
     g_gemm = reinterpret_cast<decltype(g_gemm)>(p[0]);
     g_linear_bytes = reinterpret_cast<decltype(g_linear_bytes)>(p[1]);
     g_linear = reinterpret_cast<decltype(g_linear)>(p[2]);
@@ -251,6 +255,10 @@ PyObject *bind_ops(PyObject *, PyObject *args)
     g_logprobs = reinterpret_cast<decltype(g_logprobs)>(p[6]);
     Py_INCREF(error);
     Py_XSETREF(g_error, error);
+    Py_INCREF(w8);
+    Py_XSETREF(g_w8_class, w8);
+    Py_INCREF(moe_class);
+    Py_XSETREF(g_moe_class, moe_class);
     Py_RETURN_NONE;
 }
 

@@ -41,7 +41,7 @@ def _ops():
             from . import _launch as native
             native.bind_ops(*(ctypes.cast(getattr(lib, name), _vp).value for name in (
                 "tst_w8_gemm", "tst_w8_linear_workspace_bytes", "tst_w8_linear", "tst_moe_workspace_bytes", "tst_moe",
-                "tst_logprobs_workspace_bytes", "tst_logprobs")), TstgemmError)
+                "tst_logprobs_workspace_bytes", "tst_logprobs")), TstgemmError, W8, Moe)
             _native = native
     return _lib
 
@@ -133,9 +133,17 @@ class W8:
     """8-bit weights in their device form (tst_w8_pack) with the scale of each output channel."""
 
     def __init__(self, K, N, count, packed, scale):
-        if packed.numel() != count * _bytes("tst_w8_bytes", K, N) or scale.numel() != count * N:
-            raise ValueError("packed and scale must be those of count matrices K x N")
         self.K, self.N, self.count, self.packed, self.scale = K, N, count, packed, scale
+        self._check()
+
+    def _check(self):
+        """The kernels go by K and N: what they read has to be there."""
+        import torch
+        p, s = self.packed, self.scale
+        if not (isinstance(p, torch.Tensor) and isinstance(s, torch.Tensor) and p.dtype == torch.uint8 and s.dtype == torch.float32 and p.is_contiguous()
+                and s.is_contiguous() and p.device == s.device and p.numel() == self.count * _bytes("tst_w8_bytes", self.K, self.N)
+                and s.numel() == self.count * self.N):
+            raise ValueError("packed (uint8) and scale (float32) must be those of count matrices K x N, contiguous and on one device")
 
 
 def _pack(W, what, stream):
@@ -171,6 +179,7 @@ def _layer(w, b, dev):
     import torch
     if not isinstance(w, W8) or w.count != 1 or w.packed.get_device() != dev:
         raise ValueError("w must be the W8 of one matrix on the operands' device")
+    w._check()
     return None if b is None else _dense(b, "b", torch.float32, (w.N,), dev)
 
 

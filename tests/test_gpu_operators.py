@@ -597,6 +597,33 @@ def test_more_rows_than_a_launch_takes():
         assert ((got - want).abs() <= 50 * U * (1 + want.abs())).all()
 
 
+def test_weights_are_those_of_the_pack():
+    """Objects that have the names of a W8 or a Moe, or whose sizes have been changed, are refused: the kernels read as much as K and N say."""
+    import types
+
+    from paper_2510_06957_amd import operators
+    W, t, b, w = layer(128, 64, 68)
+    X = tokens(3, 128, "bf16", 69)
+    Q, s = tg.tst_quantize(X)
+    native, moe, x = operators._native, packed(experts(4, 64, 32, "bf16", 70)), tokens(2, 64, "bf16", 71)
+    same = types.SimpleNamespace(K=128, N=64, count=1, packed=w.packed, scale=w.scale)
+    like = types.SimpleNamespace(_raw=moe._raw, device_index=moe.device_index, D=64, dtype=moe.dtype)
+    assert native.w8_linear(X, same, None) is None and native.w8_gemm(Q, s, same, None, None) is None and native.moe(x, like, 2, True) is None
+    for call in (lambda: tg.tst_w8_linear(X, same), lambda: tg.tst_w8_gemm(Q, s, same), lambda: tg.tst_moe(x, like, 2)):
+        with pytest.raises(ValueError):
+            call()
+    want = tg.tst_w8_linear(X, w)
+    for name, value in (("N", 32), ("K", 64), ("packed", w.packed[:4096]), ("scale", w.scale[:32]), ("scale", w.scale.cpu()), ("packed", w.packed.cpu())):
+        kept = getattr(w, name)
+        setattr(w, name, value)
+        assert native.w8_linear(X, w, None) is None and native.w8_gemm(Q, s, w, None, None) is None
+        for call in (lambda: tg.tst_w8_linear(X, w), lambda: tg.tst_w8_gemm(Q, s, w)):
+            with pytest.raises(ValueError):
+                call()
+        setattr(w, name, kept)
+    assert torch.equal(tg.tst_w8_linear(X, w), want)
+
+
 def test_large_strides():
     """Rows far apart, up to what the product takes; and offsets that pass 32 bits."""
     W, t, b, w = layer(96, 40, 56)

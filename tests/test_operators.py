@@ -174,3 +174,16 @@ def test_the_native_half_hands_back_what_is_not_on_a_gpu():
     for call in (lambda: native.w8_linear(x), lambda: native.w8_gemm(x), lambda: native.moe(x), lambda: native.logprobs(x)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_w8_takes_no_tensors_that_hold_less_than_the_kernels_read():
+    import torch
+    packed, scale = torch.zeros(2048, dtype=torch.uint8), torch.ones(32)
+    w = tg.W8(64, 32, 1, packed, scale)
+    for p, s in ((packed[:1].expand(2048), scale), (torch.zeros(4096, dtype=torch.uint8)[::2], scale), (packed, scale[:1].expand(32)),
+                 (packed, scale.to(torch.float16)), (packed.to(torch.bool), scale), (packed, scale.to("meta")), (packed.numpy(), scale), (packed, [1.0] * 32)):
+        with pytest.raises(ValueError):
+            tg.W8(64, 32, 1, p, s)
+    w.K = 65
+    with pytest.raises(ValueError):
+        w._check()
