@@ -24,12 +24,12 @@ PyObject *g_error;   // TstgemmError
 PyObject *g_w8_class, *g_moe_class;   // W8 and Moe
 PyObject *s_K, *s_N, *s_count, *s_packed, *s_scale, *s_raw, *s_device_index;
 
-// A tensor of torch's own class with memory of its own on the current device.
+// A tensor of torch's own class with memory of its own on the current device, which holds its values as they are.
 const at::Tensor *plain(PyObject *o, int dev)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.get_device() != dev) return nullptr;
+    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.is_neg() || t.get_device() != dev) return nullptr;
     return &t;
 }
 const at::Tensor *dense(PyObject *o, int dev, at::ScalarType type)

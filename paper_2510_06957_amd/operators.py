@@ -75,6 +75,8 @@ def _rows(x, what, dtype=None):
         raise ValueError(f"{what} must be on the current device")
     n, k = x.shape
     stride = x.stride(0) if n > 1 else max(k, 1)
+    if x.is_neg():   # a view whose memory holds the values negated
+        raise ValueError(f"{what} must hold its values as they are (resolve_neg())")
     if k < 1 or (k > 1 and x.stride(1) != 1) or stride < k:
         raise ValueError(f"{what} must have contiguous rows of at least one entry that do not overlap")
     return n, k, stride
@@ -83,7 +85,7 @@ def _rows(x, what, dtype=None):
 def _dense(x, what, dtype, shape, dev):
     import torch
     if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype == dtype and tuple(x.shape) == tuple(shape) and x.is_contiguous()
-            and x.get_device() == dev):
+            and not x.is_neg() and x.get_device() == dev):
         raise ValueError(f"{what} must be a contiguous {dtype} CUDA tensor of shape {list(shape)} on the operands' device")
     return x.data_ptr()
 
@@ -149,7 +151,7 @@ class W8:
 def _pack(W, what, stream):
     """W: [K, N] or [count, K, N]"""
     import torch
-    if not (isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.int8 and W.dim() in (2, 3) and W.is_contiguous() and W.numel()):
+    if not (isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.int8 and W.dim() in (2, 3) and W.is_contiguous() and not W.is_neg() and W.numel()):
         raise ValueError(f"{what} must be a contiguous int8 CUDA tensor [K, N] or [count, K, N]")
     dev = W.get_device()
     if dev != torch.cuda.current_device():

@@ -624,6 +624,22 @@ def test_weights_are_those_of_the_pack():
     assert torch.equal(tg.tst_w8_linear(X, w), want)
 
 
+def test_views_that_negate_are_refused():
+    """The imaginary part of a conjugate is a view of memory that holds the values negated."""
+    from paper_2510_06957_amd import operators
+    W, t, b, w = layer(1, 5, 72)
+    z = torch.randn((6, 1), dtype=torch.complex64, device="cuda")
+    x = z.conj().imag
+    assert x.is_neg()
+    bias = torch.randn(5, device="cuda")
+    for call in (lambda: tg.tst_quantize(x), lambda: tg.tst_w8_linear(x, w), lambda: tg.tst_logprobs(x),
+                 lambda: tg.tst_w8_linear(x.resolve_neg(), w, torch._neg_view(bias))):
+        with pytest.raises(ValueError):
+            call()
+    assert operators._native.w8_linear(x, w, None) is None and operators._native.logprobs(x, None, 1) is None
+    assert torch.equal(tg.tst_w8_linear(x.resolve_neg(), w), tg.tst_w8_linear(-z.imag.contiguous(), w))
+
+
 def test_large_strides():
     """Rows far apart, up to what the product takes; and offsets that pass 32 bits."""
     W, t, b, w = layer(96, 40, 56)
