@@ -480,6 +480,21 @@ def test_logprobs_alternatives_of_rows_with_nan(V, R, dtype):
         assert torch.isnan(of_token).all() and torch.isnan(entropy).all() and torch.isnan(of_top).all()
 
 
+@pytest.mark.parametrize("low", [-1e4, -3e4, -1e9])
+@pytest.mark.parametrize("R", [9, 1030])
+@pytest.mark.parametrize("V,top", [(700, 20), (40007, 20), (70000, 64)])
+def test_logprobs_of_rows_masked_with_finite_values(V, top, R, low):
+    """Masks that are neither infinite nor the type's lowest value: entries like any other, that tie."""
+    for dtype in ("f32", "bf16", "f16")[:2 if low == -1e9 else 3]:
+        Z = torch.zeros((R, V), dtype=TYPES[dtype], device="cuda")
+        Z[:9] = logits(9, V, dtype, 73)
+        n = torch.arange(V, device="cuda")
+        keep = [n % 1000 == 7, n < 3, n >= V - 2, n == V // 2, n % 64 == 0, n < 0, n % 2 == 0, (n > V // 3) & (n < V // 3 + 30), n >= 0]
+        for r, k in enumerate(keep):
+            Z[r, ~k] = low
+        check_logprobs(Z, torch.arange(R) % V, top, slice(0, 9))
+
+
 def test_logprobs_of_tokens_outside_the_vocabulary():
     Z = logits(3, 500, "bf16", 27)
     t = torch.tensor([[-1, 4], [500, 499], [2 ** 40, -2 ** 40]], device="cuda")
