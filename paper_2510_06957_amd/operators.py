@@ -47,6 +47,9 @@ def _ops():
 
 
 def _call(name, *args):
+    for value, kind in zip(args, _SIGNATURES[name]):
+        if kind is _ci and not -2 ** 31 <= value < 2 ** 31:   # ctypes would take its low 32 bits
+            raise TstgemmError(-1, name)
     rc = getattr(_ops(), name)(*args)
     if rc != 0:
         raise TstgemmError(rc, name)

@@ -187,3 +187,19 @@ def test_w8_takes_no_tensors_that_hold_less_than_the_kernels_read():
     w.K = 65
     with pytest.raises(ValueError):
         w._check()
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """... where what is left of them in 32 bits would be a size of its own."""
+    n = ctypes.c_size_t()
+    s = moe_struct()
+    a = 1 << 20
+    for name, args in (("tst_logprobs_workspace_bytes", (2 ** 32 + 5, 100, 3)), ("tst_logprobs_workspace_bytes", (5, 2 ** 32 + 100, 3)),
+                       ("tst_logprobs_workspace_bytes", (5, 100, 2 ** 32 + 3)), ("tst_moe_workspace_bytes", (ctypes.byref(s), 2 ** 32 + 5, 2)),
+                       ("tst_moe_workspace_bytes", (ctypes.byref(s), 5, 2 ** 32 + 2)), ("tst_w8_bytes", (2 ** 32 + 64, 16)), ("tst_w8_bytes", (64, -2 ** 32 + 16))):
+        with pytest.raises(tg.TstgemmError) as e:
+            operators._bytes(name, *args)
+        assert e.value.code == EINVAL
+    with pytest.raises(tg.TstgemmError):
+        operators._call("tst_quantize", a, 0, 2 ** 32 + 64, a, 2 ** 32 + 64, a, 2 ** 32, 64, None)   # 0 rows are left
+    operators._call("tst_quantize", a, 0, 2 ** 40, a, 2 ** 40, a, 0, 64, None)                       # strides have 64 bits
