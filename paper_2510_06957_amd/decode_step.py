@@ -78,12 +78,15 @@ def generate(model, tokens, steps, top=4):
     return [torch.stack(o) for o in zip(*out)]
 
 
-def main():
+def main(argv=None):
     ap = argparse.ArgumentParser()
     ap.add_argument("--tokens", type=int, default=4)
     ap.add_argument("--steps", type=int, default=8)
-    a = ap.parse_args()
-    model = Model()
+    a = ap.parse_args(argv)
+    vocabulary = 2000
+    if not 1 <= a.tokens <= vocabulary or a.steps < 1:   # an index behind the embedding would end the process on the GPU
+        ap.error(f"--tokens takes 1 to {vocabulary}, --steps 1 or more")
+    model = Model(vocabulary=vocabulary)
     ids, of_top, entropy = generate(model, torch.arange(a.tokens, device="cuda"), a.steps)
     for s in range(a.steps):
         print(f"step {s}: " + "  ".join(f"{t} (log p {p:.2f}, entropy {h:.2f})" for t, p, h in zip(ids[s].tolist(), of_top[s].tolist(), entropy[s].tolist())))

@@ -203,3 +203,11 @@ def test_sizes_beyond_32_bits_are_refused():
     with pytest.raises(tg.TstgemmError):
         operators._call("tst_quantize", a, 0, 2 ** 32 + 64, a, 2 ** 32 + 64, a, 2 ** 32, 64, None)   # 0 rows are left
     operators._call("tst_quantize", a, 0, 2 ** 40, a, 2 ** 40, a, 0, 64, None)                       # strides have 64 bits
+
+
+@pytest.mark.parametrize("argv", [["--tokens", "2001"], ["--tokens", "0"], ["--tokens", "-1"], ["--steps", "0"]])
+def test_the_example_refuses_tokens_and_steps_that_are_not_there(argv, capsys):
+    from paper_2510_06957_amd import decode_step
+    with pytest.raises(SystemExit) as e:
+        decode_step.main(argv)
+    assert e.value.code == 2 and "--tokens" in capsys.readouterr().err
