@@ -76,8 +76,7 @@ int tst_w8_linear(const void *X, int type, int64_t x_stride, const void *packed,
  *   g    = gate_scale[e][f] sum_d X[t][d] gate[e][d][f],  u the same with up,  h[f] = g / (1 + e^-g) * u
  *   Y[t][c] = sum over the chosen e of down_scale[e][c] sum_f (p h[f]) down[e][f][c]
  * Weights are 8-bit with a scale for each output channel (ternary matrices are a case of them); X, router and Y have one type.  The
- * activations keep the bits of their type in the products; h keeps 16 bits of its mantissa where the type has 16 bits and 24 where
- * it is fp32, sums are fp32.  A token that holds an infinity or a NaN has NaN results and does not touch the others.
+ * activations keep the bits of their type in the products, h the 24 of fp32, and sums are fp32.  A token that holds an infinity or a NaN has NaN results and does not touch the others.
  */
 typedef struct tst_moe {
     size_t struct_size;        /* sizeof(tst_moe_t) */

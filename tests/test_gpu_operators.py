@@ -318,6 +318,35 @@ def test_moe_of_experts_with_many_members(T, E, k, D, F, most, dtype):
     assert torch.equal(tg.tst_moe(X, moe, k)[0], Y)
 
 
+@pytest.mark.parametrize("T", [5, 20, 60])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_moe_keeps_the_bits_of_h(T, dtype):
+    """Columns of the result that are the difference of two entries of h some 2^-13 apart.  Each token has one entry that is not zero, so that
+    sums round only where they have to: g and u by 4 units (planes, scale), silu of a positive g turns them into at most 1.3 of that and adds 4 for
+    the exponential, the sum and the division, the products with u, its error and p 6, the cut to 24 bits 1; the second product has six terms."""
+    r = rng(74, T)
+    D, F = 16, 32
+    x = np.zeros((T, D))
+    x[:, 0] = 1 + r.random(T)
+    X = torch.from_numpy(x).to(TYPES[dtype]).cuda()
+    w = dict(router=torch.ones((1, D), dtype=TYPES[dtype]), gate=torch.from_numpy(r.integers(-128, 128, (1, D, F)).astype(np.int8)),
+             up=torch.from_numpy(r.integers(-128, 128, (1, D, F)).astype(np.int8)), down=torch.zeros((1, F, D), dtype=torch.int8), gate_scale=torch.full((1, F), 0.03), up_scale=torch.from_numpy((0.01 + 0.01 * r.random((1, F))).astype(np.float32)),
+             down_scale=torch.from_numpy((0.5 + r.random((1, D))).astype(np.float32)))
+    for c in range(D):
+        w["gate"][0, 0, 2 * c] = w["gate"][0, 0, 2 * c + 1] = int(r.integers(20, 100))
+        w["up"][0, 0, 2 * c] = w["up"][0, 0, 2 * c + 1] = int(r.integers(20, 128))
+        w["up_scale"][0, 2 * c + 1] = w["up_scale"][0, 2 * c] * (1 - 2.0 ** -13 * (1 + r.random()))
+        w["down"][0, 2 * c, c], w["down"][0, 2 * c + 1, c] = 64, -64
+    g = (f64(X) @ f64(w["gate"][0])) * f64(w["gate_scale"][0])
+    h = g / (1 + np.exp(-g)) * (f64(X) @ f64(w["up"][0])) * f64(w["up_scale"][0])
+    want = (h @ f64(w["down"][0])) * f64(w["down_scale"][0])
+    bound = (4 * 1.3 + 4 + 4 + 6 + 1 + 6 + 2) * U * (h @ np.abs(f64(w["down"][0]))) * f64(w["down_scale"][0])
+    assert (bound < 0.05 * np.abs(want)).all()
+    Y, ids, p = tg.tst_moe(X, packed(w), 1)
+    assert (p == 1).all()
+    assert_within(Y, want, bound, dtype, "Y")
+
+
 def test_moe_ties_go_to_the_lowest_expert():
     r = rng(13)
     rows = r.standard_normal((3, 80))
