@@ -6,8 +6,11 @@
 // largest is a lower bound of the row's n-th largest logit, so only what reaches it (seldom much more than n) goes into a list in the
 // LDS, with its place; a member's rank is the number of members before it.
 //
-// Bound by memory and, about as much, by the exponentials: 1024 x 131072 bf16 with one alternative 55 us, 4.9 TB/s, with 20 of them 85.  Few
-// rows are bound by latency: 1 x 131072 with 20 alternatives 10.9 us and 5.7 for joining the splits.
+// Bound by memory and, about as much, by the exponentials: 1024 x 131072 bf16 with one alternative 55 us, 4.9 TB/s.  With 20 of them it takes
+// 92, and 700 x 30000 35: the wavefronts learn their bounds each for itself.  Rows off 16-byte borders go an entry at a time: 1024 x 131071
+// 132 us.  Few rows are bound by latency: 1 x 131072 with 20 alternatives 10.5 us and 5.2 for joining the splits.
+// Entries that are infinite or the type's lowest value are known for masked ones and skipped; masks of other values (-1e9) tie like any logits,
+// and a row that has hardly any others takes about twice as long (1024 x 131072 bf16 with 20 alternatives 209 us in place of 108).
 #include "ops_internal.h"
 
 namespace tst {
@@ -40,6 +43,8 @@ constexpr int kShort = 192, kRoom = kMaxTop + 64 * 8;
 constexpr float kNan = __builtin_nanf("");
 typedef unsigned long long Key;
 
+// e^d below is 2^fl32(d log2 e), off by up to 2^-24 of d log2 e.  With the exponent's rounding put back by an fma the results' errors against 64 bits
+// are the same (1024 x 131072 bf16: 5 to 8e-8, both ways) and the kernel takes 70 us in place of 60.
 struct Shared {
     Key list[kWaves][kRoom], best[kWaves][kMaxTop], sorted[kMaxTop];
     float sums[3][kWaves], lost[kWaves];
@@ -387,7 +392,10 @@ k_logprobs_join(const LogArgs a)
     finish<TYPE>(a, r, all, sum, weighted, sorted);
 }
 
-// Splits of a row: while there are fewer than two workgroups for a compute unit, of a chunk for each wavefront at least.
+// Splits of a row: while there are fewer than two workgroups for a compute unit, of a chunk for each wavefront at least.  us from Python in splits and
+// as whole rows, bf16, with 1 and 20 alternatives: 1 x 131072 10.7 16.2 and 21 56, 128 x 131072 20.9 38.3 and 29.0 62.0, 256 x 131072 30.0 55.6 and
+// 30.0 62.3, 400 x 131072 35.9 64.0 and 34.0 69.7; 64 x 32000 10.9 16.1 and 12.2 28.1, 256 x 32000 15.6 28.0 and 12.9 29.2, 400 x 32000 18.6 33.9
+// and 15.2 31.8: where two splits are all, they pay for long rows and many alternatives alone.
 int splits_of(int R, int V, int type)
 {
     const int64_t least = (int64_t)kThreads * kFewVectors * (16 / type_bytes(type));

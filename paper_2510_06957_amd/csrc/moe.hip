@@ -252,8 +252,9 @@ __device__ __forceinline__ void meet()
 // k_moe_up: h = silu(x gate) (x up) p for each token and expert it chose, as operands.  Every workgroup finds the experts by itself;
 // the first one writes them out.  An item of work is one expert x 16 columns of its gate and up, for all tokens; wavefronts share D
 // and hold U blocks of it on the way: a block's registers are loaded again, for the round or the item to come, as soon as it is used.
-// Bound by the weights' bytes: one token, two experts of 4096 x 11008 (180 MB) 36.8 us, 4.9 TB/s; 16 tokens, 64 experts of 2048 x 1024, 4
-// each (some 170 MB) 37.
+// Bound by the weights' bytes: one token, two experts of 4096 x 11008 (180 MB) 36.2 us, 5.0 TB/s; 16 tokens, 64 experts of 2048 x 1024, 4
+// each (some 170 MB) 36.  More tokens are not: 64 of them on all 64 experts (268 MB) 98 us, in fp32 on 128 of 2048 x 768 (403 MB) 262: every workgroup
+// chooses for all tokens before it asks for a weight, and tiles of members behind the second ask for X when they need it.
 constexpr int kUpWaves = 8;
 
 template <int TYPE, int NT>
@@ -394,7 +395,8 @@ k_moe_up(const MoeArgs a)
 // ------------------------------------------------------------------------------------------------------------------
 // k_moe_down: 64 columns of Y for all tokens.  The blocks of all experts in use, one expert behind another, are shared by the workgroups of
 // a split and their wavefronts, each with a run of them and U on the way.  Four pieces of weights use one operand of h, which
-// comes from the L2: with 16 columns the registers of h on its way left too few for the weights (86 MB of weights 41 us; now 20, 4.3 TB/s).
+// comes from the L2: with 16 columns the registers of h on its way left too few for the weights (86 MB of weights 41 us; now 20.7, 4.2 TB/s).
+// 64 tokens: 134 MB 52 us, 361 MB (8 experts of 4096 x 11008) 194.
 // Between experts a wavefront scales its sums with the expert's channels and adds them to those of the token.
 constexpr int kDownCols = 4;   // pieces of 16
 constexpr int kDownWaves = 8;
@@ -558,7 +560,9 @@ k_moe_join(const MoeArgs a)
     static_cast<typename E::bits *>(a.Y)[i] = E::put(y);
 }
 
-// Workgroups that share the experts of a column tile, so that every compute unit has one; each has at least one block for a wavefront.
+// Workgroups that share the experts of a column tile, so that every compute unit has one where D reaches 1024 (kMaxSplits); each has at least one
+// block for a wavefront.  us of whole calls as chosen, with one and with 4, bf16: one token, 2 of 8 experts 4096 x 11008 72 90 73; 16 tokens,
+// 4 of 64 experts 2048 x 1024 74 133 81; 4 tokens, 6 of 64 42 67 44; 16 tokens, 2 of 16 experts 1024 x 4096 68 165 84.
 constexpr int kMaxSplits = 16;
 int most_splits(int D)
 {
@@ -600,6 +604,8 @@ template <int TYPE, int NT> hipError_t launch_moe_nt(const MoeArgs &a, hipStream
     if (a.wide) k_moe_router<TYPE, true><<<router, kRouterWaves * 64, 0, stream>>>(a);
     else k_moe_router<TYPE, false><<<router, kRouterWaves * 64, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
+    // Two workgroups of k_moe_up for each compute unit, also where registers (16 tokens and more in fp32 or fp16) or the LDS (hundreds of experts) hold
+    // one: the others start when the first are done.
     const size_t lds = Chosen<NT>::bytes(a);
     const int64_t items = (int64_t)(a.E < a.T * a.top ? a.E : a.T * a.top) * (pad64(a.F) / 16), groups = 2 * (int64_t)compute_units();
     k_moe_up<TYPE, NT><<<(unsigned)(items < groups ? items : groups), kUpWaves * 64, lds, stream>>>(a);
@@ -663,6 +669,8 @@ int tst_moe(const void *X, int64_t x_stride, const tst_moe_t *moe, int top_k, in
         const hipError_t e = tst::for_type(m.type, [&](auto type) {
             constexpr int TYPE = decltype(type)::value;
             hipStream_t st = static_cast<hipStream_t>(stream);
+            // tiles of tokens: 16 tokens with 1, 2 and 4 of them 74 75 79 us (bf16, 4 of 64 experts 2048 x 1024) and 85 104 106 (fp32), 32 tokens with
+            // 2 and 4 115 and 118, 170 and 172
             return n <= 16 ? tst::launch_moe_nt<TYPE, 1>(a, st) : n <= 32 ? tst::launch_moe_nt<TYPE, 2>(a, st) : tst::launch_moe_nt<TYPE, 4>(a, st);
         });
         if (e != hipSuccess) return TSTGEMM_EHIP;

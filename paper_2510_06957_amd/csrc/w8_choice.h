@@ -5,9 +5,9 @@ namespace tst {
 
 constexpr int kStepK = 128;   // of K that a workgroup takes at a time
 
-// Which kernel and tile.  All of them are bound by what a compute unit can load (about 65 GB/s each, over all sizes measured), so the
-// choice is the one for which the busiest compute unit loads least: rounds of workgroups x bytes of a workgroup, and for k_w8_rows the
-// sums that its wavefronts exchange.  Measured with K = N = 4096 (us): 256 rows 11.8 with 64 x 64 tiles of k_w8_rows, 23 with k_w8_tiles<4>,
+// Which kernel and tile.  With all of them the busiest compute unit loads some 65 GB/s, over all sizes measured (no limit of the hardware: a copy
+// of tiles through the LDS moves 110), so the choice is the one for which it loads least: rounds of workgroups x bytes of a workgroup, and for
+// k_w8_rows the sums that its wavefronts exchange.  Measured with K = N = 4096 (us): 256 rows 11.8 with 64 x 64 tiles of k_w8_rows, 23 with k_w8_tiles<4>,
 // 31 with k_w8_tiles<8>; 512 rows 20 / 24 / 31; 1024 rows 36 / 24 / 32; 2048 rows 70 / 38 / 36; 4096 rows 61 with k_w8_tiles<8>, 72
 // with <4>.  64 x 16384 x 4096: 17.3 with 32 x 32 tiles of k_w8_rows, 18.3 with 64 x 16, 26 with 64 x 64.
 struct GemmTile {

@@ -8,8 +8,9 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------------------------
 // k_quantize: one workgroup per row; the row's largest magnitude, then its codes.  Magnitudes are compared as integers: of
-// non-negative floats the bits order as the values do, with infinity and NaN above every number.  Bound by memory for many rows (2048 x
-// 4096 bf16 7.0 us, 3.6 TB/s read and written), by latency for few (37 x 2053 fp16 4.6 us).
+// non-negative floats the bits order as the values do, with infinity and NaN above every number.  2048 x 4096 bf16 7.0 us, 3.6 TB/s read and
+// written where a large copy reaches 5.2: a workgroup has two loads a thread on the way, a meeting behind them, then the stores, and is done.
+// Few rows are bound by latency (37 x 2053 fp16 4.7 us).
 // The row stays in the registers on the way if it fits (64 bytes for a thread), else it is read twice.
 constexpr int kQuantBytes = 64;
 
@@ -241,7 +242,10 @@ k_w8_rows(const GemmArgs a)
 // ------------------------------------------------------------------------------------------------------------------
 // k_w8_few: tst_w8_linear() for a token or a few in one launch: every workgroup quantises them by itself, while its first weights are on
 // their way, keeps the codes in the LDS, and goes on as k_w8_rows with one row tile and one column tile.  Bound by the weights: 1 x 4096 x
-// 11008 7.6 us on the GPU, 5.9 TB/s (the codes by a kernel of their own: 3.3 and 8.6 us; two column tiles 8.8).
+// 11008 7.6 us on the GPU, 5.9 TB/s (two column tiles 8.8).  us from Python, and of the two launches of other calls, bf16, 1 to 4 rows:
+// 4096 x 11008 8.8 9.8 11.3 12.6 and 12.5 12.7 12.4 12.7, 4096 x 4096 5.3 6.3 5.8 7.7 and 9.4 9.6 9.3 9.4, 1024 x 4096 5.3 and 9.7 each,
+// 8192 x 4096 8.2 9.7 and 10.4 10.5, 16384 x 4096 13.7 and 14.6: what a further row costs is what every workgroup quantises again, and
+// with kFewCodes codes in all it comes to the launch that it saves.
 constexpr int kFewRows = 4, kFewCodes = 16384;   // rows, and rows x (K padded to kStepK), at most
 
 template <int TYPE>
@@ -348,9 +352,9 @@ k_w8_few(const GemmArgs a, const typename Entry<TYPE>::bits *X, int64_t x_stride
 // ------------------------------------------------------------------------------------------------------------------
 // k_w8_tiles: 256 columns x 16 MF rows of Y for a workgroup of four wavefronts, 64 columns x all its rows each.  What a wavefront
 // takes of W nobody else in the workgroup needs, so it goes from memory straight into the registers (a piece of the packed form is an
-// operand of the matrix instruction); X goes through the LDS, 128 of K at a time in two buffers, in slots as in k_w8_rows.  Bound by what a
-// compute unit can load: 48 KiB a step for 256 x 128 results.  4096 x 8192 x 8192 217 us, 2.53 POP/s (a library's product of this size 236;
-// instructions of 32 x 32 x 32 9 % slower; a tile of 256 x 256 does not fit the registers), 2048 x 4096 x 4096 38 us.
+// operand of the matrix instruction); X goes through the LDS, 128 of K at a time in two buffers, in slots as in k_w8_rows.  Bound by its
+// loads: 48 KiB a step for 256 x 128 results.  4096 x 8192 x 8192 217 us, 2.53 POP/s (a library's product of this size 236;
+// instructions of 32 x 32 x 32 9 % slower; a tile of 256 x 256 does not fit the registers of four wavefronts), 2048 x 4096 x 4096 38 us.
 constexpr int kTileThreads = 256, kTileCols = 256;
 
 template <int TYPE, int MF>
@@ -496,7 +500,8 @@ hipError_t launch_quantize(const void *X, int type, int64_t x_stride, int8_t *Q,
         constexpr int T = decltype(t)::value, V = 16 / sizeof(bits);
         const bool wide = aligned(X, 16) && K % V == 0 && x_stride % V == 0 && aligned(Q, V) && q_stride % V == 0;
         const bits *x = static_cast<const bits *>(X);
-        // few rows get more threads each (1 x 16385 fp16 5 us in place of 20)
+        // Few rows get more threads each.  With rows off 16-byte borders, an entry a load, 16 to 300 rows of 16384 bf16 take 8.6 us with 1024 threads
+        // and 14 with 256, 1024 rows of 4096 11.1 and 8.9 (from Python); on borders the two differ by less than a call's own time.
         const bool few = M < compute_units();
         if (wide && few) k_quantize<T, true, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
         else if (few) k_quantize<T, false, 1024><<<M, 1024, 0, stream>>>(x, x_stride, Q, q_stride, scale, K);
