@@ -1,0 +1,516 @@
+// Attention of new tokens over a paged cache of 8-bit keys and values (tst_kv_attention).
+//
+// Z^T = K Q^T and Y^T = V^T P^T, so that a query's logits, weights and sums stay in the lanes with its number (mod 16) from one product to the next: no
+// lane hands a weight to another.  A wavefront takes 64 tokens, four blocks of 16, at a time: quarter g of its lanes holds the logits of block g, and with
+// them one scale of keys and one of values.  The 16 x 16 x 32 instruction does not mind in which order the rows of its operands stand, so row m of the
+// t-th tile of keys is token 4 t + m % 4 of block m / 4, and a lane's 16 weights are those that the 16 codes of one channel in its block's layout meet.
+//
+// Codes become fp16 exactly (1024 + code + 128 by its bits, less 1152).  A query's row is scaled by a power of two so that its largest entry is in [2^14, 2^15) and
+// cut into fp16 (11 bits, and 11 more in a second plane for fp32).  Weights meet a value's scale relative to the largest seen so far, times 2^15: with 11 bits (22 for
+// fp32) down to 2^-29 of the largest, an absolute 2^-40 of it below.  Sums are fp32.
+//
+// The keys of a sequence are cut into chunks of one length, found from all sequences' lengths on the device so that the workgroups have about as much to do
+// each whatever the batch is; the host knows how many there are at most.  Chunks of one tile of rows are joined by k_join.
+#include "attention_internal.h"
+
+namespace tst {
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = 4, kUnit = 64;   // tokens of a wavefront at a time
+constexpr int kLeastChunk = kWaves;     // units
+constexpr float kNan = __builtin_nanf("");
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLeastScale = 1e-36f;   // of values, as the reference that weights are relative to
+
+struct KvArgs {
+    Cache cache;
+    Sequences seqs;
+    Rows q;
+    int q_heads, group, rows;   // query heads of a key head; rows of a tile: 16 for each row tile
+    int wanted;                 // chunks of a head that are wanted in all; 0: no sequence is cut
+    float scale;
+    void *y;
+    f32x4 *sums;                // [heads][items][tiles][64 lanes]
+    float2 *states;             // [heads][items][16 x row tiles]: largest logit, sum of weights
+    int items;                  // of a head, at most
+};
+
+// What a wavefront knows of the call: the chunks' length, and which piece of which sequence an item is.
+struct Item {
+    int seq, tile, chunk, chunks;   // chunks of the tile; seq -1: none
+    int64_t first;                  // number of the tile's first chunk
+};
+
+__device__ __forceinline__ int units_of(const KvArgs &a, int i)
+{
+    const int most = a.seqs.columns << a.cache.page_shift;   // a length behind the table's end meets one block that is not there
+    return (min(max(a.seqs.lens[i], 0), most + 1) + kUnit - 1) / kUnit;
+}
+__device__ __forceinline__ int tiles_of(const KvArgs &a, int i)
+{
+    return (int)(((int64_t)span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + a.rows - 1) / a.rows);
+}
+
+__device__ __forceinline__ int64_t wave_sum(int64_t v)
+{
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// The length of chunks, in units of 64 tokens.
+__device__ __forceinline__ int chunk_length(const KvArgs &a)
+{
+    const int lane = threadIdx.x % 64;
+    int64_t all = 0;
+    for (int i = lane; i < a.seqs.count; i += 64) all += (int64_t)tiles_of(a, i) * units_of(a, i);
+    all = wave_sum(all);
+    const int64_t length = (all + a.wanted - 1) / a.wanted;
+    return (int)min(max(length, (int64_t)kLeastChunk), (int64_t)1 << 30);
+}
+
+// Item `at`: sequences in order, a sequence's tiles in order, a tile's chunks in order.
+__device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t at)
+{
+    const int lane = threadIdx.x % 64;
+    int64_t before = 0;
+    for (int base = 0; base < a.seqs.count; base += 64) {
+        const int i = base + lane;
+        int64_t mine = 0;
+        int chunks = 0;
+        if (i < a.seqs.count) {
+            chunks = max((units_of(a, i) + length - 1) / length, 1);
+            mine = (int64_t)tiles_of(a, i) * chunks;
+        }
+        int64_t upto = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const unsigned long long behind = __ballot(before + upto > at);
+        if (behind) {
+            const int l = __ffsll(behind) - 1;
+            const int n = __shfl(chunks, l);
+            const int64_t start = before + __shfl(upto, l) - __shfl(mine, l);
+            const int rest = (int)(at - start);
+            return Item{base + l, rest / n, rest % n, n, at - rest % n};
+        }
+        before += __shfl(upto, 63);
+    }
+    return Item{-1, 0, 0, 0, 0};
+}
+
+// Four codes as fp16: 1024 + (code + 128) by its bits, less 1152.
+__device__ __forceinline__ void widen(unsigned four, f16x2 &lo, f16x2 &hi)
+{
+    const unsigned u = four ^ 0x80808080u;
+    const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+    lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(u, 0x64646464u, 0x00050004u)) + off;
+    hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(u, 0x64646464u, 0x00070006u)) + off;
+}
+__device__ __forceinline__ f16x8 widen8(unsigned a, unsigned b)
+{
+    f16x2 v[4];
+    widen(a, v[0], v[1]);
+    widen(b, v[2], v[3]);
+    return __builtin_shufflevector(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3), __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <int TYPE, int ROW, int RT> struct Shape {
+    static constexpr int kPlanes = TYPE == TST_F32 ? 2 : 1;
+    static constexpr int kSteps = ROW / 32;      // of 32 channels
+    static constexpr int kWide = ROW / 64;       // loads of 16 bytes of a lane in a row of keys; 8 more bytes where ROW % 64 = 32
+    static constexpr int kTiles = ROW / 16;      // of 16 channels
+};
+// The channel that entry i of step j stands for in a lane of quarter g: 16 bytes of a row are two steps.
+template <int ROW> __device__ __forceinline__ int channel(int j, int g) { return j < ROW / 64 * 2 ? j / 2 * 64 + g * 16 + j % 2 * 8 : j / 2 * 64 + g * 8; }
+
+template <int TYPE, int ROW, int RT> struct Keys {
+    u32x4 wide[4][Shape<TYPE, ROW, RT>::kWide];
+    u32x2 rest[4];
+    float k_scale, v_scale;
+};
+
+// Adds what another wavefront or chunk has, relative to largest logits of its own.
+__device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
+
+template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(const KvArgs &a, const Span &rows, int tile, int head, const f32x4 (&o)[RT][ROW / 16], const float (&sum)[RT], const int (&limit)[RT])
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    const int lane = threadIdx.x % 64, g = lane / 16, size = a.cache.size;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int64_t rho = (int64_t)tile * a.rows + rt * 16 + lane % 16;
+        if (rho >= (int64_t)rows.n * a.group) continue;
+        const int t = (int)(rho / a.group), h = head * a.group + (int)(rho - (int64_t)t * a.group);
+        Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
+        const float inverse = limit[rt] == 0 ? 0.f : 1.f / sum[rt];
+        const bool whole = (size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
+#pragma unroll
+        for (int dt = 0; dt < ROW / 16; ++dt) {
+            const int d = 16 * dt + 4 * g;
+            Bits b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = Entry<TYPE>::put(o[rt][dt][e] * inverse);
+            if (whole) {
+                if (d < size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), b, sizeof(b));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < size) out[d + e] = b[e];
+            }
+        }
+    }
+}
+
+template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves) k_kv_attention(KvArgs a)
+{
+    typedef Shape<TYPE, ROW, RT> S;
+    typedef typename Entry<TYPE>::bits Bits;
+    __shared__ f32x4 shared[kWaves / 2][RT * S::kTiles][64];
+    __shared__ float2 states[kWaves][RT][16];
+    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y;
+    Item it;
+    int begin = 0, end = 0;
+    if (a.wanted) {
+        const int length = uniform(chunk_length(a));
+        it = find_item(a, length, blockIdx.x);
+        if (it.seq < 0) return;
+        begin = it.chunk * length;
+        end = min(begin + length, units_of(a, it.seq));
+    } else {
+        // tiles of sequence i have the numbers from offsets[i] * group / rows + i on
+        auto base = [&](int i) { return (int64_t)(a.seqs.offsets ? min(max(a.seqs.offsets[i], 0), a.seqs.tokens) : i) * a.group / a.rows + i; };
+        int lo = 0, n = a.seqs.count;
+        while (n > 1) {
+            const int step = (n + 63) / 64, i = lo + lane * step;
+            const bool before = lane * step < n && base(min(i, a.seqs.count - 1)) <= (int)blockIdx.x;
+            const int c = max(__popcll(__ballot(before)), 1) - 1;
+            lo += c * step;
+            n = min(step, n - c * step);
+        }
+        const int first = (int)base(lo);
+        it = Item{lo, (int)blockIdx.x - first, 0, 1, 0};
+        if (it.tile < 0 || it.tile >= tiles_of(a, lo)) return;
+        end = units_of(a, lo);
+    }
+    const int seq = uniform(it.seq), tile = uniform(it.tile);
+    begin = uniform(begin), end = uniform(end);
+    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
+    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition);
+
+    // queries
+    f16x8 q[RT][S::kPlanes][S::kSteps];
+    float factor[RT];
+    int limit[RT];   // keys that the row sees
+    int least = kMaxPosition;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int64_t rho = (int64_t)tile * a.rows + rt * 16 + m16;
+        const bool there = rho < (int64_t)rows.n * a.group;
+        const int t = there ? (int)(rho / a.group) : 0, h = head * a.group + (there ? (int)(rho - (int64_t)t * a.group) : 0);
+        const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + t) * a.q.token + h * a.q.head;
+        limit[rt] = there ? max(len - rows.n + t + 1, 0) : 0;
+        if (there) least = min(least, limit[rt]);
+        float x[S::kSteps][8];
+        unsigned most = 0;
+#pragma unroll
+        for (int j = 0; j < S::kSteps; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = channel<ROW>(j, g) + e;
+                x[j][e] = there && d < a.cache.size ? Entry<TYPE>::get(row[d]) : 0.f;
+                most = max(most, __float_as_uint(x[j][e]) & 0x7fffffffu);
+            }
+        most = max(most, (unsigned)__shfl_xor((int)most, 16));
+        most = max(most, (unsigned)__shfl_xor((int)most, 32));
+        const bool finite = most < 0x7f800000u;
+        const int up = most == 0 || !finite ? 0 : 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(most));
+        factor[rt] = finite ? __builtin_ldexpf(a.scale * kLog2e, -up) : kNan;
+#pragma unroll
+        for (int j = 0; j < S::kSteps; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = finite ? __builtin_ldexpf(x[j][e], up) : 0.f;
+                const _Float16 hi = (_Float16)v;
+                q[rt][0][j][e] = hi;
+                if constexpr (S::kPlanes == 2) q[rt][1][j][e] = (_Float16)(v - (float)hi);
+            }
+    }
+    for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d));
+    least = uniform(least);   // all rows see the keys below this
+
+    f32x4 o[RT][S::kTiles];
+    float most[RT], sum[RT], reference = kLeastScale;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        most[rt] = -INFINITY, sum[rt] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // pages of the blocks whose keys and whose values this lane reads, -1: none; behind the sequence's end: any
+    auto page_at = [&](int block) { return block * kKvBlock < len ? page_of(a.cache, a.seqs, seq, block) : -2; };
+    Keys<TYPE, ROW, RT> keys;
+    auto load_keys = [&](int u, int k_page, int v_page) {
+        const int block = 4 * u + m16 / 4;
+        const int8_t *at = a.cache.k + (block_at(a.cache, max(k_page, 0), head, block) * kKvBlock + m16 % 4) * ROW + g * 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int w = 0; w < S::kWide; ++w) keys.wide[t][w] = *reinterpret_cast<const u32x4 *>(at + 4 * t * ROW + 64 * w);
+            if constexpr (ROW % 64 != 0) keys.rest[t] = *reinterpret_cast<const u32x2 *>(at + 4 * t * ROW + 64 * S::kWide - g * 8);
+        }
+        const int64_t mine = block_at(a.cache, max(v_page, 0), head, 4 * u + g);
+        keys.k_scale = v_page >= 0 ? a.cache.k_scale[mine] : v_page == -1 ? kNan : 0.f;
+        keys.v_scale = v_page >= 0 ? a.cache.v_scale[mine] : v_page == -1 ? kNan : 0.f;
+    };
+
+    int u = begin + wave;
+    int k_page = 0, v_page = 0;
+    if (u < end) {
+        k_page = page_at(4 * u + m16 / 4), v_page = page_at(4 * u + g);
+        load_keys(u, k_page, v_page);
+    }
+    for (; u < end; u += kWaves) {
+        const int next = u + kWaves;
+        int k_next = 0, v_next = 0;
+        if (next < end) k_next = page_at(4 * next + m16 / 4), v_next = page_at(4 * next + g);
+        u32x4 values[S::kTiles];
+        const int8_t *v_at = a.cache.v + (block_at(a.cache, max(v_page, 0), head, 4 * u + g) * ROW + m16) * kKvBlock;
+#pragma unroll
+        for (int dt = 0; dt < S::kTiles; ++dt) values[dt] = *reinterpret_cast<const u32x4 *>(v_at + 16 * dt * kKvBlock);
+
+        f32x4 z[RT][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) z[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < S::kSteps; ++j) {
+                const f16x8 k = j < 2 * S::kWide ? widen8(keys.wide[t][j / 2][j % 2 * 2], keys.wide[t][j / 2][j % 2 * 2 + 1]) : widen8(keys.rest[t][0], keys.rest[t][1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int p = 0; p < S::kPlanes; ++p) z[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][p][j], z[rt][t], 0, 0, 0);
+            }
+        }
+        const float k_scale = keys.k_scale, v_scale = keys.v_scale;
+        if (next < end) load_keys(next, k_next, v_next);
+
+        const bool cut = (u + 1) * kUnit > least;
+        float largest = reference;
+        largest = fmaxf(largest, v_scale);
+        largest = fmaxf(largest, __shfl_xor(largest, 16));
+        largest = fmaxf(largest, __shfl_xor(largest, 32));
+        const float part = reference / largest, v_part = v_scale / largest * 32768.f;
+        reference = largest;
+        f16x8 w[RT][S::kPlanes][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float f = factor[rt] * k_scale;
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = z[rt][t][e] * f;
+                    if (cut) v = u * kUnit + g * kKvBlock + 4 * t + e < limit[rt] ? v : -INFINITY;
+                    z[rt][t][e] = v;
+                    top = fmaxf(top, v);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(most[rt], top), base = now == -INFINITY ? 0.f : now;
+            const float keep = __builtin_amdgcn_exp2f(most[rt] - base) ;
+            most[rt] = now;
+            float s = 0.f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(z[rt][t][e] - base);
+                    s += p;
+                    float x = p * v_part;
+                    if (cut) x = z[rt][t][e] == -INFINITY ? 0.f : x;
+                    const _Float16 hi = (_Float16)x;
+                    w[rt][0][t / 2][t % 2 * 4 + e] = hi;
+                    if constexpr (S::kPlanes == 2) w[rt][1][t / 2][t % 2 * 4 + e] = (_Float16)(x - (float)hi);
+                }
+            sum[rt] = sum[rt] * keep + s;
+            const float times = keep * part;
+            if (__any(times != 1.f)) {
+#pragma unroll
+                for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < S::kTiles; ++dt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const f16x8 v = widen8(values[dt][2 * j], values[dt][2 * j + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int p = 0; p < S::kPlanes; ++p) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][p][j], o[rt][dt], 0, 0, 0);
+            }
+        k_page = k_next, v_page = v_next;
+    }
+
+    // the wavefronts' sums: relative to the largest logit of all, then two and two
+    float all[RT], total[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        sum[rt] += __shfl_xor(sum[rt], 16);
+        sum[rt] += __shfl_xor(sum[rt], 32);
+        if (g == 0) states[wave][rt][m16] = float2{most[rt], sum[rt]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        all[rt] = -INFINITY, total[rt] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all[rt] = fmaxf(all[rt], states[w][rt][m16].x);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total[rt] += states[w][rt][m16].y * weight_of(states[w][rt][m16].x, all[rt]);
+        const float times = weight_of(most[rt], all[rt]) * reference * (1.f / 32768.f);
+#pragma unroll
+        for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = times == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][dt] * times;
+    }
+#pragma unroll
+    for (int half = kWaves / 2; half; half >>= 1) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int dt = 0; dt < S::kTiles; ++dt) shared[wave - half][rt * S::kTiles + dt][lane] = o[rt][dt];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] += shared[wave][rt * S::kTiles + dt][lane];
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    if (it.chunks == 1) {
+        write_rows<TYPE, ROW, RT>(a, rows, tile, head, o, total, limit);
+        return;
+    }
+    const int64_t place = (int64_t)head * a.items + blockIdx.x;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int dt = 0; dt < S::kTiles; ++dt) a.sums[(place * (RT * S::kTiles) + rt * S::kTiles + dt) * 64 + lane] = o[rt][dt];
+        if (g == 0) a.states[place * (RT * 16) + rt * 16 + m16] = float2{all[rt], total[rt]};
+    }
+}
+
+// Joins the chunks of a tile: a wavefront for 16 channels of 16 rows.  Its workgroup has the number of the tile's first chunk.
+template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64) k_kv_join(KvArgs a)
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    constexpr int kTiles = ROW / 16;
+    const int lane = threadIdx.x, g = lane / 16, m16 = lane % 16, head = blockIdx.y, rt = blockIdx.z / kTiles, dt = blockIdx.z % kTiles;
+    const int length = uniform(chunk_length(a));
+    const Item it = find_item(a, length, blockIdx.x);
+    if (it.seq < 0 || it.chunk != 0 || it.chunks == 1) return;
+    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, it.seq);
+    const int64_t place = (int64_t)head * a.items + blockIdx.x;
+    const float2 *states = a.states + place * (RT * 16) + rt * 16 + m16;
+    const f32x4 *sums = a.sums + (place * (RT * kTiles) + rt * kTiles + dt) * 64 + lane;
+    const int n = uniform(min(it.chunks, a.items - (int)blockIdx.x));   // (fewer where offsets do not ascend)
+    float all = -INFINITY;
+    for (int c = 0; c < n; ++c) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
+    float total = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int c = 0; c < n; ++c) {
+        const float2 s = states[(int64_t)c * (RT * 16)];
+        const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
+        const float w = weight_of(s.x, all);
+        total += w * s.y;
+        if (w != 0.f) o += w * v;
+    }
+    const int64_t rho = (int64_t)it.tile * a.rows + rt * 16 + m16;
+    if (rho >= (int64_t)rows.n * a.group) return;
+    const int t = (int)(rho / a.group), h = head * a.group + (int)(rho - (int64_t)t * a.group), size = a.cache.size;
+    Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
+    const float inverse = 1.f / total;   // (a sequence of several chunks: rows of positions below 0 are those that see nothing)
+    const bool sees = min(max(a.seqs.lens[it.seq], 0), kMaxPosition) - rows.n + t >= 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(sees ? o[e] * inverse : 0.f);
+}
+
+// How a call is cut.
+struct Cut {
+    int row_tiles, wanted;
+    int64_t items;   // workgroups of a head, at most
+    size_t states, total;
+};
+Cut cut_of(const tst_kv_cache_t *c, const tst_sequences_t *s, int q_heads)
+{
+    Cut k{};
+    const int group = q_heads / c->heads, row = kv_row(c->head_size);
+    const int64_t rows = (int64_t)s->tokens * group;   // of a key head
+    k.row_tiles = s->sequences && rows > (int64_t)s->sequences * 16 && row <= 128 ? 2 : 1;
+    const int64_t tiles = rows / (16 * k.row_tiles) + s->sequences;
+    const int64_t most = ((int64_t)s->columns * c->page_tokens + kUnit) / kUnit;   // units of the longest sequence there can be
+    const int wanted = blocks_of(2 * compute_units(), c->heads);
+    k.wanted = s->sequences <= 1024 && tiles <= 16 * (int64_t)wanted && most > kLeastChunk ? wanted : 0;
+    k.items = tiles + k.wanted;
+    const size_t states = (size_t)k.items * c->heads * k.row_tiles * 16;
+    k.states = k.wanted ? round256(states * row * sizeof(float)) : 0;
+    k.total = k.wanted ? k.states + round256(states * sizeof(float2)) : 0;
+    return k;
+}
+
+}  // namespace
+}  // namespace tst
+
+extern "C" {
+
+int tst_kv_attention_workspace_bytes(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, int q_heads, size_t *bytes)
+{
+    if (int rc = tst::check_cache(cache)) return rc;
+    if (int rc = tst::check_sequences(cache, sequences)) return rc;
+    if (!bytes || q_heads < 1 || q_heads > TST_MAX_HEADS || q_heads % cache->heads || (int64_t)sequences->tokens * q_heads > TST_MAX_ROWS) return TSTGEMM_EINVAL;
+    *bytes = sequences->tokens ? tst::cut_of(cache, sequences, q_heads).total : 0;
+    return TSTGEMM_OK;
+}
+
+int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_cache_t *cache, const tst_sequences_t *sequences, float scale, void *Y,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    if (int rc = tst_kv_attention_workspace_bytes(cache, sequences, q_heads, &need)) return rc;
+    if (!tst::type_ok(type) || !(scale - scale == 0.f)) return TSTGEMM_EINVAL;
+    if (sequences->sequences == 0 || sequences->tokens == 0) return TSTGEMM_OK;
+    if (!tst::rows_ok(Q, type) || !Y || !tst::aligned(Y, tst::type_bytes(type))) return TSTGEMM_EINVAL;
+    if (need && (!workspace || workspace_bytes < need)) return TSTGEMM_EWORKSPACE;
+    if (need && !tst::aligned(workspace, 256)) return TSTGEMM_EINVAL;
+    const tst::Cut cut = tst::cut_of(cache, sequences, q_heads);
+    tst::KvArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(Q), q_heads, q_heads / cache->heads, 16 * cut.row_tiles, cut.wanted, scale, Y,
+                  static_cast<tst::f32x4 *>(workspace), reinterpret_cast<float2 *>(static_cast<char *>(workspace) + cut.states), (int)cut.items};
+    return tst::status(tst::for_type(type, [&](auto t) {
+        return tst::for_row(cache->head_size, [&](auto r) {
+            constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value, MOST = ROW <= 128 ? 2 : 1;
+            hipStream_t st = static_cast<hipStream_t>(stream);
+            const dim3 grid((unsigned)cut.items, cache->heads);
+            if (cut.row_tiles == 1) tst::k_kv_attention<TYPE, ROW, 1><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+            else tst::k_kv_attention<TYPE, ROW, MOST><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+            if (cut.wanted) {
+                if (hipError_t e = hipGetLastError()) return e;
+                const dim3 joins((unsigned)cut.items, cache->heads, ROW / 16 * cut.row_tiles);
+                if (cut.row_tiles == 1) tst::k_kv_join<TYPE, ROW, 1><<<joins, 64, 0, st>>>(a);
+                else tst::k_kv_join<TYPE, ROW, MOST><<<joins, 64, 0, st>>>(a);
+            }
+            return hipGetLastError();
+        });
+    }));
+}
+
+}  // extern "C"

@@ -1,0 +1,416 @@
+// A paged cache of keys and values in 8 bits: appending to it with the rotation by positions (tst_kv_append) and reading it back (tst_kv_read).
+//
+// A block of 16 tokens of a head is a wavefront's, keys and values apart: it finds the largest entry of the block's new tokens, and with it the
+// block's scale, before anything is rounded, and nobody else writes there.  Lane (u, j) has channels 8 u .. 8 u + 7 of tokens 4 j .. 4 j + 3, so the four
+// codes of a channel make a dword of the values' layout [channel][token].
+#include "attention_internal.h"
+
+namespace tst {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr float kNan = __builtin_nanf("");
+
+struct AppendArgs {
+    Cache cache;
+    Sequences seqs;
+    Rows k, v, q;
+    int q_heads, kv_groups;   // workgroups of a block's heads that have keys and values; those behind have queries
+    const float *cos, *sin;
+    int positions, pairs;
+    bool interleaved;
+    void *q_out, *k_out;
+};
+
+// Channels d .. d + 7 of a row of `size` entries, 0 behind its end.
+template <int TYPE, bool WIDE> __device__ __forceinline__ void load8(const typename Entry<TYPE>::bits *row, int d, int size, float (&x)[8])
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    if constexpr (WIDE) {
+        union {
+            u32x4 v[sizeof(Bits) / 2];
+            Bits e[8];
+        } u;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Bits) / 2; ++i) u.v[i] = reinterpret_cast<const u32x4 *>(row + d)[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = Entry<TYPE>::get(u.e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = d + i < size ? Entry<TYPE>::get(row[d + i]) : 0.f;
+    }
+}
+template <int TYPE, bool WIDE> __device__ __forceinline__ void store8(typename Entry<TYPE>::bits *row, int d, int size, const float (&x)[8])
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    if constexpr (WIDE) {
+        union {
+            u32x4 v[sizeof(Bits) / 2];
+            Bits e[8];
+        } u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u.e[i] = Entry<TYPE>::put(x[i]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Bits) / 2; ++i) reinterpret_cast<u32x4 *>(row + d)[i] = u.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < size) row[d + i] = Entry<TYPE>::put(x[i]);
+    }
+}
+
+// Channels d .. d + 7 of a row, rotated by position p: each product and each sum is rounded to fp32 (no fma), so that codes are defined bit for bit.
+template <int TYPE, bool WIDE> __device__ __forceinline__ void rotated8(const AppendArgs &a, const typename Entry<TYPE>::bits *row, int d, int p, float (&x)[8])
+{
+#pragma clang fp contract(off)
+    load8<TYPE, WIDE>(row, d, a.cache.size, x);
+    const int P = a.pairs;
+    if (d >= 2 * P) return;
+    const bool there = p >= 0 && p < a.positions;
+    const float *cs = a.cos + (int64_t)(there ? p : 0) * P, *sn = a.sin + (int64_t)(there ? p : 0) * P;
+    if constexpr (WIDE) {   // pairs are a multiple of 8 (of 4 if they are neighbours)
+        if (a.interleaved) {
+            f32x4 c = *reinterpret_cast<const f32x4 *>(cs + d / 2), s = *reinterpret_cast<const f32x4 *>(sn + d / 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x0 = x[2 * i], x1 = x[2 * i + 1];
+                const float ci = there ? c[i] : kNan, si = there ? s[i] : kNan;
+                const float a0 = x0 * ci, b0 = x1 * si, a1 = x1 * ci, b1 = x0 * si;
+                x[2 * i] = a0 - b0;
+                x[2 * i + 1] = a1 + b1;
+            }
+        } else {
+            const int at = d < P ? d : d - P;
+            float other[8];
+            load8<TYPE, true>(row, d < P ? d + P : d - P, a.cache.size, other);
+            f32x4 c[2], s[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) c[i] = reinterpret_cast<const f32x4 *>(cs + at)[i], s[i] = reinterpret_cast<const f32x4 *>(sn + at)[i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float ci = there ? c[i / 4][i % 4] : kNan, si = there ? s[i / 4][i % 4] : kNan;
+                const float m = x[i] * ci, n = other[i] * si;
+                x[i] = d < P ? m - n : m + n;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = d + i;
+            if (e >= 2 * P) break;
+            const bool low = a.interleaved ? e % 2 == 0 : e < P;
+            const int at = a.interleaved ? e / 2 : (low ? e : e - P), mate = a.interleaved ? e ^ 1 : (low ? e + P : e - P);
+            const float c = there ? cs[at] : kNan, s = there ? sn[at] : kNan;
+            const float m = x[i] * c, n = Entry<TYPE>::get(row[mate]) * s;
+            x[i] = low ? m - n : m + n;
+        }
+    }
+}
+
+__device__ __forceinline__ int code_of(float y, float inverse)
+{
+    const float q = __builtin_rintf(y * inverse);
+    return (int)fminf(fmaxf(q, -127.f), 127.f);
+}
+__device__ __forceinline__ unsigned rescaled(unsigned four, float share)
+{
+    unsigned out = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out |= ((unsigned)(int)__builtin_rintf((float)(int8_t)(four >> 8 * i) * share) & 255u) << 8 * i;
+    return out;
+}
+
+// Tokens from .. to of a block, keys or values of a head.
+template <int TYPE, bool WIDE> __device__ __forceinline__ void append_block(const AppendArgs &a, bool values, int head, int seq, int block, int from, int to, int row0, unsigned *lds)
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    const int lane = threadIdx.x % 64, j = lane % 4, size = a.cache.size, units = (size + 7) / 8, row = kv_row(size);
+    const Rows &in = values ? a.v : a.k;
+    const Bits *data = static_cast<const Bits *>(in.data) + head * in.head;
+    float x[2][4][8];
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int u = lane / 4 + 16 * i;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][t][e] = 0.f;
+            const int token = 4 * j + t;
+            if (u >= units || token < from || token > to) continue;
+            const Bits *r = data + (int64_t)(row0 + token - from) * in.token;
+            if (values) load8<TYPE, WIDE>(r, 8 * u, size, x[i][t]);
+            else {
+                rotated8<TYPE, WIDE>(a, r, 8 * u, block * kKvBlock + token, x[i][t]);
+                if (a.k_out) store8<TYPE, WIDE>(static_cast<Bits *>(a.k_out) + ((int64_t)(row0 + token - from) * a.cache.heads + head) * size, 8 * u, size, x[i][t]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[i][t][e]) & 0x7fffffffu);
+        }
+    }
+    const int page = page_of(a.cache, a.seqs, seq, block);
+    if (page < 0) return;
+    const int64_t at = block_at(a.cache, page, head, block);
+    float *scales = (values ? a.cache.v_scale : a.cache.k_scale) + at;
+    int8_t *codes = (values ? a.cache.v : a.cache.k) + at * kKvBlock * row;
+
+    const float largest = __uint_as_float(wave_max(most));
+    const float before = from > 0 ? *scales : 0.f, fresh = largest / 127.f;
+    const bool finite = largest <= 3.402823466e38f && before == before;
+    const float scale = !finite ? kNan : fmaxf(before, fresh);
+    const float inverse = finite ? fminf(1.f / scale, 3.402823466e38f) : 0.f;   // scale 0: 0 * FLT_MAX = 0
+    const bool grown = finite && scale > before && from > 0;
+    const float share = grown ? before / scale : 1.f;
+    unsigned q[2][4][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                q[i][t][w] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[i][t][w] |= (finite ? (unsigned)code_of(x[i][t][4 * w + e], inverse) & 255u : 0u) << 8 * e;
+            }
+    if (lane == 0) *scales = scale;
+    if (!values) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int u = lane / 4 + 16 * i;
+            if (u >= units) continue;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int token = 4 * j + t;
+                u32x2 *to8 = reinterpret_cast<u32x2 *>(codes + token * row + 8 * u);
+                if (token >= from && token <= to) *to8 = u32x2{q[i][t][0], q[i][t][1]};
+                else if (token < from && grown) *to8 = u32x2{rescaled((*to8)[0], share), rescaled((*to8)[1], share)};
+            }
+        }
+        return;
+    }
+    // values: dwords of four tokens, rows of a channel through the LDS, joined with the tokens that were there
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int u = lane / 4 + 16 * i;
+        if (u >= units) continue;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                unsigned four = 0;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) four |= (q[i][t][w] >> 8 * e & 255u) << 8 * t;
+                lds[(8 * u + 4 * w + e) * 4 + j] = four;
+            }
+    }
+    order_wave();
+    const bool whole = from == 0;   // nothing was there: zeros behind the last token
+    for (int d = lane; d < size; d += 64) {
+        u32x4 four = reinterpret_cast<const u32x4 *>(lds)[d];
+        u32x4 *to16 = reinterpret_cast<u32x4 *>(codes + d * kKvBlock);
+        if (!whole) {
+            const u32x4 old = *to16;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const unsigned kept = grown ? rescaled(old[w], share) : old[w];
+                unsigned mask = 0;   // bytes of tokens before `from`
+#pragma unroll
+                for (int t = 0; t < 4; ++t) mask |= 4 * w + t < from ? 255u << 8 * t : 0u;
+                four[w] = (kept & mask) | (four[w] & ~mask);
+            }
+        }
+        *to16 = four;
+    }
+}
+
+template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_kv_append(AppendArgs a)
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    __shared__ __attribute__((aligned(16))) unsigned lds[kWaves][TST_MAX_HEAD_SIZE * kKvBlock / 4];
+    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int at = blockIdx.x;
+    const int seq = a.seqs.offsets ? uniform(find_sequence(a.seqs.offsets, a.seqs.tokens, a.seqs.count, kKvBlock, 2, at)) : at;
+    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
+    const int piece = a.seqs.offsets ? at - (rows.first / kKvBlock + 2 * seq) : 0;
+    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition), first = len - rows.n;   // position of the first row; negative where there are more rows
+    const int block = (first >> 4) + piece;
+    if (rows.n == 0 || piece < 0 || block > (len - 1) >> 4) return;
+    const int from = max(first - block * kKvBlock, 0), to = min(len - 1 - block * kKvBlock, kKvBlock - 1);
+    const int row0 = rows.first + block * kKvBlock + from - first;
+    if ((int)blockIdx.y < a.kv_groups) {
+        const int item = blockIdx.y * kWaves + wave;
+        if (item < 2 * a.cache.heads) append_block<TYPE, WIDE>(a, item & 1, item >> 1, seq, block, from, to, row0, lds[wave]);
+        return;
+    }
+    // queries: rows of four heads for each wavefront, a unit of 8 channels for each lane
+    const int h0 = ((blockIdx.y - a.kv_groups) * kWaves + wave) * 4, heads = min(a.q_heads - h0, 4), size = a.cache.size, units = (size + 7) / 8;
+    const int across = units <= 8 ? 8 : units <= 16 ? 16 : 32, u = lane & (across - 1);
+    if (heads <= 0 || u >= units) return;
+    const int count = heads * (to - from + 1);
+    for (int i = lane / across; i < count; i += 64 / across) {
+        const int t = i / heads, h = h0 + i - t * heads, r = row0 + t;
+        float x[8];
+        rotated8<TYPE, WIDE>(a, static_cast<const Bits *>(a.q.data) + (int64_t)r * a.q.token + h * a.q.head, 8 * u, block * kKvBlock + from + t, x);
+        store8<TYPE, WIDE>(static_cast<Bits *>(a.q_out) + ((int64_t)r * a.q_heads + h) * size, 8 * u, size, x);
+    }
+}
+
+// What a code stands for, rounded to fp32 (the compiler would otherwise round the product to fp16 at once).
+__device__ __forceinline__ float value_of(unsigned four, int i, float scale)
+{
+    float v = (float)(int8_t)(four >> 8 * i) * scale;
+    asm("" : "+v"(v));
+    return v;
+}
+
+struct ReadArgs {
+    Cache cache;
+    Sequences seqs;
+    void *k_out, *v_out;
+};
+
+template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_kv_read(ReadArgs a)
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int at = blockIdx.x;
+    const int seq = a.seqs.offsets ? uniform(find_sequence(a.seqs.offsets, a.seqs.tokens, a.seqs.count, kKvBlock, 2, at)) : at;
+    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
+    const int piece = a.seqs.offsets ? at - (rows.first / kKvBlock + 2 * seq) : 0;
+    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition), first = len - rows.n;
+    const int block = (first >> 4) + piece;
+    const int item = blockIdx.y * kWaves + wave;
+    if (rows.n == 0 || piece < 0 || block > (len - 1) >> 4 || item >= 2 * a.cache.heads) return;
+    const int from = max(first - block * kKvBlock, 0), to = min(len - 1 - block * kKvBlock, kKvBlock - 1);
+    const int row0 = rows.first + block * kKvBlock + from - first;
+    const bool values = item & 1;
+    const int head = item >> 1, size = a.cache.size, units = (size + 7) / 8, row = kv_row(size);
+    const int page = page_of(a.cache, a.seqs, seq, block);
+    const int64_t place = page < 0 ? 0 : block_at(a.cache, page, head, block);
+    const float scale = page < 0 ? kNan : (values ? a.cache.v_scale : a.cache.k_scale)[place];
+    const int8_t *codes = (values ? a.cache.v : a.cache.k) + place * kKvBlock * row;
+    Bits *out = static_cast<Bits *>(values ? a.v_out : a.k_out) + ((int64_t)row0 * a.cache.heads + head) * size;
+    const int64_t next = (int64_t)a.cache.heads * size;   // entries from token to token
+    if (!values) {
+        const int across = units <= 8 ? 8 : units <= 16 ? 16 : 32, u = lane & (across - 1);
+        if (u >= units) return;
+        for (int t = from + lane / across; t <= to; t += 64 / across) {
+            const u32x2 eight = *reinterpret_cast<const u32x2 *>(codes + t * row + 8 * u);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = value_of(eight[e / 4], e % 4, scale);
+            store8<TYPE, WIDE>(out + (t - from) * next, 8 * u, size, x);
+        }
+        return;
+    }
+    for (int d = lane; d < size; d += 64) {
+        const u32x4 sixteen = *reinterpret_cast<const u32x4 *>(codes + d * kKvBlock);
+#pragma unroll
+        for (int t = 0; t < kKvBlock; ++t)
+            if (t >= from && t <= to) out[(t - from) * next + d] = Entry<TYPE>::put(value_of(sixteen[t / 4], t % 4, scale));
+    }
+}
+
+bool wide(const Rows &x, int type)
+{
+    const int64_t per = 16 / (int64_t)type_bytes(type);
+    return aligned(x.data, 16) && x.token % per == 0 && x.head % per == 0;
+}
+
+}  // namespace
+
+int check_cache(const tst_kv_cache_t *c)
+{
+    size_t codes = 0, scales = 0;
+    if (!c || c->struct_size != sizeof(tst_kv_cache_t) || tst_kv_cache_bytes(c->pages, c->page_tokens, c->heads, c->head_size, &codes, &scales) != TSTGEMM_OK)
+        return TSTGEMM_EINVAL;
+    return c->k_codes && c->v_codes && c->k_scale && c->v_scale && aligned(c->k_codes, 16) && aligned(c->v_codes, 16) && aligned(c->k_scale, 4) && aligned(c->v_scale, 4)
+               ? TSTGEMM_OK : TSTGEMM_EINVAL;
+}
+
+int check_sequences(const tst_kv_cache_t *c, const tst_sequences_t *s)
+{
+    if (!s || s->struct_size != sizeof(tst_sequences_t) || s->sequences < 0 || s->sequences > TST_MAX_SEQUENCES || s->tokens < 0 || s->tokens > TST_MAX_TOKENS)
+        return TSTGEMM_EINVAL;
+    if (!s->offsets && s->tokens != s->sequences) return TSTGEMM_EINVAL;
+    if (s->columns < 1 || s->table_stride < s->columns || s->table_stride > INT64_MAX / 4 / (TST_MAX_SEQUENCES + 1) || (int64_t)s->columns * c->page_tokens > kMaxPosition)
+        return TSTGEMM_EINVAL;
+    if (s->sequences == 0 || s->tokens == 0) return TSTGEMM_OK;
+    return s->lens && s->table && aligned(s->offsets, 4) && aligned(s->lens, 4) && aligned(s->table, 4) ? TSTGEMM_OK : TSTGEMM_EINVAL;
+}
+
+// Strides up to 2^38 keep every offset of a row and head below 2^63.
+bool rows_ok(const tst_heads_t *x, int type)
+{
+    constexpr int64_t most = (int64_t)1 << 38;
+    return x && x->data && aligned(x->data, type_bytes(type)) && x->token_stride >= 0 && x->head_stride >= 0 && x->token_stride <= most && x->head_stride <= most;
+}
+
+}  // namespace tst
+
+extern "C" {
+
+int tst_kv_row(int head_size) { return head_size < 1 || head_size > TST_MAX_HEAD_SIZE ? 0 : tst::kv_row(head_size); }
+
+int tst_kv_cache_bytes(int pages, int page_tokens, int heads, int head_size, size_t *codes, size_t *scales)
+{
+    const int row = tst_kv_row(head_size);
+    if (!codes || !scales || pages < 1 || page_tokens < 16 || page_tokens > 256 || (page_tokens & (page_tokens - 1)) || heads < 1 || heads > TST_MAX_HEADS || !row)
+        return TSTGEMM_EINVAL;
+    *scales = (size_t)pages * heads * (page_tokens / tst::kKvBlock);
+    *codes = *scales * tst::kKvBlock * row;
+    return TSTGEMM_OK;
+}
+
+int tst_kv_append(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, int type, const tst_heads_t *K, const tst_heads_t *V,
+                  const tst_heads_t *Q, int q_heads, const tst_rotation_t *rotation, void *q_out, void *k_out, void *stream)
+{
+    if (int rc = tst::check_cache(cache)) return rc;
+    if (int rc = tst::check_sequences(cache, sequences)) return rc;
+    if (!tst::type_ok(type) || (Q && (q_heads < 1 || q_heads > TST_MAX_HEADS)) || (!Q && q_out)) return TSTGEMM_EINVAL;
+    const tst_rotation_t *r = rotation;
+    if (r && (r->struct_size != sizeof(tst_rotation_t) || !r->cos || !r->sin || !tst::aligned(r->cos, 4) || !tst::aligned(r->sin, 4) || r->positions < 1 || r->pairs < 1 ||
+              r->pairs > cache->head_size / 2))
+        return TSTGEMM_EINVAL;
+    if (sequences->sequences == 0 || sequences->tokens == 0) return TSTGEMM_OK;
+    const size_t entry = tst::type_bytes(type);
+    if (!tst::rows_ok(K, type) || !tst::rows_ok(V, type) || (Q && (!q_out || !tst::rows_ok(Q, type))) || !tst::aligned(q_out, entry) || !tst::aligned(k_out, entry)) return TSTGEMM_EINVAL;
+    tst::AppendArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(K), tst::rows_of(V), tst::rows_of(Q), Q ? q_heads : 0,
+                      tst::blocks_of(2 * cache->heads, tst::kWaves), r ? r->cos : nullptr, r ? r->sin : nullptr, r ? r->positions : 0, r ? r->pairs : 0,
+                      r && r->interleaved, q_out, k_out};
+    // vectors of 16 bytes: rows, their pairs and the angles lie on borders
+    const bool wide = tst::wide(a.k, type) && tst::wide(a.v, type) && (!Q || (tst::wide(a.q, type) && tst::aligned(q_out, 16))) && tst::aligned(k_out, 16) && cache->head_size % 8 == 0 &&
+                      a.pairs % (a.interleaved ? 4 : 8) == 0 && tst::aligned(a.cos, 16) && tst::aligned(a.sin, 16);
+    const dim3 grid(sequences->offsets ? tst::pieces(sequences->tokens, sequences->sequences, tst::kKvBlock, 2) : sequences->sequences,
+                    a.kv_groups + tst::blocks_of(a.q_heads, 4 * tst::kWaves));
+    return tst::status(tst::for_type(type, [&](auto t) {
+        constexpr int TYPE = decltype(t)::value;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        if (wide) tst::k_kv_append<TYPE, true><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        else tst::k_kv_append<TYPE, false><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        return hipGetLastError();
+    }));
+}
+
+int tst_kv_read(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, int type, void *k_out, void *v_out, void *stream)
+{
+    if (int rc = tst::check_cache(cache)) return rc;
+    if (int rc = tst::check_sequences(cache, sequences)) return rc;
+    if (!tst::type_ok(type)) return TSTGEMM_EINVAL;
+    if (sequences->sequences == 0 || sequences->tokens == 0) return TSTGEMM_OK;
+    const size_t entry = tst::type_bytes(type);
+    if (!k_out || !v_out || !tst::aligned(k_out, entry) || !tst::aligned(v_out, entry)) return TSTGEMM_EINVAL;
+    const tst::ReadArgs a{tst::cache_of(cache), tst::sequences_of(sequences), k_out, v_out};
+    const bool wide = tst::aligned(k_out, 16) && cache->head_size % 8 == 0;
+    const dim3 grid(sequences->offsets ? tst::pieces(sequences->tokens, sequences->sequences, tst::kKvBlock, 2) : sequences->sequences,
+                    tst::blocks_of(2 * cache->heads, tst::kWaves));
+    return tst::status(tst::for_type(type, [&](auto t) {
+        constexpr int TYPE = decltype(t)::value;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        if (wide) tst::k_kv_read<TYPE, true><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        else tst::k_kv_read<TYPE, false><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        return hipGetLastError();
+    }));
+}
+
+}  // extern "C"
