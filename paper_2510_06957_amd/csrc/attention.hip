@@ -9,11 +9,20 @@
 // fp32 operands are cut into three bf16 planes by cutting mantissas off (exact) and six products of planes are summed: all but 2^-24 of a product.
 #include "attention_internal.h"
 
+#include <cmath>
+
+#ifndef V_QB
+#define V_QB 1
+#define V_NW 8
+#define V_OCC 2
+#endif
 namespace tst {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kNan = __builtin_nanf("");
@@ -23,7 +32,8 @@ struct PromptArgs {
     Rows q, k, v;
     int q_heads, heads, group, size, sequences, tokens, tiles;
     const int32_t *offsets;
-    float scale;   // times log2 e
+    float scale;   // its magnitude times log2 e; 2^-126 for 0 and less, so that -inf stays what it is
+    bool negative;
     void *y;
     bool wide;     // rows of Q, K and V on 16-byte borders, of a multiple of 8 entries
 };
@@ -83,17 +93,43 @@ template <int TYPE> __device__ __forceinline__ Planes<TYPE> planes_of(const Raw<
     return out;
 }
 
+// Two weights as the second product takes them, and their sum.
+template <int TYPE> struct Pair;
+template <> struct Pair<TST_BF16> {
+    typedef __bf16 entry;
+    bf16x2 v;
+    __device__ __forceinline__ Pair(entry a, entry b) : v{a, b} {}
+    __device__ __forceinline__ float added(float sum) const { return __builtin_amdgcn_fdot2_f32_bf16(v, bf16x2{(entry)1.f, (entry)1.f}, sum, false); }
+    __device__ __forceinline__ unsigned bits() const { return __builtin_bit_cast(unsigned, v); }
+};
+template <> struct Pair<TST_F16> {
+    typedef _Float16 entry;
+    f16x2 v;
+    __device__ __forceinline__ Pair(entry a, entry b) : v{a, b} {}
+    __device__ __forceinline__ float added(float sum) const { return __builtin_amdgcn_fdot2(v, f16x2{(entry)1.f, (entry)1.f}, sum, false); }
+    __device__ __forceinline__ unsigned bits() const { return __builtin_bit_cast(unsigned, v); }
+};
+
 template <int TYPE> __device__ __forceinline__ f32x16 product(u32x4 a, u32x4 b, f32x16 c)
 {
     if constexpr (TYPE == TST_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// The largest of a lane's logits, NaN if one is (what does not care for NaN costs an instruction more for each).
+__device__ __forceinline__ float largest_of(const f32x16 &z)
+{
+    float m = z[0];
+#pragma unroll
+    for (int r = 1; r < 15; r += 2) m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, z[r]), z[r + 1]);
+    return __builtin_elementwise_maximum(m, z[15]);
+}
+
 // The larger of a value and that of the lane 32 away.
 __device__ __forceinline__ float across_max(float v)
 {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float across_sum(float v)
 {
@@ -106,7 +142,8 @@ template <int TYPE, int ROW, int QB, int NW> struct Shape {
     static constexpr int kRows = NW * QB * 32;             // of a tile
     static constexpr int kKeys = TYPE == TST_F32 ? 32 : 64;
     static constexpr int kBuffers = TYPE == TST_F32 ? 1 : 2;
-    static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + 32;   // bytes; neighbours' reads fall into other banks
+    // bytes from key to key: 16 rows of keys, and 4 rows of 32 channels of values, fall into different banks
+    static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + (ROW % 128 == 96 ? 0 : 64);
     static constexpr int kPlaneK = kKeys * kStrideK, kPlaneV = kKeys * kStrideV;
     static constexpr int kBuffer = kPlanes * (kPlaneK + kPlaneV);
     static constexpr int kChunks = (kKeys * (ROW / 8) + 64 * NW - 1) / (64 * NW);   // of 8 entries that a thread stages, of K and as many of V
@@ -117,7 +154,7 @@ template <int TYPE, int ROW, int QB, int NW> struct Shape {
 constexpr float kSlack = 8.f;
 template <int TYPE> constexpr float kShift = TYPE == TST_F16 ? 7.f : 0.f;
 
-template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(64 * NW) k_attention(PromptArgs a)
+template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(64 * NW, V_OCC) k_attention(PromptArgs a)
 {
     typedef Shape<TYPE, ROW, QB, NW> S;
     typedef typename Entry<TYPE>::bits Bits;
@@ -168,7 +205,15 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
         const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + max(token[b], 0)) * a.q.token + q_head[b] * a.q.head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            const Planes<TYPE> x = planes_of<TYPE>(load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, a.wide));
+            Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, a.wide);
+            if (a.negative) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (TYPE == TST_F32) raw.e[e] = -raw.e[e];
+                    else raw.e[e] ^= 0x8000;
+                }
+            }
+            const Planes<TYPE> x = planes_of<TYPE>(raw);
 #pragma unroll
             for (int p = 0; p < P; ++p) q[b][p][s] = x.p[p];
         }
@@ -263,17 +308,16 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
             u32x4 w[QB][P][kSub][2];
 #pragma unroll
             for (int b = 0; b < QB; ++b) {
-                float top = -INFINITY;
+                if (cut) {
 #pragma unroll
-                for (int s = 0; s < kSub; ++s)
+                    for (int s = 0; s < kSub; ++s)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float v = z[b][s][r] * a.scale;
-                        if (cut) v = kt * S::kKeys + s * 32 + 8 * (r / 4) + 4 * half + r % 4 < limit[b] ? v : -INFINITY;
-                        z[b][s][r] = v;
-                        top = fmaxf(top, v);
-                    }
-                top = across_max(top);
+                        for (int r = 0; r < 16; ++r)
+                            if (kt * S::kKeys + s * 32 + 8 * (r / 4) + 4 * half + r % 4 >= limit[b]) z[b][s][r] = -INFINITY;
+                }
+                float top = largest_of(z[b][0]);
+                if constexpr (kSub == 2) top = __builtin_elementwise_maximum(top, largest_of(z[b][kSub - 1]));
+                top = across_max(top) * a.scale;
                 if (__any(top > base[b] + kSlack)) {
                     const float now = fmaxf(base[b], top), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base[b] - now);
                     base[b] = now;
@@ -287,8 +331,8 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
                 for (int s = 0; s < kSub; ++s) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        z[b][s][r] = __builtin_amdgcn_exp2f(z[b][s][r] - from);
-                        s_all += z[b][s][r];
+                        z[b][s][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][s][r], a.scale, -from));
+                        if constexpr (TYPE == TST_F32) s_all += z[b][s][r];
                     }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
@@ -299,16 +343,13 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
                             const Planes<TYPE> px = planes_of<TYPE>(x);
 #pragma unroll
                             for (int p = 0; p < P; ++p) w[b][p][s][j] = px.p[p];
-                        } else if constexpr (TYPE == TST_BF16) {
-                            bf16x8 x;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = (__bf16)z[b][s][8 * j + i];
-                            w[b][0][s][j] = __builtin_bit_cast(u32x4, x);
                         } else {
-                            f16x8 x;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = (_Float16)z[b][s][8 * j + i];
-                            w[b][0][s][j] = __builtin_bit_cast(u32x4, x);
+                            for (int i = 0; i < 4; ++i) {
+                                const Pair<TYPE> pair = {(typename Pair<TYPE>::entry)z[b][s][8 * j + 2 * i], (typename Pair<TYPE>::entry)z[b][s][8 * j + 2 * i + 1]};
+                                s_all = pair.added(s_all);
+                                w[b][0][s][j][i] = pair.bits();
+                            }
                         }
                     }
                 }
@@ -393,11 +434,11 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
     if (!tst::rows_ok(Q, type) || !tst::rows_ok(K, type) || !tst::rows_ok(V, type) || !offsets || !tst::aligned(offsets, 4) || !Y || !tst::aligned(Y, tst::type_bytes(type)))
         return TSTGEMM_EINVAL;
     const int group = q_heads / heads;
-    tst::PromptArgs a{tst::rows_of(Q), tst::rows_of(K), tst::rows_of(V), q_heads, heads, group, head_size, sequences, tokens, 0, offsets, scale * tst::kLog2e, Y, false};
+    tst::PromptArgs a{tst::rows_of(Q), tst::rows_of(K), tst::rows_of(V), q_heads, heads, group, head_size, sequences, tokens, 0, offsets, std::fmax(std::fabs(scale) * tst::kLog2e, 1.17549435e-38f), scale < 0, Y, false};
     a.wide = tst::wide(a.q, type, head_size) && tst::wide(a.k, type, head_size) && tst::wide(a.v, type, head_size);
     return tst::status(tst::for_type(type, [&](auto t) {
         return tst::for_row(head_size, [&](auto r) {
-            constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value, QB = 1, NW = 4;
+            constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value, QB = V_QB, NW = V_NW;
             a.tiles = (int)((int64_t)tokens * group / tst::Shape<TYPE, ROW, QB, NW>::kRows) + sequences;
             tst::k_attention<TYPE, ROW, QB, NW><<<(unsigned)a.tiles * heads, 64 * NW, 0, static_cast<hipStream_t>(stream)>>>(a);
             return hipGetLastError();
