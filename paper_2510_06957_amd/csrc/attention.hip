@@ -11,11 +11,6 @@
 
 #include <cmath>
 
-#ifndef V_QB
-#define V_QB 1
-#define V_NW 8
-#define V_OCC 2
-#endif
 namespace tst {
 namespace {
 
@@ -137,16 +132,18 @@ __device__ __forceinline__ float across_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <int TYPE, int ROW, int QB, int NW> struct Shape {
+// FAST: 16-bit operands whose rows lie on 16-byte borders.
+template <int TYPE, int ROW, bool FAST> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
-    static constexpr int kRows = NW * QB * 32;             // of a tile
-    static constexpr int kKeys = TYPE == TST_F32 ? 32 : 64;
-    static constexpr int kBuffers = TYPE == TST_F32 ? 1 : 2;
+    static constexpr int kWaves = FAST && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
+    static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
+    static constexpr int kKeys = FAST && ROW <= 128 ? 64 : 32;             // of a tile in the LDS
+    static constexpr int kBuffersK = FAST ? 3 : 1, kBuffersV = FAST ? 2 : 1;   // (K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
     // bytes from key to key: 16 rows of keys, and 4 rows of 32 channels of values, fall into different banks
     static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + (ROW % 128 == 96 ? 0 : 64);
     static constexpr int kPlaneK = kKeys * kStrideK, kPlaneV = kKeys * kStrideV;
-    static constexpr int kBuffer = kPlanes * (kPlaneK + kPlaneV);
-    static constexpr int kChunks = (kKeys * (ROW / 8) + 64 * NW - 1) / (64 * NW);   // of 8 entries that a thread stages, of K and as many of V
+    static constexpr int kBufferK = kPlanes * kPlaneK, kBufferV = kPlanes * kPlaneV;
+    static constexpr int kChunks = (kKeys * (ROW / 8) + kThreads - 1) / kThreads;   // of 8 entries that a thread stages, of K and as many of V
 };
 
 // Weights are 2^shift times those relative to the row's base, which the largest logit may pass by 2^kSlack before all is scaled anew: fp16 holds them with 11 bits
@@ -154,12 +151,63 @@ template <int TYPE, int ROW, int QB, int NW> struct Shape {
 constexpr float kSlack = 8.f;
 template <int TYPE> constexpr float kShift = TYPE == TST_F16 ? 7.f : 0.f;
 
-template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(64 * NW, V_OCC) k_attention(PromptArgs a)
+// A tile of keys or values on its way from memory to the LDS: 8 entries a chunk.
+template <int TYPE, int ROW, bool FAST> struct Staged {
+    typedef Shape<TYPE, ROW, FAST> S;
+    Raw<TYPE> raw[S::kChunks];
+    static __device__ __forceinline__ int key_of(int i) { return (threadIdx.x + S::kThreads * i) / (ROW / 8); }
+    static __device__ __forceinline__ int channel_of(int i) { return (threadIdx.x + S::kThreads * i) % (ROW / 8) * 8; }
+
+    // the tile's keys; zeros behind `keys`
+    __device__ __forceinline__ void load(const typename Entry<TYPE>::bits *data, int64_t stride, int tile, int keys, int size, bool wide)
+    {
+        const typename Entry<TYPE>::bits *at = data + (int64_t)tile * S::kKeys * stride;
+        const int left = keys - tile * S::kKeys;
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i) {
+            const bool there = key_of(i) < min(left, S::kKeys);
+            if constexpr (FAST) {   // (offsets within a tile have 32 bits)
+                u32x4 v = {0, 0, 0, 0};
+                if (there && channel_of(i) < size) v = *reinterpret_cast<const u32x4 *>(at + ((unsigned)key_of(i) * (unsigned)stride + (unsigned)channel_of(i)));
+                raw[i] = __builtin_bit_cast(Raw<TYPE>, v);
+            } else raw[i] = load_raw<TYPE>(at + key_of(i) * stride, channel_of(i), size, there, wide);
+        }
+    }
+    // Values that some rows of the tile do not see: 0 times an infinity would be a NaN, so what is not finite becomes a 0, and the first such key of the channel
+    // is remembered.
+    __device__ __forceinline__ void mend(int tile, int *spoilt, int &any)
+    {
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = Entry<TYPE>::get(raw[i].e[e]);
+                if (!(x - x == 0.f)) {
+                    raw[i].e[e] = 0;
+                    atomicMin(&spoilt[channel_of(i) + e], tile * S::kKeys + key_of(i));
+                    any = 1;
+                }
+            }
+    }
+    __device__ __forceinline__ void store(char *to, int stride, int plane) const
+    {
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i) {
+            if (key_of(i) >= S::kKeys) continue;
+            const Planes<TYPE> x = planes_of<TYPE>(raw[i]);
+#pragma unroll
+            for (int p = 0; p < S::kPlanes; ++p) *reinterpret_cast<u32x4 *>(to + p * plane + key_of(i) * stride + channel_of(i) * 2) = x.p[p];
+        }
+    }
+};
+
+template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape<TYPE, ROW, FAST>::kThreads), (Shape<TYPE, ROW, FAST>::kWaves / 4)) k_attention(PromptArgs a)
 {
-    typedef Shape<TYPE, ROW, QB, NW> S;
+    typedef Shape<TYPE, ROW, FAST> S;
     typedef typename Entry<TYPE>::bits Bits;
-    constexpr int P = S::kPlanes, kSteps = ROW / 16, kTiles = ROW / 32, kSub = S::kKeys / 32;
-    __shared__ __attribute__((aligned(16))) char lds[S::kBuffers * S::kBuffer];
+    constexpr int P = S::kPlanes, kSteps = ROW / 16, kTiles = ROW / 32, kSub = S::kKeys / 32;   // 32 keys at a time
+    __shared__ __attribute__((aligned(16))) char lds_k[S::kBuffersK * S::kBufferK];
+    __shared__ __attribute__((aligned(16))) char lds_v[S::kBuffersV * S::kBufferV];
     __shared__ int spoilt[ROW];   // the first key whose value of the channel is not finite, among the keys that some of the tile's rows do not see
     __shared__ int any_spoilt;
     const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
@@ -187,25 +235,20 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
     const int keys = last_token + 1;          // that the tile sees
     const int tiles = (keys + S::kKeys - 1) / S::kKeys;
 
-    for (int d = threadIdx.x; d < ROW; d += 64 * NW) spoilt[d] = 0x7fffffff;
+    for (int d = threadIdx.x; d < ROW; d += S::kThreads) spoilt[d] = 0x7fffffff;
     if (threadIdx.x == 0) any_spoilt = 0;
 
-    u32x4 q[QB][P][kSteps];
-    int limit[QB];     // keys that the row sees
-    int token[QB], q_head[QB];
-    int least = 0x7fffffff, largest = 0;
-#pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int64_t rho = rho0 + (wave * QB + b) * 32 + col;
-        const bool there = rho < (int64_t)rows.n * a.group;
-        token[b] = there ? (int)(rho / a.group) : -1;
-        q_head[b] = head * a.group + (there ? (int)(rho - (int64_t)token[b] * a.group) : 0);
-        limit[b] = token[b] + 1;
-        if (there) least = min(least, limit[b]), largest = max(largest, limit[b]);
-        const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + max(token[b], 0)) * a.q.token + q_head[b] * a.q.head;
+    u32x4 q[P][kSteps];
+    const int64_t rho = rho0 + wave * 32 + col;
+    const bool there = rho < (int64_t)rows.n * a.group;
+    const int token = there ? (int)(rho / a.group) : -1;
+    const int q_head = head * a.group + (there ? (int)(rho - (int64_t)token * a.group) : 0);
+    const int limit = token + 1;              // keys that the row sees
+    {
+        const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + max(token, 0)) * a.q.token + q_head * a.q.head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, a.wide);
+            Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, FAST || a.wide);
             if (a.negative) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -215,202 +258,217 @@ template <int TYPE, int ROW, int QB, int NW> __global__ void __launch_bounds__(6
             }
             const Planes<TYPE> x = planes_of<TYPE>(raw);
 #pragma unroll
-            for (int p = 0; p < P; ++p) q[b][p][s] = x.p[p];
+            for (int p = 0; p < P; ++p) q[p][s] = x.p[p];
         }
     }
+    int least = there ? limit : 0x7fffffff, largest = limit;
     for (int d = 1; d < 32; d <<= 1) least = min(least, __shfl_xor(least, d)), largest = max(largest, __shfl_xor(largest, d));
-    least = uniform(least), largest = uniform(largest);
+    least = uniform(least) == 0x7fffffff ? 0 : uniform(least);
+    const int own = (uniform(largest) + 31) / 32;   // times 32 keys that the wavefront's rows see
 
-    f32x16 o[QB][kTiles];
-    float base[QB], sum[QB];     // logits are relative to base, in powers of two
+    f32x16 o[kTiles];
+    float base = -INFINITY, sum = 0.f;     // logits are relative to base, in powers of two
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        base[b] = -INFINITY, sum[b] = 0.f;
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[b][t][r] = 0.f;
-    }
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
 
     const Bits *k_data = static_cast<const Bits *>(a.k.data) + (int64_t)rows.first * a.k.token + head * a.k.head;
     const Bits *v_data = static_cast<const Bits *>(a.v.data) + (int64_t)rows.first * a.v.token + head * a.v.head;
-    Raw<TYPE> k_raw[S::kChunks], v_raw[S::kChunks];
-    auto load = [&](int kt) {
+    Staged<TYPE, ROW, FAST> k_tile, v_tile;
+    auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
+    auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
+    auto store_k = [&](int kt) { k_tile.store(lds_k + kt % S::kBuffersK * S::kBufferK, S::kStrideK, S::kPlaneK); };
+    auto store_v = [&](int kt) {
+        if ((kt + 1) * S::kKeys > first_token + 1) v_tile.mend(kt, spoilt, any_spoilt);
+        v_tile.store(lds_v + kt % S::kBuffersV * S::kBufferV, S::kStrideV, S::kPlaneV);
+    };
+
+    typedef u32x4 Weights[P][2];
+    auto first_product = [&](int sub, f32x16 &z) {
+        const char *at = lds_k + sub / kSub % S::kBuffersK * S::kBufferK + (sub % kSub * 32 + col) * S::kStrideK + half * 16;
 #pragma unroll
-        for (int i = 0; i < S::kChunks; ++i) {
-            const int c = threadIdx.x + 64 * NW * i, key = kt * S::kKeys + c / (ROW / 8), d = c % (ROW / 8) * 8;
-            const bool there = key < keys && c < S::kKeys * (ROW / 8);
-            k_raw[i] = load_raw<TYPE>(k_data + (int64_t)min(key, keys - 1) * a.k.token, d, a.size, there, a.wide);
-            v_raw[i] = load_raw<TYPE>(v_data + (int64_t)min(key, keys - 1) * a.v.token, d, a.size, there, a.wide);
+        for (int r = 0; r < 16; ++r) z[r] = 0.f;
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) {
+            u32x4 k[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) k[p] = *reinterpret_cast<const u32x4 *>(at + p * S::kPlaneK + step * 32);
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int r = 0; p + r < P; ++r) z = product<TYPE>(k[p], q[r][step], z);
         }
     };
-    auto store = [&](int kt) {
-        char *buffer = lds + kt % S::kBuffers * S::kBuffer;
-        // values that some rows do not see: 0 times an infinity would be a NaN, so what is not finite is a 0 there and remembered
-        if ((kt + 1) * S::kKeys > first_token + 1) {
+    auto mask = [&](int sub, f32x16 &z) {
+        if ((sub + 1) * 32 > least) {
 #pragma unroll
-            for (int i = 0; i < S::kChunks; ++i) {
-                const int c = threadIdx.x + 64 * NW * i, key = kt * S::kKeys + c / (ROW / 8), d = c % (ROW / 8) * 8;
+            for (int r = 0; r < 16; ++r)
+                if (sub * 32 + 8 * (r / 4) + 4 * half + r % 4 >= limit) z[r] = -INFINITY;
+        }
+    };
+    auto rebase = [&](const f32x16 &z) {
+        const float top = across_max(largest_of(z)) * a.scale;
+        if (__any(top > base + kSlack)) {
+            const float now = fmaxf(base, top), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - now);
+            base = now;
+            sum *= keep;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = Entry<TYPE>::get(v_raw[i].e[e]);
-                    if (!(x - x == 0.f)) {
-                        v_raw[i].e[e] = 0;
-                        atomicMin(&spoilt[d + e], key);
-                        any_spoilt = 1;
-                    }
+            for (int t = 0; t < kTiles; ++t) o[t] *= keep;
+        }
+    };
+    auto weights = [&](const f32x16 &z, Weights &w) {
+        const float from = base == -INFINITY ? 0.f : base - kShift<TYPE>;
+        float p[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[r], a.scale, -from));
+            if constexpr (TYPE == TST_F32) sum += p[r];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (TYPE == TST_F32) {
+                Raw<TYPE> x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x.e[i] = p[8 * j + i];
+                const Planes<TYPE> px = planes_of<TYPE>(x);
+#pragma unroll
+                for (int q = 0; q < P; ++q) w[q][j] = px.p[q];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Pair<TYPE> pair = {(typename Pair<TYPE>::entry)p[8 * j + 2 * i], (typename Pair<TYPE>::entry)p[8 * j + 2 * i + 1]};
+                    sum = pair.added(sum);
+                    w[0][j][i] = pair.bits();
                 }
             }
         }
+    };
+    auto second_product = [&](int sub, const Weights &w) {
+        // four keys of a lane's channel: in each group of 16 lanes, lanes 4 r .. 4 r + 3 point to 16 channels of the r-th key
+        const char *from = lds_v + sub / kSub % S::kBuffersV * S::kBufferV + (sub % kSub * 32 + 4 * half + lane % 16 / 4) * S::kStrideV + (col / 16 * 16 + lane % 4 * 4) * 2;
 #pragma unroll
-        for (int i = 0; i < S::kChunks; ++i) {
-            const int c = threadIdx.x + 64 * NW * i, key = c / (ROW / 8), d = c % (ROW / 8) * 8;
-            if (key >= S::kKeys) continue;
-            const Planes<TYPE> kp = planes_of<TYPE>(k_raw[i]), vp = planes_of<TYPE>(v_raw[i]);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                *reinterpret_cast<u32x4 *>(buffer + p * S::kPlaneK + key * S::kStrideK + d * 2) = kp.p[p];
-                *reinterpret_cast<u32x4 *>(buffer + P * S::kPlaneK + p * S::kPlaneV + key * S::kStrideV + d * 2) = vp.p[p];
+            for (int t = 0; t < kTiles; ++t) {
+                u32x4 v[P];
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    u32x2 part[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const char *at = from + p * S::kPlaneV + (16 * j + 8 * i) * S::kStrideV + t * 64;
+                        part[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
+                    }
+                    v[p] = u32x4{part[0][0], part[0][1], part[1][0], part[1][1]};
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int r = 0; p + r < P; ++r) o[t] = product<TYPE>(v[p], w[r][j], o[t]);
             }
-        }
     };
 
     __syncthreads();     // spoilt is clear
-    load(0);
-    store(0);
-    __syncthreads();
-    for (int kt = 0; kt < tiles; ++kt) {
-        if (kt + 1 < tiles) load(kt + 1);
-        const char *buffer = lds + kt % S::kBuffers * S::kBuffer;
-        if (kt * S::kKeys < largest) {
-            f32x16 z[QB][kSub];
+    if constexpr (!FAST) {
+        for (int kt = 0; kt < tiles; ++kt) {
+            if (kt == 0) load_k(0), load_v(0);
+            store_k(kt), store_v(kt);
+            __syncthreads();
+            if (kt + 1 < tiles) load_k(kt + 1), load_v(kt + 1);
 #pragma unroll
             for (int s = 0; s < kSub; ++s) {
-#pragma unroll
-                for (int b = 0; b < QB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) z[b][s][r] = 0.f;
-#pragma unroll
-                for (int step = 0; step < kSteps; ++step) {
-                    u32x4 k[P];
-#pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        k[p] = *reinterpret_cast<const u32x4 *>(buffer + p * S::kPlaneK + (s * 32 + col) * S::kStrideK + (16 * step + 8 * half) * 2);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b)
-#pragma unroll
-                        for (int p = 0; p < P; ++p)
-#pragma unroll
-                            for (int r = 0; p + r < P; ++r) z[b][s] = product<TYPE>(k[p], q[b][r][step], z[b][s]);
+                const int sub = kt * kSub + s;
+                if (sub < own) {
+                    f32x16 z;
+                    Weights w;
+                    first_product(sub, z);
+                    mask(sub, z);
+                    rebase(z);
+                    weights(z, w);
+                    second_product(sub, w);
                 }
             }
-            const bool cut = (kt + 1) * S::kKeys > least;
-            u32x4 w[QB][P][kSub][2];
-#pragma unroll
-            for (int b = 0; b < QB; ++b) {
-                if (cut) {
-#pragma unroll
-                    for (int s = 0; s < kSub; ++s)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (kt * S::kKeys + s * 32 + 8 * (r / 4) + 4 * half + r % 4 >= limit[b]) z[b][s][r] = -INFINITY;
-                }
-                float top = largest_of(z[b][0]);
-                if constexpr (kSub == 2) top = __builtin_elementwise_maximum(top, largest_of(z[b][kSub - 1]));
-                top = across_max(top) * a.scale;
-                if (__any(top > base[b] + kSlack)) {
-                    const float now = fmaxf(base[b], top), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base[b] - now);
-                    base[b] = now;
-                    sum[b] *= keep;
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t) o[b][t] *= keep;
-                }
-                const float from = base[b] == -INFINITY ? 0.f : base[b] - kShift<TYPE>;
-                float s_all = 0.f;
-#pragma unroll
-                for (int s = 0; s < kSub; ++s) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        z[b][s][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][s][r], a.scale, -from));
-                        if constexpr (TYPE == TST_F32) s_all += z[b][s][r];
-                    }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if constexpr (TYPE == TST_F32) {
-                            Raw<TYPE> x;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x.e[i] = z[b][s][8 * j + i];
-                            const Planes<TYPE> px = planes_of<TYPE>(x);
-#pragma unroll
-                            for (int p = 0; p < P; ++p) w[b][p][s][j] = px.p[p];
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const Pair<TYPE> pair = {(typename Pair<TYPE>::entry)z[b][s][8 * j + 2 * i], (typename Pair<TYPE>::entry)z[b][s][8 * j + 2 * i + 1]};
-                                s_all = pair.added(s_all);
-                                w[b][0][s][j][i] = pair.bits();
-                            }
-                        }
-                    }
-                }
-                sum[b] += s_all;
-            }
-            // four keys of a lane's channel: in each group of 16 lanes, lanes 4 r .. 4 r + 3 point to 16 channels of the r-th key
-            const char *v_at = buffer + P * S::kPlaneK + (4 * half + lane % 16 / 4) * S::kStrideV + (col / 16 * 16 + lane % 4 * 4) * 2;
-#pragma unroll
-            for (int s = 0; s < kSub; ++s)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
-                        u32x4 v[P];
-#pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            u32x2 part[2];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const char *at = v_at + p * S::kPlaneV + (s * 32 + 16 * j + 8 * i) * S::kStrideV + t * 64;
-                                part[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
-                            }
-                            v[p] = u32x4{part[0][0], part[0][1], part[1][0], part[1][1]};
-                        }
-#pragma unroll
-                        for (int b = 0; b < QB; ++b)
-#pragma unroll
-                            for (int p = 0; p < P; ++p)
-#pragma unroll
-                                for (int r = 0; p + r < P; ++r) o[b][t] = product<TYPE>(v[p], w[b][r][s][j], o[b][t]);
-                    }
+            __syncthreads();
         }
-        if (S::kBuffers == 1) __syncthreads();   // everybody has read the only buffer
-        if (kt + 1 < tiles) store(kt + 1);
+    } else {
+        // While the matrix cores work on the next 32 keys' logits, the other units make the weights of these, which they then take.  K is a tile ahead of V.
+        f32x16 z[2];
+        load_k(0), load_v(0);
+        store_k(0), store_v(0);
+        if (tiles > 1) load_k(1), store_k(1);
         __syncthreads();
+        if (own > 0) {
+            first_product(0, z[0]);
+            mask(0, z[0]);
+            rebase(z[0]);
+        }
+        auto inner = [&](int sub, f32x16 &now, f32x16 &next) {     // all rows see the next 32 keys
+            Weights w;
+            first_product(sub + 1, next);
+            weights(now, w);
+            __builtin_amdgcn_sched_barrier(0);
+            second_product(sub, w);
+            rebase(next);
+        };
+        auto last = [&](int sub, f32x16 &now, f32x16 &next) {      // some do not, or there are none
+            if (sub >= own) return;
+            Weights w;
+            weights(now, w);
+            second_product(sub, w);
+            if (sub + 1 >= own) return;
+            first_product(sub + 1, next);
+            mask(sub + 1, next);
+            rebase(next);
+        };
+        auto tile_step = [&](int kt, auto step, f32x16 &first, f32x16 &second) {
+            if (kt + 2 < tiles) load_k(kt + 2);
+            if (kt + 1 < tiles) load_v(kt + 1);
+            step(kt * kSub, first, second);
+            if constexpr (kSub == 2) step(kt * kSub + 1, second, first);
+            if (kt + 2 < tiles) store_k(kt + 2);
+            if (kt + 1 < tiles) store_v(kt + 1);
+            __syncthreads();
+        };
+        int kt = 0;
+        if constexpr (kSub == 2) {
+            const int whole = (least / 32 - 1) / 2;
+            for (; kt < whole; ++kt) tile_step(kt, inner, z[0], z[1]);
+            for (; kt < tiles; ++kt) tile_step(kt, last, z[0], z[1]);
+        } else {
+            const int whole = (least / 32 - 1) / 2 * 2;
+            for (; kt < whole; kt += 2) {
+                tile_step(kt, inner, z[0], z[1]);
+                tile_step(kt + 1, inner, z[1], z[0]);
+            }
+            for (; kt < tiles; kt += 2) {
+                tile_step(kt, last, z[0], z[1]);
+                if (kt + 1 < tiles) tile_step(kt + 1, last, z[1], z[0]);
+            }
+        }
     }
 
+    if (!there) return;
     const bool bad = any_spoilt;
+    const float inverse = 1.f / across_sum(sum);
+    Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + token) * a.q_heads + q_head) * a.size;
+    const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        if (token[b] < 0) continue;
-        const float inverse = 1.f / across_sum(sum[b]);
-        Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + token[b]) * a.q_heads + q_head[b]) * a.size;
-        const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
+        for (int r = 0; r < 16; r += 4) {
+            const int d = 32 * t + 2 * r + 4 * half;
+            Bits four[4];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d = 32 * t + 2 * r + 4 * half;
-                Bits four[4];
+            for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(bad && spoilt[d + e] < limit ? kNan : o[t][r + e] * inverse);
+            if (whole) {
+                if (d < a.size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), four, sizeof(four));
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(bad && spoilt[d + e] < limit[b] ? kNan : o[b][t][r + e] * inverse);
-                if (whole) {
-                    if (d < a.size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), four, sizeof(four));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (d + e < a.size) out[d + e] = four[e];
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < a.size) out[d + e] = four[e];
             }
-    }
+        }
 }
 
 bool wide(const Rows &x, int type, int size)
@@ -438,9 +496,21 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
     a.wide = tst::wide(a.q, type, head_size) && tst::wide(a.k, type, head_size) && tst::wide(a.v, type, head_size);
     return tst::status(tst::for_type(type, [&](auto t) {
         return tst::for_row(head_size, [&](auto r) {
-            constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value, QB = V_QB, NW = V_NW;
-            a.tiles = (int)((int64_t)tokens * group / tst::Shape<TYPE, ROW, QB, NW>::kRows) + sequences;
-            tst::k_attention<TYPE, ROW, QB, NW><<<(unsigned)a.tiles * heads, 64 * NW, 0, static_cast<hipStream_t>(stream)>>>(a);
+            constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value;
+            hipStream_t st = static_cast<hipStream_t>(stream);
+            auto launch = [&](auto fast) {
+                constexpr bool FAST = decltype(fast)::value;
+                typedef tst::Shape<TYPE, ROW, FAST> S;
+                a.tiles = (int)((int64_t)tokens * group / S::kRows) + sequences;
+                tst::k_attention<TYPE, ROW, FAST><<<(unsigned)a.tiles * heads, S::kThreads, 0, st>>>(a);
+            };
+            if constexpr (TYPE != TST_F32) {
+                if (a.wide && a.k.token <= 1 << 24 && a.v.token <= 1 << 24) {
+                    launch(std::true_type{});
+                    return hipGetLastError();
+                }
+            }
+            launch(std::false_type{});
             return hipGetLastError();
         });
     }));
