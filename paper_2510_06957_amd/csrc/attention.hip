@@ -11,6 +11,9 @@
 
 #include <cmath>
 
+#ifndef V_OCC64
+#define V_OCC64 2
+#endif
 namespace tst {
 namespace {
 
@@ -136,6 +139,7 @@ __device__ __forceinline__ float across_sum(float v)
 template <int TYPE, int ROW, bool FAST> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
     static constexpr int kWaves = FAST && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
+    static constexpr int kOccupancy = FAST && ROW <= 64 ? V_OCC64 : kWaves / 4;
     static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
     static constexpr int kKeys = FAST && ROW <= 128 ? 64 : 32;             // of a tile in the LDS
     static constexpr int kBuffersK = FAST ? 3 : 1, kBuffersV = FAST ? 2 : 1;   // (K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
@@ -166,10 +170,11 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i) {
             const bool there = key_of(i) < min(left, S::kKeys);
-            if constexpr (FAST) {   // (offsets within a tile have 32 bits)
-                u32x4 v = {0, 0, 0, 0};
-                if (there && channel_of(i) < size) v = *reinterpret_cast<const u32x4 *>(at + ((unsigned)key_of(i) * (unsigned)stride + (unsigned)channel_of(i)));
-                raw[i] = __builtin_bit_cast(Raw<TYPE>, v);
+            if constexpr (FAST) {
+                // from somewhere in the tile whatever it is (zeros come in store()): a load that depends on the lane would have to be waited for
+                // before the next.  (offsets within a tile have 32 bits)
+                const int key = min(key_of(i), left - 1), channel = channel_of(i) < size ? channel_of(i) : 0;
+                raw[i] = __builtin_bit_cast(Raw<TYPE>, *reinterpret_cast<const u32x4 *>(at + ((unsigned)key * (unsigned)stride + (unsigned)channel)));
             } else raw[i] = load_raw<TYPE>(at + key_of(i) * stride, channel_of(i), size, there, wide);
         }
     }
@@ -189,8 +194,13 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
                 }
             }
     }
-    __device__ __forceinline__ void store(char *to, int stride, int plane) const
+    __device__ __forceinline__ void store(char *to, int stride, int plane, int left, int size)
     {
+        if (FAST && (left < S::kKeys || size < ROW)) {
+#pragma unroll
+            for (int i = 0; i < S::kChunks; ++i)
+                if (key_of(i) >= left || channel_of(i) >= size) raw[i] = Raw<TYPE>{};
+        }
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i) {
             if (key_of(i) >= S::kKeys) continue;
@@ -201,7 +211,7 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
     }
 };
 
-template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape<TYPE, ROW, FAST>::kThreads), (Shape<TYPE, ROW, FAST>::kWaves / 4)) k_attention(PromptArgs a)
+template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape<TYPE, ROW, FAST>::kThreads), (Shape<TYPE, ROW, FAST>::kOccupancy)) k_attention(PromptArgs a)
 {
     typedef Shape<TYPE, ROW, FAST> S;
     typedef typename Entry<TYPE>::bits Bits;
@@ -278,10 +288,10 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     Staged<TYPE, ROW, FAST> k_tile, v_tile;
     auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
     auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
-    auto store_k = [&](int kt) { k_tile.store(lds_k + kt % S::kBuffersK * S::kBufferK, S::kStrideK, S::kPlaneK); };
+    auto store_k = [&](int kt) { k_tile.store(lds_k + kt % S::kBuffersK * S::kBufferK, S::kStrideK, S::kPlaneK, keys - kt * S::kKeys, a.size); };
     auto store_v = [&](int kt) {
         if ((kt + 1) * S::kKeys > first_token + 1) v_tile.mend(kt, spoilt, any_spoilt);
-        v_tile.store(lds_v + kt % S::kBuffersV * S::kBufferV, S::kStrideV, S::kPlaneV);
+        v_tile.store(lds_v + kt % S::kBuffersV * S::kBufferV, S::kStrideV, S::kPlaneV, keys - kt * S::kKeys, a.size);
     };
 
     typedef u32x4 Weights[P][2];
