@@ -11,9 +11,6 @@
 
 #include <cmath>
 
-#ifndef V_OCC64
-#define V_OCC64 2
-#endif
 namespace tst {
 namespace {
 
@@ -139,7 +136,7 @@ __device__ __forceinline__ float across_sum(float v)
 template <int TYPE, int ROW, bool FAST> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
     static constexpr int kWaves = FAST && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
-    static constexpr int kOccupancy = FAST && ROW <= 64 ? V_OCC64 : kWaves / 4;
+    static constexpr int kOccupancy = FAST && ROW <= 64 ? 4 : kWaves / 4;
     static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
     static constexpr int kKeys = FAST && ROW <= 128 ? 64 : 32;             // of a tile in the LDS
     static constexpr int kBuffersK = FAST ? 3 : 1, kBuffersV = FAST ? 2 : 1;   // (K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
@@ -154,6 +151,46 @@ template <int TYPE, int ROW, bool FAST> struct Shape {
 // down to 2^-21 of the largest.
 constexpr float kSlack = 8.f;
 template <int TYPE> constexpr float kShift = TYPE == TST_F16 ? 7.f : 0.f;
+
+// The tile of rows that workgroups of a number have, -1: none.  A sequence's tiles come one after another, since they read the same keys and values, the last,
+// which sees most of them, first.  Of up to 64 sequences the shortest come first: what is left at the end are then the shortest tiles of the longest (4096 and 1024 tokens, 32
+// heads of 128: 182 us, 190 the other way round); of more, the last.
+struct Place {
+    int first, n, tile;   // of the sequence: its first row and how many it has; tokens * query heads <= 2^27, so rows of tiles have 32 bits
+};
+__device__ __forceinline__ Place place_of(const PromptArgs &a, int rows, int number)
+{
+    const int lane = threadIdx.x % 64;
+    if (a.sequences <= 64) {
+        const Span span = lane < a.sequences ? span_of(a.offsets, a.tokens, lane) : Span{0, 0};
+        const int mine = (span.n * a.group + rows - 1) / rows;
+        int before = 0;     // tiles of shorter sequences
+        for (int i = 0; i < a.sequences; ++i) {
+            const int other = __builtin_amdgcn_readlane(mine, i);
+            before += other < mine || (other == mine && i > lane) ? other : 0;
+        }
+        const int at = number - before;
+        const unsigned long long here = __ballot(at >= 0 && at < mine);
+        if (!here) return Place{0, 0, -1};
+        const int seq = __ffsll(here) - 1;
+        return Place{__builtin_amdgcn_readlane(span.first, seq), __builtin_amdgcn_readlane(span.n, seq), __builtin_amdgcn_readlane(mine - 1 - at, seq)};
+    }
+    // tiles of sequence i have the numbers from offsets[i] * group / rows + i on
+    auto base = [&](int i) { return min(max(a.offsets[i], 0), a.tokens) * a.group / rows + i; };
+    const int at = a.tiles - 1 - number;
+    int seq = 0, n = a.sequences;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = seq + lane * step;
+        const bool before = lane * step < n && base(min(i, a.sequences)) <= at;
+        const int c = max(__popcll(__ballot(before)), 1) - 1;
+        seq += c * step;
+        n = min(step, n - c * step);
+    }
+    seq = uniform(seq);
+    const Span span = span_of(a.offsets, a.tokens, seq);
+    const int tile = at - base(seq);
+    return Place{span.first, span.n, tile >= 0 && tile * (int64_t)rows < span.n * a.group ? tile : -1};
+}
 
 // A tile of keys or values on its way from memory to the LDS: 8 entries a chunk.
 template <int TYPE, int ROW, bool FAST> struct Staged {
@@ -221,41 +258,35 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     __shared__ int spoilt[ROW];   // the first key whose value of the channel is not finite, among the keys that some of the tile's rows do not see
     __shared__ int any_spoilt;
     const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
-    // tiles of sequence i have the numbers from offsets[i] * group / rows + i on; the last tiles, which see most keys, come first
-    const int head = blockIdx.x % a.heads, number = a.tiles - 1 - (int)(blockIdx.x / a.heads);
-    int seq = 0;
-    {
-        auto base = [&](int i) { return (int64_t)min(max(a.offsets[i], 0), a.tokens) * a.group / S::kRows + i; };
-        int n = a.sequences;
-        while (n > 1) {
-            const int step = (n + 63) / 64, i = seq + lane * step;
-            const bool before = lane * step < n && base(min(i, a.sequences)) <= number;
-            const int c = max(__popcll(__ballot(before)), 1) - 1;
-            seq += c * step;
-            n = min(step, n - c * step);
-        }
-        seq = uniform(seq);
-    }
-    const Span rows = span_of(a.offsets, a.tokens, seq);
-    const int tile = number - (int)((int64_t)min(max(a.offsets[seq], 0), a.tokens) * a.group / S::kRows + seq);
-    if (tile < 0 || (int64_t)tile * S::kRows >= (int64_t)rows.n * a.group) return;
+    const int head = blockIdx.x % a.heads;
+    const Place place = place_of(a, S::kRows, (int)(blockIdx.x / a.heads));
+    if (place.tile < 0) return;
+    const int tile = uniform(place.tile), n = uniform(place.n), first = uniform(place.first);
 
-    const int64_t rho0 = (int64_t)tile * S::kRows;
-    const int first_token = (int)(rho0 / a.group), last_token = (int)min((rho0 + S::kRows - 1) / a.group, (int64_t)rows.n - 1);
+    const unsigned group = a.group, rho0 = tile * S::kRows;
+    const int first_token = rho0 / group, last_token = min((int)((rho0 + S::kRows - 1) / group), n - 1);
     const int keys = last_token + 1;          // that the tile sees
     const int tiles = (keys + S::kKeys - 1) / S::kKeys;
+
+    const Bits *k_data = static_cast<const Bits *>(a.k.data) + (int64_t)first * a.k.token + head * a.k.head;
+    const Bits *v_data = static_cast<const Bits *>(a.v.data) + (int64_t)first * a.v.token + head * a.v.head;
+    Staged<TYPE, ROW, FAST> k_tile, v_tile, k_next;
+    auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
+    auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
+    load_k(0), load_v(0);
+    if (FAST && tiles > 1) k_next.load(k_data, a.k.token, 1, keys, a.size, true);
 
     for (int d = threadIdx.x; d < ROW; d += S::kThreads) spoilt[d] = 0x7fffffff;
     if (threadIdx.x == 0) any_spoilt = 0;
 
     u32x4 q[P][kSteps];
-    const int64_t rho = rho0 + wave * 32 + col;
-    const bool there = rho < (int64_t)rows.n * a.group;
-    const int token = there ? (int)(rho / a.group) : -1;
-    const int q_head = head * a.group + (there ? (int)(rho - (int64_t)token * a.group) : 0);
+    const unsigned rho = rho0 + wave * 32 + col;
+    const bool there = rho < (unsigned)n * group;
+    const int token = there ? (int)(rho / group) : -1;
+    const int q_head = head * a.group + (there ? (int)(rho - token * group) : 0);
     const int limit = token + 1;              // keys that the row sees
     {
-        const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + max(token, 0)) * a.q.token + q_head * a.q.head;
+        const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(first + max(token, 0)) * a.q.token + q_head * a.q.head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, FAST || a.wide);
@@ -283,11 +314,6 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
 
-    const Bits *k_data = static_cast<const Bits *>(a.k.data) + (int64_t)rows.first * a.k.token + head * a.k.head;
-    const Bits *v_data = static_cast<const Bits *>(a.v.data) + (int64_t)rows.first * a.v.token + head * a.v.head;
-    Staged<TYPE, ROW, FAST> k_tile, v_tile;
-    auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
-    auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
     auto store_k = [&](int kt) { k_tile.store(lds_k + kt % S::kBuffersK * S::kBufferK, S::kStrideK, S::kPlaneK, keys - kt * S::kKeys, a.size); };
     auto store_v = [&](int kt) {
         if ((kt + 1) * S::kKeys > first_token + 1) v_tile.mend(kt, spoilt, any_spoilt);
@@ -382,7 +408,6 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     __syncthreads();     // spoilt is clear
     if constexpr (!FAST) {
         for (int kt = 0; kt < tiles; ++kt) {
-            if (kt == 0) load_k(0), load_v(0);
             store_k(kt), store_v(kt);
             __syncthreads();
             if (kt + 1 < tiles) load_k(kt + 1), load_v(kt + 1);
@@ -404,9 +429,8 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     } else {
         // While the matrix cores work on the next 32 keys' logits, the other units make the weights of these, which they then take.  K is a tile ahead of V.
         f32x16 z[2];
-        load_k(0), load_v(0);
         store_k(0), store_v(0);
-        if (tiles > 1) load_k(1), store_k(1);
+        if (tiles > 1) k_next.store(lds_k + S::kBufferK, S::kStrideK, S::kPlaneK, keys - S::kKeys, a.size);
         __syncthreads();
         if (own > 0) {
             first_product(0, z[0]);
@@ -461,7 +485,7 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     if (!there) return;
     const bool bad = any_spoilt;
     const float inverse = 1.f / across_sum(sum);
-    Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + token) * a.q_heads + q_head) * a.size;
+    Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(first + token) * a.q_heads + q_head) * a.size;
     const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)

@@ -392,3 +392,11 @@ def test_prompts_sizes(size, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_prompts_scales(large, scale, dtype):
     check_prompt([200, 33], 4, 1, 64, dtype, 25, large=large, scale=scale)
+
+
+def test_prompts_of_many_sequences():
+    """More sequences than are put in order by their lengths, and as many; the others are 0 to 40 tokens long."""
+    for n, long in ((64, 700), (65, 700), (1500, 300)):
+        lens = [int(x) for x in rng(26, n).integers(0, 41, n)]
+        lens[n // 3] = long
+        check_prompt(lens, 2, 1, 64, "bf16", 26)
