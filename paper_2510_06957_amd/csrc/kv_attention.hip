@@ -13,6 +13,9 @@
 // each whatever the batch is; the host knows how many there are at most.  Chunks of one tile of rows are joined by k_join.
 #include "attention_internal.h"
 
+#ifndef V_WANT
+#define V_WANT 2
+#endif
 namespace tst {
 namespace {
 
@@ -38,12 +41,6 @@ struct KvArgs {
     int items;                  // of a head, at most
 };
 
-// What a wavefront knows of the call: the chunks' length, and which piece of which sequence an item is.
-struct Item {
-    int seq, tile, chunk, chunks;   // chunks of the tile; seq -1: none
-    int64_t first;                  // number of the tile's first chunk
-};
-
 __device__ __forceinline__ int units_of(const KvArgs &a, int i)
 {
     const int most = a.seqs.columns << a.cache.page_shift;   // a length behind the table's end meets one block that is not there
@@ -51,7 +48,7 @@ __device__ __forceinline__ int units_of(const KvArgs &a, int i)
 }
 __device__ __forceinline__ int tiles_of(const KvArgs &a, int i)
 {
-    return (int)(((int64_t)span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + a.rows - 1) / a.rows);
+    return (span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + a.rows - 1) / a.rows;   // (tokens * query heads <= 2^27)
 }
 
 __device__ __forceinline__ int64_t wave_sum(int64_t v)
@@ -71,19 +68,20 @@ __device__ __forceinline__ int chunk_length(const KvArgs &a)
     return (int)min(max(length, (int64_t)kLeastChunk), (int64_t)1 << 30);
 }
 
-// Item `at`: sequences in order, a sequence's tiles in order, a tile's chunks in order.
+__device__ __forceinline__ int chunks_of(const KvArgs &a, int i, int length) { return max((units_of(a, i) + length - 1) / length, 1); }
+
+// Item `at`: sequences in order, a sequence's tiles in order, a tile's chunks in order.  seq -1: there are fewer.
+struct Item {
+    int seq, tile, chunk, chunks;   // chunks of the tile
+};
 __device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t at)
 {
     const int lane = threadIdx.x % 64;
     int64_t before = 0;
     for (int base = 0; base < a.seqs.count; base += 64) {
         const int i = base + lane;
-        int64_t mine = 0;
-        int chunks = 0;
-        if (i < a.seqs.count) {
-            chunks = max((units_of(a, i) + length - 1) / length, 1);
-            mine = (int64_t)tiles_of(a, i) * chunks;
-        }
+        const int chunks = i < a.seqs.count ? chunks_of(a, i, length) : 1;
+        const int64_t mine = i < a.seqs.count ? (int64_t)tiles_of(a, i) * chunks : 0;
         int64_t upto = mine;
         for (int d = 1; d < 64; d <<= 1) {
             const int64_t other = __shfl_up(upto, d);
@@ -93,13 +91,39 @@ __device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t a
         if (behind) {
             const int l = __ffsll(behind) - 1;
             const int n = __shfl(chunks, l);
-            const int64_t start = before + __shfl(upto, l) - __shfl(mine, l);
-            const int rest = (int)(at - start);
-            return Item{base + l, rest / n, rest % n, n, at - rest % n};
+            const int rest = (int)(at - (before + __shfl(upto, l) - __shfl(mine, l)));
+            return Item{base + l, rest / n, rest % n, n};
         }
         before += __shfl(upto, 63);
     }
-    return Item{-1, 0, 0, 0, 0};
+    return Item{-1, 0, 0, 0};
+}
+__device__ __forceinline__ int64_t items_before(const KvArgs &a, int seq, int length)
+{
+    int64_t n = 0;
+    for (int i = threadIdx.x % 64; i < seq; i += 64) n += (int64_t)tiles_of(a, i) * chunks_of(a, i, length);
+    return wave_sum(n);
+}
+
+// Tiles of sequence i have the numbers from offsets[i] * group / rows + i on.  tile -1: a number that none has.
+struct Slot {
+    int seq, tile;
+};
+__device__ __forceinline__ Slot find_slot(const KvArgs &a, int at)
+{
+    const int lane = threadIdx.x % 64;
+    auto base = [&](int i) { return (a.seqs.offsets ? min(max(a.seqs.offsets[i], 0), a.seqs.tokens) : i) * a.group / a.rows + i; };
+    int lo = 0, n = a.seqs.count;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = lo + lane * step;
+        const bool before = lane * step < n && base(min(i, a.seqs.count - 1)) <= at;
+        const int c = max(__popcll(__ballot(before)), 1) - 1;
+        lo += c * step;
+        n = min(step, n - c * step);
+    }
+    lo = uniform(lo);
+    const int tile = uniform(at - base(lo));
+    return Slot{lo, tile >= 0 && tile < tiles_of(a, lo) ? tile : -1};
 }
 
 // Four codes as fp16: 1024 + (code + 128) by its bits, less 1152.
@@ -142,9 +166,9 @@ template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(
     const int lane = threadIdx.x % 64, g = lane / 16, size = a.cache.size;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int64_t rho = (int64_t)tile * a.rows + rt * 16 + lane % 16;
-        if (rho >= (int64_t)rows.n * a.group) continue;
-        const int t = (int)(rho / a.group), h = head * a.group + (int)(rho - (int64_t)t * a.group);
+        const unsigned rho = tile * a.rows + rt * 16 + lane % 16;
+        if (rho >= (unsigned)(rows.n * a.group)) continue;
+        const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group);
         Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
         const float inverse = limit[rt] == 0 ? 0.f : 1.f / sum[rt];
         const bool whole = (size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
@@ -181,20 +205,10 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         begin = it.chunk * length;
         end = min(begin + length, units_of(a, it.seq));
     } else {
-        // tiles of sequence i have the numbers from offsets[i] * group / rows + i on
-        auto base = [&](int i) { return (int64_t)(a.seqs.offsets ? min(max(a.seqs.offsets[i], 0), a.seqs.tokens) : i) * a.group / a.rows + i; };
-        int lo = 0, n = a.seqs.count;
-        while (n > 1) {
-            const int step = (n + 63) / 64, i = lo + lane * step;
-            const bool before = lane * step < n && base(min(i, a.seqs.count - 1)) <= (int)blockIdx.x;
-            const int c = max(__popcll(__ballot(before)), 1) - 1;
-            lo += c * step;
-            n = min(step, n - c * step);
-        }
-        const int first = (int)base(lo);
-        it = Item{lo, (int)blockIdx.x - first, 0, 1, 0};
-        if (it.tile < 0 || it.tile >= tiles_of(a, lo)) return;
-        end = units_of(a, lo);
+        const Slot slot = find_slot(a, blockIdx.x);
+        if (slot.tile < 0) return;
+        it = Item{slot.seq, slot.tile, 0, 1};
+        end = units_of(a, slot.seq);
     }
     const int seq = uniform(it.seq), tile = uniform(it.tile);
     begin = uniform(begin), end = uniform(end);
@@ -208,9 +222,9 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     int least = kMaxPosition;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int64_t rho = (int64_t)tile * a.rows + rt * 16 + m16;
-        const bool there = rho < (int64_t)rows.n * a.group;
-        const int t = there ? (int)(rho / a.group) : 0, h = head * a.group + (there ? (int)(rho - (int64_t)t * a.group) : 0);
+        const unsigned rho = tile * a.rows + rt * 16 + m16;
+        const bool there = rho < (unsigned)(rows.n * a.group);
+        const int t = there ? rho / (unsigned)a.group : 0, h = head * a.group + (there ? (int)(rho - t * a.group) : 0);
         const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + t) * a.q.token + h * a.q.head;
         limit[rt] = there ? max(len - rows.n + t + 1, 0) : 0;
         if (there) least = min(least, limit[rt]);
@@ -408,38 +422,50 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     }
 }
 
-// Joins the chunks of a tile: a wavefront for 16 channels of 16 rows.  Its workgroup has the number of the tile's first chunk.
-template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64) k_kv_join(KvArgs a)
+// Joins the chunks of a tile: a workgroup for 16 channels of 16 rows, whose wavefronts share the chunks.
+template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves) k_kv_join(KvArgs a)
 {
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int kTiles = ROW / 16;
-    const int lane = threadIdx.x, g = lane / 16, m16 = lane % 16, head = blockIdx.y, rt = blockIdx.z / kTiles, dt = blockIdx.z % kTiles;
-    const int length = uniform(chunk_length(a));
-    const Item it = find_item(a, length, blockIdx.x);
-    if (it.seq < 0 || it.chunk != 0 || it.chunks == 1) return;
-    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, it.seq);
-    const int64_t place = (int64_t)head * a.items + blockIdx.x;
+    __shared__ f32x4 shared[kWaves][64];
+    __shared__ float totals[kWaves][64];
+    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y, rt = blockIdx.z / kTiles, dt = blockIdx.z % kTiles;
+    const Slot slot = find_slot(a, blockIdx.x);
+    if (slot.tile < 0) return;
+    const int length = uniform(chunk_length(a)), chunks = chunks_of(a, slot.seq, length);
+    if (chunks == 1) return;
+    const int64_t first = items_before(a, slot.seq, length) + (int64_t)slot.tile * chunks;
+    const int n = (int)min((int64_t)chunks, a.items - first);   // (fewer where offsets do not ascend)
+    const int64_t place = (int64_t)head * a.items + first;
     const float2 *states = a.states + place * (RT * 16) + rt * 16 + m16;
     const f32x4 *sums = a.sums + (place * (RT * kTiles) + rt * kTiles + dt) * 64 + lane;
-    const int n = uniform(min(it.chunks, a.items - (int)blockIdx.x));   // (fewer where offsets do not ascend)
     float all = -INFINITY;
-    for (int c = 0; c < n; ++c) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
+#pragma unroll 4
+    for (int c = g; c < n; c += 4) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
+    all = fmaxf(all, __shfl_xor(all, 16));
+    all = fmaxf(all, __shfl_xor(all, 32));
     float total = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int c = 0; c < n; ++c) {
+    for (int c = wave; c < n; c += kWaves) {
         const float2 s = states[(int64_t)c * (RT * 16)];
         const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
         const float w = weight_of(s.x, all);
         total += w * s.y;
-        if (w != 0.f) o += w * v;
+        o += w != 0.f ? w * v : f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int64_t rho = (int64_t)it.tile * a.rows + rt * 16 + m16;
-    if (rho >= (int64_t)rows.n * a.group) return;
-    const int t = (int)(rho / a.group), h = head * a.group + (int)(rho - (int64_t)t * a.group), size = a.cache.size;
+    shared[wave][lane] = o;
+    totals[wave][lane] = total;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < kWaves; ++w) o += shared[w][lane], total += totals[w][lane];
+    const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, slot.seq);
+    const unsigned rho = slot.tile * a.rows + rt * 16 + m16;
+    if (rho >= (unsigned)(rows.n * a.group)) return;
+    const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group), size = a.cache.size;
     Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
-    const float inverse = 1.f / total;   // (a sequence of several chunks: rows of positions below 0 are those that see nothing)
-    const bool sees = min(max(a.seqs.lens[it.seq], 0), kMaxPosition) - rows.n + t >= 0;
+    const bool sees = min(max(a.seqs.lens[slot.seq], 0), kMaxPosition) - rows.n + t >= 0;
+    const float inverse = 1.f / total;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(sees ? o[e] * inverse : 0.f);
@@ -448,7 +474,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64) k_kv_
 // How a call is cut.
 struct Cut {
     int row_tiles, wanted;
-    int64_t items;   // workgroups of a head, at most
+    int64_t tiles, items;   // of a head, at most
     size_t states, total;
 };
 Cut cut_of(const tst_kv_cache_t *c, const tst_sequences_t *s, int q_heads)
@@ -457,9 +483,9 @@ Cut cut_of(const tst_kv_cache_t *c, const tst_sequences_t *s, int q_heads)
     const int group = q_heads / c->heads, row = kv_row(c->head_size);
     const int64_t rows = (int64_t)s->tokens * group;   // of a key head
     k.row_tiles = s->sequences && rows > (int64_t)s->sequences * 16 && row <= 128 ? 2 : 1;
-    const int64_t tiles = rows / (16 * k.row_tiles) + s->sequences;
+    const int64_t tiles = k.tiles = rows / (16 * k.row_tiles) + s->sequences;
     const int64_t most = ((int64_t)s->columns * c->page_tokens + kUnit) / kUnit;   // units of the longest sequence there can be
-    const int wanted = blocks_of(2 * compute_units(), c->heads);
+    const int wanted = blocks_of(V_WANT * compute_units(), c->heads);
     k.wanted = s->sequences <= 1024 && tiles <= 16 * (int64_t)wanted && most > kLeastChunk ? wanted : 0;
     k.items = tiles + k.wanted;
     const size_t states = (size_t)k.items * c->heads * k.row_tiles * 16;
@@ -504,9 +530,9 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
             else tst::k_kv_attention<TYPE, ROW, MOST><<<grid, 64 * tst::kWaves, 0, st>>>(a);
             if (cut.wanted) {
                 if (hipError_t e = hipGetLastError()) return e;
-                const dim3 joins((unsigned)cut.items, cache->heads, ROW / 16 * cut.row_tiles);
-                if (cut.row_tiles == 1) tst::k_kv_join<TYPE, ROW, 1><<<joins, 64, 0, st>>>(a);
-                else tst::k_kv_join<TYPE, ROW, MOST><<<joins, 64, 0, st>>>(a);
+                const dim3 joins((unsigned)cut.tiles, cache->heads, ROW / 16 * cut.row_tiles);
+                if (cut.row_tiles == 1) tst::k_kv_join<TYPE, ROW, 1><<<joins, 64 * tst::kWaves, 0, st>>>(a);
+                else tst::k_kv_join<TYPE, ROW, MOST><<<joins, 64 * tst::kWaves, 0, st>>>(a);
             }
             return hipGetLastError();
         });
