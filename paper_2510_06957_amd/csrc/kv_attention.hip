@@ -15,6 +15,7 @@
 
 #ifndef V_WANT
 #define V_WANT 2
+#define V_OCC 2
 #endif
 namespace tst {
 namespace {
@@ -35,6 +36,7 @@ struct KvArgs {
     int q_heads, group, rows;   // query heads of a key head; rows of a tile: 16 for each row tile
     int wanted;                 // chunks of a head that are wanted in all; 0: no sequence is cut
     float scale;
+    bool wide;                  // rows of Q on 16-byte borders, of a multiple of 8 entries
     void *y;
     f32x4 *sums;                // [heads][items][tiles][64 lanes]
     float2 *states;             // [heads][items][16 x row tiles]: largest logit, sum of weights
@@ -51,11 +53,28 @@ __device__ __forceinline__ int tiles_of(const KvArgs &a, int i)
     return (span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + a.rows - 1) / a.rows;   // (tokens * query heads <= 2^27)
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v)
+// Sums of the values of lanes up to this one; in lane 63 that of all.
+__device__ __forceinline__ int64_t wave_scan(int64_t v)
 {
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    auto step = [&](auto control, auto rows) {
+        const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, decltype(rows)::value, 0xf, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), decltype(control)::value, decltype(rows)::value, 0xf, false);
+        v += (int64_t)((uint64_t)(unsigned)hi << 32 | lo);
+    };
+    typedef std::integral_constant<int, 0xf> All;
+    step(std::integral_constant<int, 0x111>{}, All{});   // row_shr 1
+    step(std::integral_constant<int, 0x112>{}, All{});
+    step(std::integral_constant<int, 0x114>{}, All{});
+    step(std::integral_constant<int, 0x118>{}, All{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast 31
     return v;
 }
+__device__ __forceinline__ int64_t lane_of(int64_t v, int lane)
+{
+    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
+}
+__device__ __forceinline__ int64_t wave_sum(int64_t v) { return lane_of(wave_scan(v), 63); }
 
 // The length of chunks, in units of 64 tokens.
 __device__ __forceinline__ int chunk_length(const KvArgs &a)
@@ -82,19 +101,15 @@ __device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t a
         const int i = base + lane;
         const int chunks = i < a.seqs.count ? chunks_of(a, i, length) : 1;
         const int64_t mine = i < a.seqs.count ? (int64_t)tiles_of(a, i) * chunks : 0;
-        int64_t upto = mine;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
-        }
+        const int64_t upto = wave_scan(mine);
         const unsigned long long behind = __ballot(before + upto > at);
         if (behind) {
             const int l = __ffsll(behind) - 1;
-            const int n = __shfl(chunks, l);
-            const int rest = (int)(at - (before + __shfl(upto, l) - __shfl(mine, l)));
+            const int n = __builtin_amdgcn_readlane(chunks, l);
+            const int rest = (int)(at - (before + lane_of(upto, l) - lane_of(mine, l)));
             return Item{base + l, rest / n, rest % n, n};
         }
-        before += __shfl(upto, 63);
+        before += lane_of(upto, 63);
     }
     return Item{-1, 0, 0, 0};
 }
@@ -147,6 +162,9 @@ template <int TYPE, int ROW, int RT> struct Shape {
     static constexpr int kSteps = ROW / 32;      // of 32 channels
     static constexpr int kWide = ROW / 64;       // loads of 16 bytes of a lane in a row of keys; 8 more bytes where ROW % 64 = 32
     static constexpr int kTiles = ROW / 16;      // of 16 channels
+    // Weights are 2^kShift times those relative to the largest logit and scale of values that all was last scaled by; what comes later may pass them by
+    // 2^kSlack and kScaleSlack times before all is scaled anew.  fp16 holds 2^15.  fp32 has no room for that: weights down to 2^-29 of the largest keep their bits.
+    static constexpr float kShift = TYPE == TST_F32 ? 32768.f : 128.f, kSlack = TYPE == TST_F32 ? 0.f : 6.f, kScaleSlack = TYPE == TST_F32 ? 1.f : 4.f;
 };
 // The channel that entry i of step j stands for in a lane of quarter g: 16 bytes of a row are two steps.
 template <int ROW> __device__ __forceinline__ int channel(int j, int g) { return j < ROW / 64 * 2 ? j / 2 * 64 + g * 16 + j % 2 * 8 : j / 2 * 64 + g * 8; }
@@ -154,8 +172,21 @@ template <int ROW> __device__ __forceinline__ int channel(int j, int g) { return
 template <int TYPE, int ROW, int RT> struct Keys {
     u32x4 wide[4][Shape<TYPE, ROW, RT>::kWide];
     u32x2 rest[4];
-    float k_scale, v_scale;
 };
+// The entry of the page table that a lane's block goes by, on its way.
+struct Page {
+    int entry;
+    bool in_table;
+};
+
+// The largest of the four quarters' values of a lane's number (mod 16); a NaN does not count.
+__device__ __forceinline__ float quarters_max(float v)
+{
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 // Adds what another wavefront or chunk has, relative to largest logits of its own.
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
@@ -189,7 +220,7 @@ template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(
     }
 }
 
-template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves) k_kv_attention(KvArgs a)
+template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves, ROW * RT <= 128 && TYPE != TST_F32 ? V_OCC : 1) k_kv_attention(KvArgs a)
 {
     typedef Shape<TYPE, ROW, RT> S;
     typedef typename Entry<TYPE>::bits Bits;
@@ -231,13 +262,24 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         float x[S::kSteps][8];
         unsigned most = 0;
 #pragma unroll
-        for (int j = 0; j < S::kSteps; ++j)
+        for (int j = 0; j < S::kSteps; ++j) {
+            const int d = channel<ROW>(j, g);
+            if (a.wide) {
+                union {
+                    u32x4 v[sizeof(Bits) / 2];
+                    Bits e[8];
+                } raw;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int d = channel<ROW>(j, g) + e;
-                x[j][e] = there && d < a.cache.size ? Entry<TYPE>::get(row[d]) : 0.f;
-                most = max(most, __float_as_uint(x[j][e]) & 0x7fffffffu);
+                for (int i = 0; i < (int)sizeof(Bits) / 2; ++i) raw.v[i] = d < a.cache.size ? reinterpret_cast<const u32x4 *>(row + d)[i] : u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = there ? Entry<TYPE>::get(raw.e[e]) : 0.f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = there && d + e < a.cache.size ? Entry<TYPE>::get(row[d + e]) : 0.f;
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[j][e]) & 0x7fffffffu);
+        }
         most = max(most, (unsigned)__shfl_xor((int)most, 16));
         most = max(most, (unsigned)__shfl_xor((int)most, 32));
         const bool finite = most < 0x7f800000u;
@@ -257,7 +299,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     least = uniform(least);   // all rows see the keys below this
 
     f32x4 o[RT][S::kTiles];
-    float most[RT], sum[RT], reference = kLeastScale;
+    float most[RT], sum[RT], reference = kLeastScale;   // of logits and of scales of values: what weights are relative to
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         most[rt] = -INFINITY, sum[rt] = 0.f;
@@ -265,112 +307,137 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // pages of the blocks whose keys and whose values this lane reads, -1: none; behind the sequence's end: any
-    auto page_at = [&](int block) { return block * kKvBlock < len ? page_of(a.cache, a.seqs, seq, block) : -2; };
+    // Loads do not depend on the lane or on what was loaded, so that each is waited for by itself: behind the last unit that one again, in place of pages that are none
+    // page 0, whose scale becomes a NaN then (0 behind the sequence's end).
+    const int32_t *table = a.seqs.table + seq * a.seqs.stride;
+    const int page_blocks = a.cache.page_shift - 4, last = max(end - 1, 0);
+    auto load_page = [&](int block) {
+        const int column = block >> page_blocks;
+        return Page{table[min(column, a.seqs.columns - 1)], column < a.seqs.columns};
+    };
+    auto is_page = [&](const Page &p) { return p.in_table && (unsigned)p.entry < (unsigned)a.cache.pages; };
+    auto lies = [&](const Page &p, int block) { return block_at(a.cache, is_page(p) ? p.entry : 0, head, block); };
+    auto scale_of = [&](float loaded, const Page &p, int block) { return block * kKvBlock >= len ? 0.f : is_page(p) ? loaded : kNan; };
     Keys<TYPE, ROW, RT> keys;
-    auto load_keys = [&](int u, int k_page, int v_page) {
+    auto load_keys = [&](int u, const Page &page) {
         const int block = 4 * u + m16 / 4;
-        const int8_t *at = a.cache.k + (block_at(a.cache, max(k_page, 0), head, block) * kKvBlock + m16 % 4) * ROW + g * 16;
+        const int8_t *at = a.cache.k + (lies(page, block) * kKvBlock + m16 % 4) * ROW + g * 16;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int w = 0; w < S::kWide; ++w) keys.wide[t][w] = *reinterpret_cast<const u32x4 *>(at + 4 * t * ROW + 64 * w);
             if constexpr (ROW % 64 != 0) keys.rest[t] = *reinterpret_cast<const u32x2 *>(at + 4 * t * ROW + 64 * S::kWide - g * 8);
         }
-        const int64_t mine = block_at(a.cache, max(v_page, 0), head, 4 * u + g);
-        keys.k_scale = v_page >= 0 ? a.cache.k_scale[mine] : v_page == -1 ? kNan : 0.f;
-        keys.v_scale = v_page >= 0 ? a.cache.v_scale[mine] : v_page == -1 ? kNan : 0.f;
     };
 
+    // The unit at hand and the next: its keys' page, its values' page, its scales; pages of the one behind.
     int u = begin + wave;
-    int k_page = 0, v_page = 0;
     if (u < end) {
-        k_page = page_at(4 * u + m16 / 4), v_page = page_at(4 * u + g);
-        load_keys(u, k_page, v_page);
-    }
-    for (; u < end; u += kWaves) {
-        const int next = u + kWaves;
-        int k_next = 0, v_next = 0;
-        if (next < end) k_next = page_at(4 * next + m16 / 4), v_next = page_at(4 * next + g);
-        u32x4 values[S::kTiles];
-        const int8_t *v_at = a.cache.v + (block_at(a.cache, max(v_page, 0), head, 4 * u + g) * ROW + m16) * kKvBlock;
+        Page k_page = load_page(4 * u + m16 / 4), v_page = load_page(4 * u + g);
+        int next = min(u + kWaves, last);
+        Page k_next = load_page(4 * next + m16 / 4), v_next = load_page(4 * next + g);
+        load_keys(u, k_page);
+        int64_t v_place = lies(v_page, 4 * u + g);
+        float k_loaded = a.cache.k_scale[v_place], v_loaded = a.cache.v_scale[v_place];
+        for (; u < end; u += kWaves) {
+            u32x4 values[S::kTiles];
+            const int8_t *v_at = a.cache.v + (v_place * ROW + m16) * kKvBlock;
 #pragma unroll
-        for (int dt = 0; dt < S::kTiles; ++dt) values[dt] = *reinterpret_cast<const u32x4 *>(v_at + 16 * dt * kKvBlock);
+            for (int dt = 0; dt < S::kTiles; ++dt) values[dt] = *reinterpret_cast<const u32x4 *>(v_at + 16 * dt * kKvBlock);
+            __builtin_amdgcn_sched_barrier(0);   // or the compiler moves the loads behind the work that hides them
 
-        f32x4 z[RT][4];
+            f32x4 z[RT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < 4; ++t) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) z[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int rt = 0; rt < RT; ++rt) z[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < S::kSteps; ++j) {
-                const f16x8 k = j < 2 * S::kWide ? widen8(keys.wide[t][j / 2][j % 2 * 2], keys.wide[t][j / 2][j % 2 * 2 + 1]) : widen8(keys.rest[t][0], keys.rest[t][1]);
+                for (int j = 0; j < S::kSteps; ++j) {
+                    const f16x8 k = j < 2 * S::kWide ? widen8(keys.wide[t][j / 2][j % 2 * 2], keys.wide[t][j / 2][j % 2 * 2 + 1]) : widen8(keys.rest[t][0], keys.rest[t][1]);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
+                    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int p = 0; p < S::kPlanes; ++p) z[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][p][j], z[rt][t], 0, 0, 0);
+                        for (int p = 0; p < S::kPlanes; ++p) z[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[rt][p][j], z[rt][t], 0, 0, 0);
+                }
             }
-        }
-        const float k_scale = keys.k_scale, v_scale = keys.v_scale;
-        if (next < end) load_keys(next, k_next, v_next);
+            const float k_scale = scale_of(k_loaded, v_page, 4 * u + g), v_scale = scale_of(v_loaded, v_page, 4 * u + g);
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(next, k_next);
+            v_place = lies(v_next, 4 * next + g);
+            k_loaded = a.cache.k_scale[v_place], v_loaded = a.cache.v_scale[v_place];
+            v_page = v_next;
+            next = min(next + kWaves, last);
+            k_next = load_page(4 * next + m16 / 4), v_next = load_page(4 * next + g);
+            __builtin_amdgcn_sched_barrier(0);
 
-        const bool cut = (u + 1) * kUnit > least;
-        float largest = reference;
-        largest = fmaxf(largest, v_scale);
-        largest = fmaxf(largest, __shfl_xor(largest, 16));
-        largest = fmaxf(largest, __shfl_xor(largest, 32));
-        const float part = reference / largest, v_part = v_scale / largest * 32768.f;
-        reference = largest;
-        f16x8 w[RT][S::kPlanes][2];
+            const bool cut = (u + 1) * kUnit > least;
+            bool anew = v_scale > reference * S::kScaleSlack;
+            float top[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const float f = factor[rt] * k_scale;
-            float top = -INFINITY;
+            for (int rt = 0; rt < RT; ++rt) {
+                const float f = factor[rt] * k_scale;
+                top[rt] = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = z[rt][t][e] * f;
-                    if (cut) v = u * kUnit + g * kKvBlock + 4 * t + e < limit[rt] ? v : -INFINITY;
-                    z[rt][t][e] = v;
-                    top = fmaxf(top, v);
+                    for (int e = 0; e < 4; ++e) z[rt][t][e] *= f;
+                if (cut) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (u * kUnit + g * kKvBlock + 4 * t + e >= limit[rt]) z[rt][t][e] = -INFINITY;
                 }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(most[rt], top), base = now == -INFINITY ? 0.f : now;
-            const float keep = __builtin_amdgcn_exp2f(most[rt] - base) ;
-            most[rt] = now;
-            float s = 0.f;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(z[rt][t][e] - base);
-                    s += p;
-                    float x = p * v_part;
-                    if (cut) x = z[rt][t][e] == -INFINITY ? 0.f : x;
-                    const _Float16 hi = (_Float16)x;
-                    w[rt][0][t / 2][t % 2 * 4 + e] = hi;
-                    if constexpr (S::kPlanes == 2) w[rt][1][t / 2][t % 2 * 4 + e] = (_Float16)(x - (float)hi);
-                }
-            sum[rt] = sum[rt] * keep + s;
-            const float times = keep * part;
-            if (__any(times != 1.f)) {
-#pragma unroll
-                for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;
+                    for (int e = 0; e < 4; ++e) top[rt] = fmaxf(top[rt], z[rt][t][e]);
+                anew |= top[rt] > most[rt] + S::kSlack;
             }
+            if (__any(anew)) {
+                const float largest = fmaxf(reference, quarters_max(v_scale)), part = reference / largest;
+                reference = largest;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float now = fmaxf(most[rt], quarters_max(top[rt])), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most[rt] - now);
+                    most[rt] = now;
+                    sum[rt] *= keep;
+                    const float times = keep * part;
+#pragma unroll
+                    for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;
+                }
+            }
+            const float v_part = v_scale / reference * S::kShift;
+            f16x8 w[RT][S::kPlanes][2];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float base = most[rt] == -INFINITY ? 0.f : most[rt];
+                float s = 0.f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(z[rt][t][e] - base);
+                        s += p;
+                        float x = p * v_part;
+                        if (cut) x = z[rt][t][e] == -INFINITY ? 0.f : x;
+                        const _Float16 hi = (_Float16)x;
+                        w[rt][0][t / 2][t % 2 * 4 + e] = hi;
+                        if constexpr (S::kPlanes == 2) w[rt][1][t / 2][t % 2 * 4 + e] = (_Float16)(x - (float)hi);
+                    }
+                sum[rt] += s;
+            }
+#pragma unroll
+            for (int dt = 0; dt < S::kTiles; ++dt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const f16x8 v = widen8(values[dt][2 * j], values[dt][2 * j + 1]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int p = 0; p < S::kPlanes; ++p) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][p][j], o[rt][dt], 0, 0, 0);
+                }
         }
-#pragma unroll
-        for (int dt = 0; dt < S::kTiles; ++dt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const f16x8 v = widen8(values[dt][2 * j], values[dt][2 * j + 1]);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int p = 0; p < S::kPlanes; ++p) o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][p][j], o[rt][dt], 0, 0, 0);
-            }
-        k_page = k_next, v_page = v_next;
     }
 
     // the wavefronts' sums: relative to the largest logit of all, then two and two
@@ -389,7 +456,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         for (int w = 0; w < kWaves; ++w) all[rt] = fmaxf(all[rt], states[w][rt][m16].x);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) total[rt] += states[w][rt][m16].y * weight_of(states[w][rt][m16].x, all[rt]);
-        const float times = weight_of(most[rt], all[rt]) * reference * (1.f / 32768.f);
+        const float times = weight_of(most[rt], all[rt]) * reference * (1.f / S::kShift);
 #pragma unroll
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = times == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][dt] * times;
     }
@@ -519,8 +586,10 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
     if (need && (!workspace || workspace_bytes < need)) return TSTGEMM_EWORKSPACE;
     if (need && !tst::aligned(workspace, 256)) return TSTGEMM_EINVAL;
     const tst::Cut cut = tst::cut_of(cache, sequences, q_heads);
-    tst::KvArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(Q), q_heads, q_heads / cache->heads, 16 * cut.row_tiles, cut.wanted, scale, Y,
+    tst::KvArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(Q), q_heads, q_heads / cache->heads, 16 * cut.row_tiles, cut.wanted, scale, false, Y,
                   static_cast<tst::f32x4 *>(workspace), reinterpret_cast<float2 *>(static_cast<char *>(workspace) + cut.states), (int)cut.items};
+    const int64_t per = 16 / (int64_t)tst::type_bytes(type);
+    a.wide = tst::aligned(Q->data, 16) && Q->token_stride % per == 0 && Q->head_stride % per == 0 && cache->head_size % 8 == 0;
     return tst::status(tst::for_type(type, [&](auto t) {
         return tst::for_row(cache->head_size, [&](auto r) {
             constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value, MOST = ROW <= 128 ? 2 : 1;
