@@ -13,10 +13,6 @@
 // each whatever the batch is; the host knows how many there are at most.  Chunks of one tile of rows are joined by k_join.
 #include "attention_internal.h"
 
-#ifndef V_WANT
-#define V_WANT 2
-#define V_OCC 2
-#endif
 namespace tst {
 namespace {
 
@@ -24,7 +20,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4, kUnit = 64;   // tokens of a wavefront at a time
-constexpr int kLeastChunk = kWaves;     // units
 constexpr float kNan = __builtin_nanf("");
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLeastScale = 1e-36f;   // of values, as the reference that weights are relative to
@@ -33,8 +28,8 @@ struct KvArgs {
     Cache cache;
     Sequences seqs;
     Rows q;
-    int q_heads, group, rows;   // query heads of a key head; rows of a tile: 16 for each row tile
-    int wanted;                 // chunks of a head that are wanted in all; 0: no sequence is cut
+    int q_heads, group;         // query heads of a key head
+    int parts;                  // chunks of a head that its sequences are cut into, but for their ends; 0: no sequence is cut
     float scale;
     bool wide;                  // rows of Q on 16-byte borders, of a multiple of 8 entries
     void *y;
@@ -48,9 +43,9 @@ __device__ __forceinline__ int units_of(const KvArgs &a, int i)
     const int most = a.seqs.columns << a.cache.page_shift;   // a length behind the table's end meets one block that is not there
     return (min(max(a.seqs.lens[i], 0), most + 1) + kUnit - 1) / kUnit;
 }
-__device__ __forceinline__ int tiles_of(const KvArgs &a, int i)
+template <int ROWS> __device__ __forceinline__ int tiles_of(const KvArgs &a, int i)
 {
-    return (span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + a.rows - 1) / a.rows;   // (tokens * query heads <= 2^27)
+    return (span_of(a.seqs.offsets, a.seqs.tokens, i).n * a.group + ROWS - 1) / ROWS;   // (tokens * query heads <= 2^27)
 }
 
 // Sums of the values of lanes up to this one; in lane 63 that of all.
@@ -76,47 +71,46 @@ __device__ __forceinline__ int64_t lane_of(int64_t v, int lane)
 }
 __device__ __forceinline__ int64_t wave_sum(int64_t v) { return lane_of(wave_scan(v), 63); }
 
-// The length of chunks, in units of 64 tokens.
-__device__ __forceinline__ int chunk_length(const KvArgs &a)
+// The length of chunks, in units of 64 tokens: all of them in a.parts equal ones, and up to one more for each tile.  Whole rounds of the four wavefronts.  Every wavefront
+// of the call comes to the same length, which is no shorter than that.
+template <int ROWS> __device__ __forceinline__ int chunk_length(const KvArgs &a)
 {
-    const int lane = threadIdx.x % 64;
     int64_t all = 0;
-    for (int i = lane; i < a.seqs.count; i += 64) all += (int64_t)tiles_of(a, i) * units_of(a, i);
-    all = wave_sum(all);
-    const int64_t length = (all + a.wanted - 1) / a.wanted;
-    return (int)min(max(length, (int64_t)kLeastChunk), (int64_t)1 << 30);
+    for (int i = threadIdx.x % 64; i < a.seqs.count; i += 64) all += (int64_t)tiles_of<ROWS>(a, i) * units_of(a, i);
+    const float length = (float)wave_sum(all) * (1.00001f / (float)a.parts) + 1.f;   // (a division of 64 bits takes a microsecond)
+    return ((int)fminf(length, 1 << 30) + kWaves - 1) / kWaves * kWaves;
 }
 
-__device__ __forceinline__ int chunks_of(const KvArgs &a, int i, int length) { return max((units_of(a, i) + length - 1) / length, 1); }
+__device__ __forceinline__ int chunks_of(const KvArgs &a, int i, int length) { return max((int)((unsigned)(units_of(a, i) + length - 1) / (unsigned)length), 1); }
 
 // Item `at`: sequences in order, a sequence's tiles in order, a tile's chunks in order.  seq -1: there are fewer.
 struct Item {
     int seq, tile, chunk, chunks;   // chunks of the tile
 };
-__device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t at)
+template <int ROWS> __device__ __forceinline__ Item find_item(const KvArgs &a, int length, int64_t at)
 {
     const int lane = threadIdx.x % 64;
     int64_t before = 0;
     for (int base = 0; base < a.seqs.count; base += 64) {
         const int i = base + lane;
         const int chunks = i < a.seqs.count ? chunks_of(a, i, length) : 1;
-        const int64_t mine = i < a.seqs.count ? (int64_t)tiles_of(a, i) * chunks : 0;
+        const int64_t mine = i < a.seqs.count ? (int64_t)tiles_of<ROWS>(a, i) * chunks : 0;
         const int64_t upto = wave_scan(mine);
         const unsigned long long behind = __ballot(before + upto > at);
         if (behind) {
             const int l = __ffsll(behind) - 1;
             const int n = __builtin_amdgcn_readlane(chunks, l);
             const int rest = (int)(at - (before + lane_of(upto, l) - lane_of(mine, l)));
-            return Item{base + l, rest / n, rest % n, n};
+            return Item{base + l, (int)((unsigned)rest / (unsigned)n), (int)((unsigned)rest % (unsigned)n), n};
         }
         before += lane_of(upto, 63);
     }
     return Item{-1, 0, 0, 0};
 }
-__device__ __forceinline__ int64_t items_before(const KvArgs &a, int seq, int length)
+template <int ROWS> __device__ __forceinline__ int64_t items_before(const KvArgs &a, int seq, int length)
 {
     int64_t n = 0;
-    for (int i = threadIdx.x % 64; i < seq; i += 64) n += (int64_t)tiles_of(a, i) * chunks_of(a, i, length);
+    for (int i = threadIdx.x % 64; i < seq; i += 64) n += (int64_t)tiles_of<ROWS>(a, i) * chunks_of(a, i, length);
     return wave_sum(n);
 }
 
@@ -124,10 +118,10 @@ __device__ __forceinline__ int64_t items_before(const KvArgs &a, int seq, int le
 struct Slot {
     int seq, tile;
 };
-__device__ __forceinline__ Slot find_slot(const KvArgs &a, int at)
+template <int ROWS> __device__ __forceinline__ Slot find_slot(const KvArgs &a, int at)
 {
     const int lane = threadIdx.x % 64;
-    auto base = [&](int i) { return (a.seqs.offsets ? min(max(a.seqs.offsets[i], 0), a.seqs.tokens) : i) * a.group / a.rows + i; };
+    auto base = [&](int i) { return (a.seqs.offsets ? min(max(a.seqs.offsets[i], 0), a.seqs.tokens) : i) * a.group / ROWS + i; };
     int lo = 0, n = a.seqs.count;
     while (n > 1) {
         const int step = (n + 63) / 64, i = lo + lane * step;
@@ -138,7 +132,7 @@ __device__ __forceinline__ Slot find_slot(const KvArgs &a, int at)
     }
     lo = uniform(lo);
     const int tile = uniform(at - base(lo));
-    return Slot{lo, tile >= 0 && tile < tiles_of(a, lo) ? tile : -1};
+    return Slot{lo, tile >= 0 && tile < tiles_of<ROWS>(a, lo) ? tile : -1};
 }
 
 // Four codes as fp16: 1024 + (code + 128) by its bits, less 1152.
@@ -197,7 +191,7 @@ template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(
     const int lane = threadIdx.x % 64, g = lane / 16, size = a.cache.size;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const unsigned rho = tile * a.rows + rt * 16 + lane % 16;
+        const unsigned rho = tile * (16 * RT) + rt * 16 + lane % 16;
         if (rho >= (unsigned)(rows.n * a.group)) continue;
         const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group);
         Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
@@ -220,7 +214,7 @@ template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(
     }
 }
 
-template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves, ROW * RT <= 128 && TYPE != TST_F32 ? V_OCC : 1) k_kv_attention(KvArgs a)
+template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves, ROW * RT <= 128 && TYPE != TST_F32 ? 2 : 1) k_kv_attention(KvArgs a)
 {
     typedef Shape<TYPE, ROW, RT> S;
     typedef typename Entry<TYPE>::bits Bits;
@@ -229,14 +223,14 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y;
     Item it;
     int begin = 0, end = 0;
-    if (a.wanted) {
-        const int length = uniform(chunk_length(a));
-        it = find_item(a, length, blockIdx.x);
+    if (a.parts) {
+        const int length = uniform(chunk_length<16 * RT>(a));
+        it = find_item<16 * RT>(a, length, blockIdx.x);
         if (it.seq < 0) return;
         begin = it.chunk * length;
         end = min(begin + length, units_of(a, it.seq));
     } else {
-        const Slot slot = find_slot(a, blockIdx.x);
+        const Slot slot = find_slot<16 * RT>(a, blockIdx.x);
         if (slot.tile < 0) return;
         it = Item{slot.seq, slot.tile, 0, 1};
         end = units_of(a, slot.seq);
@@ -253,7 +247,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     int least = kMaxPosition;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const unsigned rho = tile * a.rows + rt * 16 + m16;
+        const unsigned rho = tile * (16 * RT) + rt * 16 + m16;
         const bool there = rho < (unsigned)(rows.n * a.group);
         const int t = there ? rho / (unsigned)a.group : 0, h = head * a.group + (there ? (int)(rho - t * a.group) : 0);
         const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(rows.first + t) * a.q.token + h * a.q.head;
@@ -489,58 +483,66 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     }
 }
 
-// Joins the chunks of a tile: a workgroup for 16 channels of 16 rows, whose wavefronts share the chunks.
+// Joins the chunks of a tile, 16 channels of 16 rows at a time: where there are few tiles, each such part is a workgroup's, whose wavefronts share the chunks, else a
+// wavefront's, one after another.
 template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves) k_kv_join(KvArgs a)
 {
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int kTiles = ROW / 16;
     __shared__ f32x4 shared[kWaves][64];
     __shared__ float totals[kWaves][64];
-    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y, rt = blockIdx.z / kTiles, dt = blockIdx.z % kTiles;
-    const Slot slot = find_slot(a, blockIdx.x);
+    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y;
+    const Slot slot = find_slot<16 * RT>(a, blockIdx.x);
     if (slot.tile < 0) return;
-    const int length = uniform(chunk_length(a)), chunks = chunks_of(a, slot.seq, length);
+    const int length = uniform(chunk_length<16 * RT>(a)), chunks = chunks_of(a, slot.seq, length);
     if (chunks == 1) return;
-    const int64_t first = items_before(a, slot.seq, length) + (int64_t)slot.tile * chunks;
+    const int64_t first = items_before<16 * RT>(a, slot.seq, length) + (int64_t)slot.tile * chunks;
     const int n = (int)min((int64_t)chunks, a.items - first);   // (fewer where offsets do not ascend)
     const int64_t place = (int64_t)head * a.items + first;
-    const float2 *states = a.states + place * (RT * 16) + rt * 16 + m16;
-    const f32x4 *sums = a.sums + (place * (RT * kTiles) + rt * kTiles + dt) * 64 + lane;
-    float all = -INFINITY;
-#pragma unroll 4
-    for (int c = g; c < n; c += 4) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
-    all = fmaxf(all, __shfl_xor(all, 16));
-    all = fmaxf(all, __shfl_xor(all, 32));
-    float total = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int c = wave; c < n; c += kWaves) {
-        const float2 s = states[(int64_t)c * (RT * 16)];
-        const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
-        const float w = weight_of(s.x, all);
-        total += w * s.y;
-        o += w != 0.f ? w * v : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    shared[wave][lane] = o;
-    totals[wave][lane] = total;
-    __syncthreads();
-    if (wave != 0) return;
-    for (int w = 1; w < kWaves; ++w) o += shared[w][lane], total += totals[w][lane];
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, slot.seq);
-    const unsigned rho = slot.tile * a.rows + rt * 16 + m16;
-    if (rho >= (unsigned)(rows.n * a.group)) return;
-    const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group), size = a.cache.size;
-    Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
-    const bool sees = min(max(a.seqs.lens[slot.seq], 0), kMaxPosition) - rows.n + t >= 0;
-    const float inverse = 1.f / total;
+    const int sees_from = rows.n - min(max(a.seqs.lens[slot.seq], 0), kMaxPosition), size = a.cache.size;   // tokens of the call below it see nothing
+    const bool share = gridDim.z > 1;
+    for (int part = share ? blockIdx.z : wave; part < RT * kTiles; part += share ? RT * kTiles : kWaves) {
+        const int rt = part / kTiles, dt = part % kTiles;
+        const float2 *states = a.states + place * (RT * 16) + rt * 16 + m16;
+        const f32x4 *sums = a.sums + (place * (RT * kTiles) + part) * 64 + lane;
+        float all = -INFINITY;
+#pragma unroll 4
+        for (int c = g; c < n; c += 4) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
+        all = quarters_max(all);
+        float total = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int c = share ? wave : 0; c < n; c += share ? kWaves : 1) {
+            const float2 s = states[(int64_t)c * (RT * 16)];
+            const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
+            const float w = weight_of(s.x, all);
+            total += w * s.y;
+            o += w != 0.f ? w * v : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (share) {
+            shared[wave][lane] = o;
+            totals[wave][lane] = total;
+            __syncthreads();
+            if (wave != 0) return;
+            for (int w = 1; w < kWaves; ++w) o += shared[w][lane], total += totals[w][lane];
+        }
+        const unsigned rho = slot.tile * (16 * RT) + rt * 16 + m16;
+        if (rho >= (unsigned)(rows.n * a.group)) continue;
+        const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group);
+        Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
+        const float inverse = 1.f / total;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(sees ? o[e] * inverse : 0.f);
+        for (int e = 0; e < 4; ++e)
+            if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(t >= sees_from ? o[e] * inverse : 0.f);
+    }
 }
 
-// How a call is cut.
+// How a call is cut: the sequences of a head into about as many chunks as the card holds workgroups of it, so that all have as much to do, where these are more than twice
+// the tiles; else into three times as many, since the ends of sequences make them uneven and a second and third turn fill what the first leaves.  (us, once and three times as
+// many: 1 x 131072 tokens 61.6 and 71.5, 64 sequences of up to 8192 105 and 99.)
 struct Cut {
-    int row_tiles, wanted;
+    int row_tiles, parts;
     int64_t tiles, items;   // of a head, at most
     size_t states, total;
 };
@@ -550,14 +552,14 @@ Cut cut_of(const tst_kv_cache_t *c, const tst_sequences_t *s, int q_heads)
     const int group = q_heads / c->heads, row = kv_row(c->head_size);
     const int64_t rows = (int64_t)s->tokens * group;   // of a key head
     k.row_tiles = s->sequences && rows > (int64_t)s->sequences * 16 && row <= 128 ? 2 : 1;
-    const int64_t tiles = k.tiles = rows / (16 * k.row_tiles) + s->sequences;
-    const int64_t most = ((int64_t)s->columns * c->page_tokens + kUnit) / kUnit;   // units of the longest sequence there can be
-    const int wanted = blocks_of(V_WANT * compute_units(), c->heads);
-    k.wanted = s->sequences <= 1024 && tiles <= 16 * (int64_t)wanted && most > kLeastChunk ? wanted : 0;
-    k.items = tiles + k.wanted;
+    k.tiles = rows / (16 * k.row_tiles) + s->sequences;
+    const int slots = blocks_of((row * k.row_tiles <= 128 ? 2 : 1) * compute_units(), c->heads);   // by the kernels' registers
+    const int64_t longest = ((int64_t)s->columns * c->page_tokens + kUnit) / kUnit;   // units that a sequence can have
+    if (s->sequences <= 1024 && k.tiles <= 16 * (int64_t)slots && longest > kWaves) k.parts = 2 * k.tiles > slots ? 3 * slots : slots;
+    k.items = k.tiles + k.parts;
     const size_t states = (size_t)k.items * c->heads * k.row_tiles * 16;
-    k.states = k.wanted ? round256(states * row * sizeof(float)) : 0;
-    k.total = k.wanted ? k.states + round256(states * sizeof(float2)) : 0;
+    k.states = k.parts ? round256(states * row * sizeof(float)) : 0;
+    k.total = k.parts ? k.states + round256(states * sizeof(float2)) : 0;
     return k;
 }
 
@@ -586,7 +588,7 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
     if (need && (!workspace || workspace_bytes < need)) return TSTGEMM_EWORKSPACE;
     if (need && !tst::aligned(workspace, 256)) return TSTGEMM_EINVAL;
     const tst::Cut cut = tst::cut_of(cache, sequences, q_heads);
-    tst::KvArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(Q), q_heads, q_heads / cache->heads, 16 * cut.row_tiles, cut.wanted, scale, false, Y,
+    tst::KvArgs a{tst::cache_of(cache), tst::sequences_of(sequences), tst::rows_of(Q), q_heads, q_heads / cache->heads, cut.parts, scale, false, Y,
                   static_cast<tst::f32x4 *>(workspace), reinterpret_cast<float2 *>(static_cast<char *>(workspace) + cut.states), (int)cut.items};
     const int64_t per = 16 / (int64_t)tst::type_bytes(type);
     a.wide = tst::aligned(Q->data, 16) && Q->token_stride % per == 0 && Q->head_stride % per == 0 && cache->head_size % 8 == 0;
@@ -597,9 +599,9 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
             const dim3 grid((unsigned)cut.items, cache->heads);
             if (cut.row_tiles == 1) tst::k_kv_attention<TYPE, ROW, 1><<<grid, 64 * tst::kWaves, 0, st>>>(a);
             else tst::k_kv_attention<TYPE, ROW, MOST><<<grid, 64 * tst::kWaves, 0, st>>>(a);
-            if (cut.wanted) {
+            if (cut.parts) {
                 if (hipError_t e = hipGetLastError()) return e;
-                const dim3 joins((unsigned)cut.tiles, cache->heads, ROW / 16 * cut.row_tiles);
+                const dim3 joins((unsigned)cut.tiles, cache->heads, cut.tiles * cache->heads < tst::compute_units() ? ROW / 16 * cut.row_tiles : 1);
                 if (cut.row_tiles == 1) tst::k_kv_join<TYPE, ROW, 1><<<joins, 64 * tst::kWaves, 0, st>>>(a);
                 else tst::k_kv_join<TYPE, ROW, MOST><<<joins, 64 * tst::kWaves, 0, st>>>(a);
             }
