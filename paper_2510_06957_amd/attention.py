@@ -5,6 +5,7 @@ from __future__ import annotations
 import ctypes
 import math
 
+from . import binding
 from .binding import TstgemmError, _launch_stream, _load
 from .operators import _dense, _on, _result, _shared, _type, _workspace
 
@@ -20,16 +21,22 @@ _SIGNATURES = {
     "tst_attention": [_vp, _vp, _vp, _ci, _ci, _ci, _ci, _vp, _ci, _ci, _f32, _vp, _vp],
 }
 _lib = None
+_native = None   # the native half (csrc/launch_attention.cpp): calls with plain tensors that bring nothing but their operands
 
 
 def _ops():
-    global _lib
+    global _lib, _native
     if _lib is None:
         lib = _load()
         for name, args in _SIGNATURES.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, ctypes.c_int
         _lib = lib
+        if binding._launch is not None:   # built, and for this torch
+            from . import _launch as native
+            native.bind_attention(*(ctypes.cast(getattr(lib, name), _vp).value for name in (
+                "tst_kv_append", "tst_kv_read", "tst_kv_attention_workspace_bytes", "tst_kv_attention", "tst_attention")), TstgemmError, KvCache)
+            _native = native
     return _lib
 
 
@@ -148,6 +155,10 @@ def tst_kv_append(cache: KvCache, K, V, pages, lens, offsets=None, Q=None, cos=N
 
     cos, sin float32 [positions, pairs]: keys are rotated by their positions on the way, and queries Q [T, q_heads, head_size] if there are any, in halves
     (i, i + pairs) or neighbours (2 i, 2 i + 1).  Returns (Q rotated or None, K rotated if `keys` or None)."""
+    if _native is not None and stream is None:
+        done = _native.kv_append(cache, K, V, pages, lens, offsets, Q, cos, sin, interleaved, keys)
+        if done is not None:
+            return done
     import torch
     k = _heads(K, "K")
     kind, T, dev = _type(K.dtype, "K"), K.shape[0], K.get_device()
@@ -175,6 +186,10 @@ def tst_kv_append(cache: KvCache, K, V, pages, lens, offsets=None, Q=None, cos=N
 def tst_kv_read(cache: KvCache, pages, lens, tokens: int, offsets=None, dtype=None, stream=None):
     """What the codes of the last tokens of sequences stand for: (K, V), each [tokens, heads, head_size] of dtype (bfloat16 unless another is given).  offsets, lens and
     pages as in tst_kv_append."""
+    if _native is not None and stream is None:
+        done = _native.kv_read(cache, pages, lens, tokens, offsets, dtype)
+        if done is not None:
+            return done
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     kind, tokens = _type(dtype, "dtype"), int(tokens)
@@ -198,6 +213,10 @@ def _scale(scale, size):
 def tst_kv_attention(Q, cache: KvCache, pages, lens, offsets=None, scale=None, Y=None, workspace=None, stream=None):
     """Attention of new tokens, which have been appended, over the cache: Q [T, q_heads, head_size] float32, bfloat16 or float16, q_heads a multiple of the cache's heads ->
     Y of the same shape and type.  offsets, lens and pages as in tst_kv_append; scale: 1 / sqrt(head_size) unless another is given."""
+    if _native is not None and Y is None and workspace is None and stream is None:
+        done = _native.kv_attention(Q, cache, pages, lens, offsets, scale)
+        if done is not None:
+            return done
     q = _heads(Q, "Q")
     kind, (T, q_heads, size), dev = _type(Q.dtype, "Q"), Q.shape, Q.get_device()
     s = _sequences(cache, pages, lens, offsets, T)
@@ -217,6 +236,10 @@ def tst_attention(Q, K, V, offsets, scale=None, Y=None, stream=None):
     """Causal attention over whole prompts packed one behind another: Q [T, q_heads, head_size], K and V [T, heads, head_size] of one type, float32, bfloat16 or float16, q_heads a
     multiple of heads; offsets int32 [sequences + 1] on the GPU, rows offsets[i] .. offsets[i + 1] - 1 being sequence i.  Y: as Q; rows of no sequence are left as they are
     (in a Y that is made here: whatever the memory held).  scale: 1 / sqrt(head_size) unless another is given."""
+    if _native is not None and Y is None and stream is None:
+        done = _native.attention(Q, K, V, offsets, scale)
+        if done is not None:
+            return done
     import torch
     q = _heads(Q, "Q")
     kind, (T, q_heads, size), dev = _type(Q.dtype, "Q"), Q.shape, Q.get_device()

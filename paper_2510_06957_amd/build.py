@@ -53,7 +53,7 @@ def launch_command(out: pathlib.Path = LAUNCH) -> list[str]:
     for path in (home / "include", home / "include" / "torch" / "csrc" / "api" / "include",
                  pathlib.Path(hipcc()).resolve().parent.parent / "include", sysconfig.get_paths()["include"]):
         cmd += ["-isystem", str(path)]
-    cmd += [str(CSRC / "launch.cpp"), str(CSRC / "launch_ops.cpp"), f"-L{home / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10", "-o", str(out)]
+    cmd += [str(CSRC / "launch.cpp"), str(CSRC / "launch_ops.cpp"), str(CSRC / "launch_attention.cpp"), f"-L{home / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10", "-o", str(out)]
     return cmd
 
 

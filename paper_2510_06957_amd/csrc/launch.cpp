@@ -134,8 +134,9 @@ PyMODINIT_FUNC PyInit__launch()
     s_n = PyUnicode_InternFromString("N");
     s_device_index = PyUnicode_InternFromString("device_index");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    PyObject *module = launch::ops_init() ? PyModule_Create(&module_def) : nullptr;
+    PyObject *module = launch::ops_init() && launch::attention_init() ? PyModule_Create(&module_def) : nullptr;
     if (module != nullptr && PyModule_AddFunctions(module, launch::ops_methods) < 0) Py_CLEAR(module);
+    if (module != nullptr && PyModule_AddFunctions(module, launch::attention_methods) < 0) Py_CLEAR(module);
     // what it reads of a tensor is laid out as in the torch it was built for
     if (module != nullptr && PyModule_AddStringConstant(module, "torch_version", BUILT_FOR_TORCH) < 0) Py_CLEAR(module);
     return module;

@@ -1,5 +1,5 @@
-// Shared by the two halves of the Python module _launch: calls of the ternary product (launch.cpp) and of the operators around it
-// (launch_ops.cpp).
+// Shared by the parts of the Python module _launch: calls of the ternary product (launch.cpp), of the operators around it (launch_ops.cpp) and of
+// attention (launch_attention.cpp).
 #pragma once
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -35,7 +35,9 @@ struct WithoutGil {
     ~WithoutGil() { PyEval_RestoreThread(state); }
 };
 
-extern PyMethodDef ops_methods[];   // launch_ops.cpp; ends with an empty one
-bool ops_init();                    // names it looks attributes up by
+extern PyMethodDef ops_methods[];         // launch_ops.cpp; ends with an empty one
+bool ops_init();                          // names it looks attributes up by
+extern PyMethodDef attention_methods[];   // launch_attention.cpp, the same
+bool attention_init();
 
 }  // namespace launch
