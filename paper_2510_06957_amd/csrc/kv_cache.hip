@@ -1,8 +1,8 @@
 // A paged cache of keys and values in 8 bits: appending to it with the rotation by positions (tst_kv_append) and reading it back (tst_kv_read).
 //
 // A block of 16 tokens of a head is a wavefront's, keys and values apart: it finds the largest entry of the block's new tokens, and with it the
-// block's scale, before anything is rounded, and nobody else writes there.  Lane (u, j) has channels 8 u .. 8 u + 7 of tokens 4 j .. 4 j + 3, so the four
-// codes of a channel make a dword of the values' layout [channel][token].
+// block's scale, before anything is rounded, and nobody else writes there.  Of values, lane (u, j) has channels 8 u .. 8 u + 7 of tokens 4 j .. 4 j + 3, so that the
+// four codes of a channel make a dword of the layout [channel][token]; of keys and queries whose halves are rotated into one another it has 8 channels of either half.
 #include "attention_internal.h"
 
 namespace tst {
@@ -59,18 +59,26 @@ template <int TYPE, bool WIDE> __device__ __forceinline__ void store8(typename E
     }
 }
 
+// How rows are read: an entry at a time; 8 at a time, on borders; so, and rotated in halves that fill the head.
+enum Reading { kNarrow, kWide, kHalves };
+
+// Which 8 channels (kHalves: twice 8) of which tokens of a block a lane has.
+template <int HOW, int SIZES> struct Lanes {   // SIZES 1: heads of up to 128 entries, 2: 256
+    static constexpr int kUnits = HOW == kHalves ? 2 : 1, kAcross = (HOW == kHalves ? 8 : 16) * SIZES, kStep = 64 / kAcross, kPasses = kKvBlock / kStep;
+};
+
 // Channels d .. d + 7 of a row, rotated by position p: each product and each sum is rounded to fp32 (no fma), so that codes are defined bit for bit.
-template <int TYPE, bool WIDE> __device__ __forceinline__ void rotated8(const AppendArgs &a, const typename Entry<TYPE>::bits *row, int d, int p, float (&x)[8])
+template <int TYPE, int HOW> __device__ __forceinline__ void rotated8(const AppendArgs &a, const typename Entry<TYPE>::bits *row, int d, int p, float (&x)[8])
 {
 #pragma clang fp contract(off)
-    load8<TYPE, WIDE>(row, d, a.cache.size, x);
+    load8<TYPE, HOW != kNarrow>(row, d, a.cache.size, x);
     const int P = a.pairs;
     if (d >= 2 * P) return;
     const bool there = p >= 0 && p < a.positions;
     const float *cs = a.cos + (int64_t)(there ? p : 0) * P, *sn = a.sin + (int64_t)(there ? p : 0) * P;
-    if constexpr (WIDE) {   // pairs are a multiple of 8 (of 4 if they are neighbours)
+    if constexpr (HOW != kNarrow) {   // pairs are a multiple of 8 (of 4 if they are neighbours)
         if (a.interleaved) {
-            f32x4 c = *reinterpret_cast<const f32x4 *>(cs + d / 2), s = *reinterpret_cast<const f32x4 *>(sn + d / 2);
+            const f32x4 c = *reinterpret_cast<const f32x4 *>(cs + d / 2), s = *reinterpret_cast<const f32x4 *>(sn + d / 2);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x0 = x[2 * i], x1 = x[2 * i + 1];
@@ -107,6 +115,35 @@ template <int TYPE, bool WIDE> __device__ __forceinline__ void rotated8(const Ap
     }
 }
 
+// The same for halves: cos and sin of 8 pairs of a position, and both halves' channels by them.
+struct Angles {
+    f32x4 c[2], s[2];
+};
+__device__ __forceinline__ Angles angles_of(const AppendArgs &a, int pair, int p)
+{
+    const bool there = p >= 0 && p < a.positions;
+    const int64_t at = (int64_t)(there ? p : 0) * a.pairs + pair;
+    Angles g;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        g.c[i] = reinterpret_cast<const f32x4 *>(a.cos + at)[i], g.s[i] = reinterpret_cast<const f32x4 *>(a.sin + at)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g.c[i][e] = there ? g.c[i][e] : kNan, g.s[i][e] = there ? g.s[i][e] : kNan;
+    }
+    return g;
+}
+__device__ __forceinline__ void rotate(const Angles &g, float (&x)[8], float (&y)[8])
+{
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = g.c[i / 4][i % 4], s = g.s[i / 4][i % 4];
+        const float a = x[i] * c, b = y[i] * s, d = y[i] * c, e = x[i] * s;
+        x[i] = a - b;
+        y[i] = d + e;
+    }
+}
+
 __device__ __forceinline__ int code_of(float y, float inverse)
 {
     const float q = __builtin_rintf(y * inverse);
@@ -120,114 +157,188 @@ __device__ __forceinline__ unsigned rescaled(unsigned four, float share)
     return out;
 }
 
-// Tokens from .. to of a block, keys or values of a head.
-template <int TYPE, bool WIDE> __device__ __forceinline__ void append_block(const AppendArgs &a, bool values, int head, int seq, int block, int from, int to, int row0, unsigned *lds)
+// A block's scale with what comes to it.
+struct Scale {
+    float scale, inverse, share;   // share: what the codes that are there are multiplied with
+    bool finite, grown;
+};
+__device__ __forceinline__ Scale scale_of(unsigned most, float before, bool some)
+{
+    const float largest = __uint_as_float(wave_max(most));
+    Scale s;
+    s.finite = largest <= 3.402823466e38f && before == before;
+    s.scale = s.finite ? fmaxf(before, largest / 127.f) : kNan;
+    s.inverse = s.finite ? fminf(1.f / s.scale, 3.402823466e38f) : 0.f;   // scale 0: 0 * FLT_MAX = 0
+    s.grown = s.finite && s.scale > before && some;
+    s.share = s.grown ? before / s.scale : 1.f;
+    return s;
+}
+__device__ __forceinline__ unsigned four_codes(const float *x, const Scale &s)
+{
+    unsigned q = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q |= (s.finite ? (unsigned)code_of(x[e], s.inverse) & 255u : 0u) << 8 * e;
+    return q;
+}
+__device__ __forceinline__ void widest(unsigned &most, const float (&x)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[e]) & 0x7fffffffu);
+}
+
+// What a wavefront appends: tokens from .. to of a block, rows row0 .. of the call.
+struct Piece {
+    int head, seq, block, from, to, row0;
+};
+
+template <int TYPE, int HOW, int SIZES> __device__ __forceinline__ void append_keys(const AppendArgs &a, const Piece &p)
 {
     typedef typename Entry<TYPE>::bits Bits;
-    const int lane = threadIdx.x % 64, j = lane % 4, size = a.cache.size, units = (size + 7) / 8, row = kv_row(size);
-    const Rows &in = values ? a.v : a.k;
-    const Bits *data = static_cast<const Bits *>(in.data) + head * in.head;
-    float x[2][4][8];
+    typedef Lanes<HOW, SIZES> L;
+    const int lane = threadIdx.x % 64, size = a.cache.size, row = kv_row(size), count = (size + 7) / 8 / L::kUnits, k = min(lane % L::kAcross, count - 1);
+    const int page = page_of(a.cache, a.seqs, p.seq, p.block);
+    const int64_t at = block_at(a.cache, max(page, 0), p.head, p.block);
+    const Bits *data = static_cast<const Bits *>(a.k.data) + p.head * a.k.head;
+    float x[L::kPasses][L::kUnits][8];
     unsigned most = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int u = lane / 4 + 16 * i;
+    for (int i = 0; i < L::kPasses; ++i) {      // rows of the call in place of others
+        const int token = min(max(lane / L::kAcross + i * L::kStep, p.from), p.to);
+        const Bits *r = data + (int64_t)(p.row0 + token - p.from) * a.k.token;
+        if constexpr (HOW == kHalves) {
+            load8<TYPE, true>(r, 8 * k, size, x[i][0]);
+            load8<TYPE, true>(r, a.pairs + 8 * k, size, x[i][1]);
+            rotate(angles_of(a, 8 * k, p.block * kKvBlock + token), x[i][0], x[i][1]);
+        } else rotated8<TYPE, HOW>(a, r, 8 * k, p.block * kKvBlock + token, x[i][0]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int u = 0; u < L::kUnits; ++u) widest(most, x[i][u]);
+    }
+    float *scales = a.cache.k_scale + at;
+    const float before = p.from > 0 ? *scales : 0.f;
+    const Scale s = scale_of(most, before, p.from > 0);
+    if (lane == 0 && page >= 0) *scales = s.scale;
+    if (lane % L::kAcross >= count) return;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][t][e] = 0.f;
-            const int token = 4 * j + t;
-            if (u >= units || token < from || token > to) continue;
-            const Bits *r = data + (int64_t)(row0 + token - from) * in.token;
-            if (values) load8<TYPE, WIDE>(r, 8 * u, size, x[i][t]);
-            else {
-                rotated8<TYPE, WIDE>(a, r, 8 * u, block * kKvBlock + token, x[i][t]);
-                if (a.k_out) store8<TYPE, WIDE>(static_cast<Bits *>(a.k_out) + ((int64_t)(row0 + token - from) * a.cache.heads + head) * size, 8 * u, size, x[i][t]);
-            }
+    for (int i = 0; i < L::kPasses; ++i) {
+        const int token = lane / L::kAcross + i * L::kStep;
+        const bool mine = token >= p.from && token <= p.to;
+        if (token > p.to || (!mine && !s.grown)) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(x[i][t][e]) & 0x7fffffffu);
+        for (int u = 0; u < L::kUnits; ++u) {
+            const int d = 8 * k + u * a.pairs;
+            if (mine && a.k_out) store8<TYPE, HOW != kNarrow>(static_cast<Bits *>(a.k_out) + ((int64_t)(p.row0 + token - p.from) * a.cache.heads + p.head) * size, d, size, x[i][u]);
+            if (page < 0) continue;
+            u32x2 *codes = reinterpret_cast<u32x2 *>(a.cache.k + (at * kKvBlock + token) * row + d);
+            *codes = mine ? u32x2{four_codes(x[i][u], s), four_codes(x[i][u] + 4, s)} : u32x2{rescaled((*codes)[0], s.share), rescaled((*codes)[1], s.share)};
         }
     }
-    const int page = page_of(a.cache, a.seqs, seq, block);
-    if (page < 0) return;
-    const int64_t at = block_at(a.cache, page, head, block);
-    float *scales = (values ? a.cache.v_scale : a.cache.k_scale) + at;
-    int8_t *codes = (values ? a.cache.v : a.cache.k) + at * kKvBlock * row;
+}
 
-    const float largest = __uint_as_float(wave_max(most));
-    const float before = from > 0 ? *scales : 0.f, fresh = largest / 127.f;
-    const bool finite = largest <= 3.402823466e38f && before == before;
-    const float scale = !finite ? kNan : fmaxf(before, fresh);
-    const float inverse = finite ? fminf(1.f / scale, 3.402823466e38f) : 0.f;   // scale 0: 0 * FLT_MAX = 0
-    const bool grown = finite && scale > before && from > 0;
-    const float share = grown ? before / scale : 1.f;
-    unsigned q[2][4][2];
+template <int TYPE, int HOW, int SIZES> __device__ __forceinline__ void append_values(const AppendArgs &a, const Piece &p, unsigned *lds)
+{
+    typedef typename Entry<TYPE>::bits Bits;
+    const int lane = threadIdx.x % 64, j = lane % 4, size = a.cache.size, row = kv_row(size), units = (size + 7) / 8;
+    const int page = page_of(a.cache, a.seqs, p.seq, p.block);
+    if (page < 0) return;
+    const int64_t at = block_at(a.cache, page, p.head, p.block);
+    u32x4 *codes = reinterpret_cast<u32x4 *>(a.cache.v + at * kKvBlock * row);
+    const Bits *data = static_cast<const Bits *>(a.v.data) + p.head * a.v.head;
+    float x[SIZES][4][8];
+    unsigned most = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < SIZES; ++i)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                q[i][t][w] = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) q[i][t][w] |= (finite ? (unsigned)code_of(x[i][t][4 * w + e], inverse) & 255u : 0u) << 8 * e;
-            }
-    if (lane == 0) *scales = scale;
-    if (!values) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int u = lane / 4 + 16 * i;
-            if (u >= units) continue;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int token = 4 * j + t;
-                u32x2 *to8 = reinterpret_cast<u32x2 *>(codes + token * row + 8 * u);
-                if (token >= from && token <= to) *to8 = u32x2{q[i][t][0], q[i][t][1]};
-                else if (token < from && grown) *to8 = u32x2{rescaled((*to8)[0], share), rescaled((*to8)[1], share)};
-            }
+        for (int t = 0; t < 4; ++t) {           // rows of the call in place of others
+            const int token = min(max(4 * j + t, p.from), p.to);
+            load8<TYPE, HOW != kNarrow>(data + (int64_t)(p.row0 + token - p.from) * a.v.token, 8 * min(lane / 4 + 16 * i, units - 1), size, x[i][t]);
+            widest(most, x[i][t]);
         }
-        return;
-    }
-    // values: dwords of four tokens, rows of a channel through the LDS, joined with the tokens that were there
+    float *scales = a.cache.v_scale + at;
+    const float before = p.from > 0 ? *scales : 0.f;
+    u32x4 old[2 * SIZES];
+    if (p.from > 0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 2 * SIZES; ++i) old[i] = codes[min(lane + 64 * i, size - 1)];
+    }
+    const Scale s = scale_of(most, before, p.from > 0);
+    if (lane == 0) *scales = s.scale;
+    // dwords of four tokens, rows of a channel through the LDS, joined with the tokens that were there; zeros behind the last
+#pragma unroll
+    for (int i = 0; i < SIZES; ++i) {
         const int u = lane / 4 + 16 * i;
         if (u >= units) continue;
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+        for (int w = 0; w < 2; ++w) {
+            unsigned q[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) q[t] = 4 * j + t <= p.to ? four_codes(x[i][t] + 4 * w, s) : 0u;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 unsigned four = 0;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) four |= (q[i][t][w] >> 8 * e & 255u) << 8 * t;
+                for (int t = 0; t < 4; ++t) four |= (q[t] >> 8 * e & 255u) << 8 * t;
                 lds[(8 * u + 4 * w + e) * 4 + j] = four;
             }
+        }
     }
     order_wave();
-    const bool whole = from == 0;   // nothing was there: zeros behind the last token
-    for (int d = lane; d < size; d += 64) {
+#pragma unroll
+    for (int i = 0; i < 2 * SIZES; ++i) {
+        const int d = lane + 64 * i;
+        if (d >= size) continue;
         u32x4 four = reinterpret_cast<const u32x4 *>(lds)[d];
-        u32x4 *to16 = reinterpret_cast<u32x4 *>(codes + d * kKvBlock);
-        if (!whole) {
-            const u32x4 old = *to16;
+        if (p.from > 0) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const unsigned kept = grown ? rescaled(old[w], share) : old[w];
+                const unsigned kept = s.grown ? rescaled(old[i][w], s.share) : old[i][w];
                 unsigned mask = 0;   // bytes of tokens before `from`
 #pragma unroll
-                for (int t = 0; t < 4; ++t) mask |= 4 * w + t < from ? 255u << 8 * t : 0u;
+                for (int t = 0; t < 4; ++t) mask |= 4 * w + t < p.from ? 255u << 8 * t : 0u;
                 four[w] = (kept & mask) | (four[w] & ~mask);
             }
         }
-        *to16 = four;
+        codes[d] = four;
     }
 }
 
-template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_kv_append(AppendArgs a)
+// Four query heads from h0 on.
+template <int TYPE, int HOW, int SIZES> __device__ __forceinline__ void rotate_queries(const AppendArgs &a, const Piece &p, int h0)
 {
     typedef typename Entry<TYPE>::bits Bits;
-    __shared__ __attribute__((aligned(16))) unsigned lds[kWaves][TST_MAX_HEAD_SIZE * kKvBlock / 4];
-    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64;
+    typedef Lanes<HOW, SIZES> L;
+    const int lane = threadIdx.x % 64, size = a.cache.size, count = (size + 7) / 8 / L::kUnits, k = lane % L::kAcross, heads = min(a.q_heads - h0, 4);
+    if (heads <= 0 || k >= count) return;
+    for (int t = lane / L::kAcross; t <= p.to - p.from; t += L::kStep) {
+        const int r = p.row0 + t, position = p.block * kKvBlock + p.from + t;
+        const Bits *in = static_cast<const Bits *>(a.q.data) + (int64_t)r * a.q.token;
+        Bits *out = static_cast<Bits *>(a.q_out) + (int64_t)r * a.q_heads * size;
+        float x[4][L::kUnits][8];
+        if constexpr (HOW == kHalves) {
+            const Angles g = angles_of(a, 8 * k, position);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const Bits *row = in + min(h0 + h, a.q_heads - 1) * a.q.head;
+                load8<TYPE, true>(row, 8 * k, size, x[h][0]);
+                load8<TYPE, true>(row, a.pairs + 8 * k, size, x[h][1]);
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) rotate(g, x[h][0], x[h][1]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) rotated8<TYPE, HOW>(a, in + min(h0 + h, a.q_heads - 1) * a.q.head, 8 * k, position, x[h][0]);
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int u = 0; u < L::kUnits; ++u)
+                if (h < heads) store8<TYPE, HOW != kNarrow>(out + (int64_t)(h0 + h) * size, 8 * k + u * a.pairs, size, x[h][u]);
+    }
+}
+
+template <int TYPE, int HOW, int SIZES> __global__ void __launch_bounds__(64 * kWaves) k_kv_append(AppendArgs a)
+{
+    __shared__ __attribute__((aligned(16))) unsigned lds[kWaves][128 * SIZES * kKvBlock / 4];
+    const int wave = uniform(threadIdx.x / 64);
     const int at = blockIdx.x;
     const int seq = a.seqs.offsets ? uniform(find_sequence(a.seqs.offsets, a.seqs.tokens, a.seqs.count, kKvBlock, 2, at)) : at;
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
@@ -236,23 +347,16 @@ template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_
     const int block = (first >> 4) + piece;
     if (rows.n == 0 || piece < 0 || block > (len - 1) >> 4) return;
     const int from = max(first - block * kKvBlock, 0), to = min(len - 1 - block * kKvBlock, kKvBlock - 1);
-    const int row0 = rows.first + block * kKvBlock + from - first;
-    if ((int)blockIdx.y < a.kv_groups) {
-        const int item = blockIdx.y * kWaves + wave;
-        if (item < 2 * a.cache.heads) append_block<TYPE, WIDE>(a, item & 1, item >> 1, seq, block, from, to, row0, lds[wave]);
+    Piece p{0, seq, block, from, to, rows.first + block * kKvBlock + from - first};
+    if ((int)blockIdx.y >= a.kv_groups) {
+        rotate_queries<TYPE, HOW, SIZES>(a, p, ((blockIdx.y - a.kv_groups) * kWaves + wave) * 4);
         return;
     }
-    // queries: rows of four heads for each wavefront, a unit of 8 channels for each lane
-    const int h0 = ((blockIdx.y - a.kv_groups) * kWaves + wave) * 4, heads = min(a.q_heads - h0, 4), size = a.cache.size, units = (size + 7) / 8;
-    const int across = units <= 8 ? 8 : units <= 16 ? 16 : 32, u = lane & (across - 1);
-    if (heads <= 0 || u >= units) return;
-    const int count = heads * (to - from + 1);
-    for (int i = lane / across; i < count; i += 64 / across) {
-        const int t = i / heads, h = h0 + i - t * heads, r = row0 + t;
-        float x[8];
-        rotated8<TYPE, WIDE>(a, static_cast<const Bits *>(a.q.data) + (int64_t)r * a.q.token + h * a.q.head, 8 * u, block * kKvBlock + from + t, x);
-        store8<TYPE, WIDE>(static_cast<Bits *>(a.q_out) + ((int64_t)r * a.q_heads + h) * size, 8 * u, size, x);
-    }
+    const int item = blockIdx.y * kWaves + wave;
+    p.head = item >> 1;
+    if (p.head >= a.cache.heads) return;
+    if (item & 1) append_values<TYPE, HOW, SIZES>(a, p, lds[wave]);
+    else append_keys<TYPE, HOW, SIZES>(a, p);
 }
 
 // What a code stands for, rounded to fp32 (the compiler would otherwise round the product to fp16 at once).
@@ -292,22 +396,40 @@ template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_
     Bits *out = static_cast<Bits *>(values ? a.v_out : a.k_out) + ((int64_t)row0 * a.cache.heads + head) * size;
     const int64_t next = (int64_t)a.cache.heads * size;   // entries from token to token
     if (!values) {
-        const int across = units <= 8 ? 8 : units <= 16 ? 16 : 32, u = lane & (across - 1);
+        const int across = units <= 8 ? 8 : units <= 16 ? 16 : 32, u = lane & (across - 1), step = 64 / across;
         if (u >= units) return;
-        for (int t = from + lane / across; t <= to; t += 64 / across) {
-            const u32x2 eight = *reinterpret_cast<const u32x2 *>(codes + t * row + 8 * u);
-            float x[8];
+        for (int t0 = from + lane / across; t0 <= to; t0 += 4 * step) {      // four rows at a time
+            u32x2 eight[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = value_of(eight[e / 4], e % 4, scale);
-            store8<TYPE, WIDE>(out + (t - from) * next, 8 * u, size, x);
+            for (int b = 0; b < 4; ++b) eight[b] = *reinterpret_cast<const u32x2 *>(codes + min(t0 + b * step, to) * row + 8 * u);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                if (t0 + b * step > to) continue;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = value_of(eight[b][e / 4], e % 4, scale);
+                store8<TYPE, WIDE>(out + (t0 + b * step - from) * next, 8 * u, size, x);
+            }
         }
         return;
     }
-    for (int d = lane; d < size; d += 64) {
-        const u32x4 sixteen = *reinterpret_cast<const u32x4 *>(codes + d * kKvBlock);
+    // two neighbouring channels a lane, and both of a token at once where that is on a border
+    for (int d = 2 * lane; d < size; d += 128) {
+        const u32x4 *at = reinterpret_cast<const u32x4 *>(codes) + d;
+        const u32x4 two[2] = {at[0], at[1]};     // (rows of codes are longer than an odd size)
 #pragma unroll
-        for (int t = 0; t < kKvBlock; ++t)
-            if (t >= from && t <= to) out[(t - from) * next + d] = Entry<TYPE>::put(value_of(sixteen[t / 4], t % 4, scale));
+        for (int t = 0; t < kKvBlock; ++t) {
+            if (t < from || t > to) continue;
+            Bits pair[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pair[i] = Entry<TYPE>::put(value_of(two[i][t / 4], t % 4, scale));
+            Bits *to2 = out + (t - from) * next + d;
+            if constexpr (WIDE) __builtin_memcpy(__builtin_assume_aligned(to2, sizeof(pair)), pair, sizeof(pair));
+            else {
+                to2[0] = pair[0];
+                if (d + 1 < size) to2[1] = pair[1];
+            }
+        }
     }
 }
 
@@ -386,8 +508,13 @@ int tst_kv_append(const tst_kv_cache_t *cache, const tst_sequences_t *sequences,
     return tst::status(tst::for_type(type, [&](auto t) {
         constexpr int TYPE = decltype(t)::value;
         hipStream_t st = static_cast<hipStream_t>(stream);
-        if (wide) tst::k_kv_append<TYPE, true><<<grid, 64 * tst::kWaves, 0, st>>>(a);
-        else tst::k_kv_append<TYPE, false><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        auto launch = [&](auto how) {
+            if (cache->head_size <= 128) tst::k_kv_append<TYPE, decltype(how)::value, 1><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+            else tst::k_kv_append<TYPE, decltype(how)::value, 2><<<grid, 64 * tst::kWaves, 0, st>>>(a);
+        };
+        if (wide && a.pairs > 0 && !a.interleaved && 2 * a.pairs == cache->head_size) launch(std::integral_constant<int, tst::kHalves>{});
+        else if (wide) launch(std::integral_constant<int, tst::kWide>{});
+        else launch(std::integral_constant<int, tst::kNarrow>{});
         return hipGetLastError();
     }));
 }
@@ -401,7 +528,7 @@ int tst_kv_read(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, i
     const size_t entry = tst::type_bytes(type);
     if (!k_out || !v_out || !tst::aligned(k_out, entry) || !tst::aligned(v_out, entry)) return TSTGEMM_EINVAL;
     const tst::ReadArgs a{tst::cache_of(cache), tst::sequences_of(sequences), k_out, v_out};
-    const bool wide = tst::aligned(k_out, 16) && cache->head_size % 8 == 0;
+    const bool wide = tst::aligned(k_out, 16) && tst::aligned(v_out, 16) && cache->head_size % 8 == 0;
     const dim3 grid(sequences->offsets ? tst::pieces(sequences->tokens, sequences->sequences, tst::kKvBlock, 2) : sequences->sequences,
                     tst::blocks_of(2 * cache->heads, tst::kWaves));
     return tst::status(tst::for_type(type, [&](auto t) {
