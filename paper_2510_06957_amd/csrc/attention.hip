@@ -132,14 +132,16 @@ __device__ __forceinline__ float across_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// FAST: 16-bit operands whose rows lie on 16-byte borders.
+// FAST: rows lie on 16-byte borders.
 template <int TYPE, int ROW, bool FAST> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
-    static constexpr int kWaves = FAST && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
-    static constexpr int kOccupancy = FAST && ROW <= 64 ? 4 : kWaves / 4;
+    static constexpr bool kAhead = FAST && TYPE != TST_F32;      // the next keys' logits beside these keys' weights
+    static constexpr int kWaves = kAhead && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
+    static constexpr int kOccupancy = kAhead && ROW <= 64 ? 4 : kWaves / 4;
     static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
-    static constexpr int kKeys = FAST && ROW <= 128 ? 64 : 32;             // of a tile in the LDS
-    static constexpr int kBuffersK = FAST ? 3 : 1, kBuffersV = FAST ? 2 : 1;   // (K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
+    static constexpr int kKeys = kAhead && ROW <= 128 ? 64 : 32;            // of a tile in the LDS
+    // (kAhead: K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
+    static constexpr int kBuffersK = kAhead ? 3 : ROW <= 128 ? 2 : 1, kBuffersV = kAhead || ROW <= 128 ? 2 : 1;
     // bytes from key to key: 16 rows of keys, and 4 rows of 32 channels of values, fall into different banks
     static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + (ROW % 128 == 96 ? 0 : 64);
     static constexpr int kPlaneK = kKeys * kStrideK, kPlaneV = kKeys * kStrideV;
@@ -211,7 +213,13 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
                 // from somewhere in the tile whatever it is (zeros come in store()): a load that depends on the lane would have to be waited for
                 // before the next.  (offsets within a tile have 32 bits)
                 const int key = min(key_of(i), left - 1), channel = channel_of(i) < size ? channel_of(i) : 0;
-                raw[i] = __builtin_bit_cast(Raw<TYPE>, *reinterpret_cast<const u32x4 *>(at + ((unsigned)key * (unsigned)stride + (unsigned)channel)));
+                union {
+                    u32x4 v[sizeof(Raw<TYPE>) / 16];
+                    Raw<TYPE> r;
+                } u;
+#pragma unroll
+                for (int w = 0; w < (int)(sizeof(u) / 16); ++w) u.v[w] = reinterpret_cast<const u32x4 *>(at + ((unsigned)key * (unsigned)stride + (unsigned)channel))[w];
+                raw[i] = u.r;
             } else raw[i] = load_raw<TYPE>(at + key_of(i) * stride, channel_of(i), size, there, wide);
         }
     }
@@ -274,7 +282,7 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
     auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
     load_k(0), load_v(0);
-    if (FAST && tiles > 1) k_next.load(k_data, a.k.token, 1, keys, a.size, true);
+    if (S::kAhead && tiles > 1) k_next.load(k_data, a.k.token, 1, keys, a.size, true);
 
     for (int d = threadIdx.x; d < ROW; d += S::kThreads) spoilt[d] = 0x7fffffff;
     if (threadIdx.x == 0) any_spoilt = 0;
@@ -406,10 +414,10 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
     };
 
     __syncthreads();     // spoilt is clear
-    if constexpr (!FAST) {
+    if constexpr (!S::kAhead) {
+        store_k(0), store_v(0);
+        __syncthreads();
         for (int kt = 0; kt < tiles; ++kt) {
-            store_k(kt), store_v(kt);
-            __syncthreads();
             if (kt + 1 < tiles) load_k(kt + 1), load_v(kt + 1);
 #pragma unroll
             for (int s = 0; s < kSub; ++s) {
@@ -424,6 +432,8 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
                     second_product(sub, w);
                 }
             }
+            if (S::kBuffersK == 1) __syncthreads();     // everybody has read the only buffer
+            if (kt + 1 < tiles) store_k(kt + 1), store_v(kt + 1);
             __syncthreads();
         }
     } else {
@@ -538,13 +548,8 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                 a.tiles = (int)((int64_t)tokens * group / S::kRows) + sequences;
                 tst::k_attention<TYPE, ROW, FAST><<<(unsigned)a.tiles * heads, S::kThreads, 0, st>>>(a);
             };
-            if constexpr (TYPE != TST_F32) {
-                if (a.wide && a.k.token <= 1 << 24 && a.v.token <= 1 << 24) {
-                    launch(std::true_type{});
-                    return hipGetLastError();
-                }
-            }
-            launch(std::false_type{});
+            if (a.wide && a.k.token <= 1 << 24 && a.v.token <= 1 << 24) launch(std::true_type{});
+            else launch(std::false_type{});
             return hipGetLastError();
         });
     }));
