@@ -132,14 +132,15 @@ __device__ __forceinline__ float across_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// FAST: rows lie on 16-byte borders.
-template <int TYPE, int ROW, bool FAST> struct Shape {
+// How rows are read and dealt: anywhere, an entry at a time; on 16-byte borders; so, and few of them, in tiles of half the rows.
+enum Way { kAny, kFast, kFew };
+template <int TYPE, int ROW, int WAY> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
-    static constexpr bool kAhead = FAST && TYPE != TST_F32;      // the next keys' logits beside these keys' weights
-    static constexpr int kWaves = kAhead && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
-    static constexpr int kOccupancy = kAhead && ROW <= 64 ? 4 : kWaves / 4;
+    static constexpr bool kAhead = WAY != kAny && TYPE != TST_F32;      // the next keys' logits beside these keys' weights
+    static constexpr int kWaves = kAhead && WAY == kFast && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
+    static constexpr int kOccupancy = kAhead && ROW <= 64 ? 4 : kAhead && ROW <= 128 ? 2 : 1;
     static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
-    static constexpr int kKeys = kAhead && ROW <= 128 ? 64 : 32;            // of a tile in the LDS
+    static constexpr int kKeys = kAhead && WAY == kFast && ROW <= 128 ? 64 : 32;            // of a tile in the LDS
     // (kAhead: K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
     static constexpr int kBuffersK = kAhead ? 3 : ROW <= 128 ? 2 : 1, kBuffersV = kAhead || ROW <= 128 ? 2 : 1;
     // bytes from key to key: 16 rows of keys, and 4 rows of 32 channels of values, fall into different banks
@@ -195,8 +196,8 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int rows, int num
 }
 
 // A tile of keys or values on its way from memory to the LDS: 8 entries a chunk.
-template <int TYPE, int ROW, bool FAST> struct Staged {
-    typedef Shape<TYPE, ROW, FAST> S;
+template <int TYPE, int ROW, int WAY> struct Staged {
+    typedef Shape<TYPE, ROW, WAY> S;
     Raw<TYPE> raw[S::kChunks];
     static __device__ __forceinline__ int key_of(int i) { return (threadIdx.x + S::kThreads * i) / (ROW / 8); }
     static __device__ __forceinline__ int channel_of(int i) { return (threadIdx.x + S::kThreads * i) % (ROW / 8) * 8; }
@@ -209,7 +210,7 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i) {
             const bool there = key_of(i) < min(left, S::kKeys);
-            if constexpr (FAST) {
+            if constexpr (WAY != kAny) {
                 // from somewhere in the tile whatever it is (zeros come in store()): a load that depends on the lane would have to be waited for
                 // before the next.  (offsets within a tile have 32 bits)
                 const int key = min(key_of(i), left - 1), channel = channel_of(i) < size ? channel_of(i) : 0;
@@ -241,7 +242,7 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
     }
     __device__ __forceinline__ void store(char *to, int stride, int plane, int left, int size)
     {
-        if (FAST && (left < S::kKeys || size < ROW)) {
+        if (WAY != kAny && (left < S::kKeys || size < ROW)) {
 #pragma unroll
             for (int i = 0; i < S::kChunks; ++i)
                 if (key_of(i) >= left || channel_of(i) >= size) raw[i] = Raw<TYPE>{};
@@ -256,9 +257,9 @@ template <int TYPE, int ROW, bool FAST> struct Staged {
     }
 };
 
-template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape<TYPE, ROW, FAST>::kThreads), (Shape<TYPE, ROW, FAST>::kOccupancy)) k_attention(PromptArgs a)
+template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<TYPE, ROW, WAY>::kThreads), (Shape<TYPE, ROW, WAY>::kOccupancy)) k_attention(PromptArgs a)
 {
-    typedef Shape<TYPE, ROW, FAST> S;
+    typedef Shape<TYPE, ROW, WAY> S;
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int P = S::kPlanes, kSteps = ROW / 16, kTiles = ROW / 32, kSub = S::kKeys / 32;   // 32 keys at a time
     __shared__ __attribute__((aligned(16))) char lds_k[S::kBuffersK * S::kBufferK];
@@ -278,9 +279,9 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
 
     const Bits *k_data = static_cast<const Bits *>(a.k.data) + (int64_t)first * a.k.token + head * a.k.head;
     const Bits *v_data = static_cast<const Bits *>(a.v.data) + (int64_t)first * a.v.token + head * a.v.head;
-    Staged<TYPE, ROW, FAST> k_tile, v_tile, k_next;
-    auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, FAST || a.wide); };
-    auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, FAST || a.wide); };
+    Staged<TYPE, ROW, WAY> k_tile, v_tile, k_next;
+    auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, WAY != kAny || a.wide); };
+    auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, WAY != kAny || a.wide); };
     load_k(0), load_v(0);
     if (S::kAhead && tiles > 1) k_next.load(k_data, a.k.token, 1, keys, a.size, true);
 
@@ -297,7 +298,7 @@ template <int TYPE, int ROW, bool FAST> __global__ void __launch_bounds__((Shape
         const Bits *row = static_cast<const Bits *>(a.q.data) + (int64_t)(first + max(token, 0)) * a.q.token + q_head * a.q.head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, FAST || a.wide);
+            Raw<TYPE> raw = load_raw<TYPE>(row, 16 * s + 8 * half, a.size, there, WAY != kAny || a.wide);
             if (a.negative) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -542,14 +543,20 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
         return tst::for_row(head_size, [&](auto r) {
             constexpr int TYPE = decltype(t)::value, ROW = decltype(r)::value;
             hipStream_t st = static_cast<hipStream_t>(stream);
-            auto launch = [&](auto fast) {
-                constexpr bool FAST = decltype(fast)::value;
-                typedef tst::Shape<TYPE, ROW, FAST> S;
+            auto launch = [&](auto way) {
+                constexpr int WAY = decltype(way)::value;
+                typedef tst::Shape<TYPE, ROW, WAY> S;
                 a.tiles = (int)((int64_t)tokens * group / S::kRows) + sequences;
-                tst::k_attention<TYPE, ROW, FAST><<<(unsigned)a.tiles * heads, S::kThreads, 0, st>>>(a);
+                tst::k_attention<TYPE, ROW, WAY><<<(unsigned)a.tiles * heads, S::kThreads, 0, st>>>(a);
             };
-            if (a.wide && a.k.token <= 1 << 24 && a.v.token <= 1 << 24) launch(std::true_type{});
-            else launch(std::false_type{});
+            if (!a.wide || a.k.token > 1 << 24 || a.v.token > 1 << 24) launch(std::integral_constant<int, tst::kAny>{});
+            else if constexpr (TYPE != TST_F32 && ROW <= 128) {
+                // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole, 32 heads of
+                // 128, 8 of keys: 256 tokens 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149)
+                const int64_t whole = (int64_t)tokens * group / tst::Shape<TYPE, ROW, tst::kFast>::kRows * heads;
+                if (2 * whole < 3 * tst::compute_units()) launch(std::integral_constant<int, tst::kFew>{});
+                else launch(std::integral_constant<int, tst::kFast>{});
+            } else launch(std::integral_constant<int, tst::kFast>{});
             return hipGetLastError();
         });
     }));
