@@ -355,7 +355,8 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
     auto rebase = [&](const f32x16 &z) {
         const float top = across_max(largest_of(z)) * a.scale;
         if (__any(top > base + kSlack)) {
-            const float now = fmaxf(base, top), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - now);
+            const float now = top > base + kSlack ? top : base, keep =   // (by the row itself alone)
+                now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - now);
             base = now;
             sum *= keep;
 #pragma unroll

@@ -22,7 +22,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kWaves = 4, kUnit = 64;   // tokens of a wavefront at a time
 constexpr float kNan = __builtin_nanf("");
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLeastScale = 1e-36f;   // of values, as the reference that weights are relative to
+constexpr float kLeastScale = 1e-33f;   // of values, as what weights are relative to: 2^15 over it is finite
 
 struct KvArgs {
     Cache cache;
@@ -293,10 +293,11 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     least = uniform(least);   // all rows see the keys below this
 
     f32x4 o[RT][S::kTiles];
-    float most[RT], sum[RT], reference = kLeastScale;   // of logits and of scales of values: what weights are relative to
+    // What a row's weights are relative to, of logits and of scales of values, by what the row itself sees alone; 2^kShift over the latter.
+    float most[RT], reference[RT], inverse[RT], sum[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        most[rt] = -INFINITY, sum[rt] = 0.f;
+        most[rt] = -INFINITY, sum[rt] = 0.f, reference[rt] = kLeastScale, inverse[rt] = S::kShift / kLeastScale;
 #pragma unroll
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -365,8 +366,8 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
             __builtin_amdgcn_sched_barrier(0);
 
             const bool cut = (u + 1) * kUnit > least;
-            bool anew = v_scale > reference * S::kScaleSlack;
-            float top[RT];
+            bool anew = false;
+            float top[RT], v_own[RT];     // v_own: 0 for a block that the row does not see
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const float f = factor[rt] * k_scale;
@@ -375,37 +376,38 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) z[rt][t][e] *= f;
+                v_own[rt] = v_scale;
                 if (cut) {
+                    const int from = u * kUnit + g * kKvBlock;
+                    if (from >= limit[rt]) v_own[rt] = 0.f;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (u * kUnit + g * kKvBlock + 4 * t + e >= limit[rt]) z[rt][t][e] = -INFINITY;
+                            if (from + 4 * t + e >= limit[rt]) z[rt][t][e] = -INFINITY;
                 }
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top[rt] = fmaxf(top[rt], z[rt][t][e]);
-                anew |= top[rt] > most[rt] + S::kSlack;
+                anew |= top[rt] > most[rt] + S::kSlack || v_own[rt] > reference[rt] * S::kScaleSlack;
             }
             if (__any(anew)) {
-                const float largest = fmaxf(reference, quarters_max(v_scale)), part = reference / largest;
-                reference = largest;
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    const float now = fmaxf(most[rt], quarters_max(top[rt])), keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most[rt] - now);
-                    most[rt] = now;
+                    const float t = quarters_max(top[rt]), v = quarters_max(v_own[rt]);
+                    const float now = t > most[rt] + S::kSlack ? t : most[rt], largest = v > reference[rt] * S::kScaleSlack ? v : reference[rt];
+                    const float keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most[rt] - now), times = keep * (reference[rt] / largest);
+                    most[rt] = now, reference[rt] = largest, inverse[rt] = S::kShift / largest;
                     sum[rt] *= keep;
-                    const float times = keep * part;
 #pragma unroll
                     for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;
                 }
             }
-            const float v_part = v_scale / reference * S::kShift;
             f16x8 w[RT][S::kPlanes][2];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const float base = most[rt] == -INFINITY ? 0.f : most[rt];
+                const float base = most[rt] == -INFINITY ? 0.f : most[rt], v_part = v_own[rt] * inverse[rt];
                 float s = 0.f;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
@@ -450,7 +452,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         for (int w = 0; w < kWaves; ++w) all[rt] = fmaxf(all[rt], states[w][rt][m16].x);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) total[rt] += states[w][rt][m16].y * weight_of(states[w][rt][m16].x, all[rt]);
-        const float times = weight_of(most[rt], all[rt]) * reference * (1.f / S::kShift);
+        const float times = weight_of(most[rt], all[rt]) * (reference[rt] * (1.f / S::kShift));
 #pragma unroll
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = times == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][dt] * times;
     }

@@ -51,7 +51,9 @@ const int32_t *int32(PyObject *o, int dev, int64_t n)
 const at::Tensor *angles(PyObject *o, int dev)
 {
     const at::Tensor *t = plain(o, dev);
-    return t != nullptr && t->scalar_type() == at::kFloat && t->dim() == 2 && t->is_contiguous() && t->size(0) <= INT_MAX && t->size(1) <= TST_MAX_HEAD_SIZE ? t : nullptr;
+    return t != nullptr && t->scalar_type() == at::kFloat && t->dim() == 2 && t->is_contiguous() && t->size(0) >= 1 && t->size(0) <= INT_MAX && t->size(1) >= 1 &&
+                   t->size(1) <= TST_MAX_HEAD_SIZE
+               ? t : nullptr;
 }
 
 // A cache and the sequences of a call; ok only if all of it fits.

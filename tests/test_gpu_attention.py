@@ -400,3 +400,415 @@ def test_prompts_of_many_sequences():
         lens = [int(x) for x in rng(26, n).integers(0, 41, n)]
         lens[n // 3] = long
         check_prompt(lens, 2, 1, 64, "bf16", 26)
+
+
+@pytest.mark.parametrize("q_heads,heads,size,dtype", [(64, 8, 64, "bf16"), (64, 8, 96, "f16"), (64, 16, 128, "bf16"), (66, 2, 128, "f16"), (64, 64, 64, "f16"), (64, 8, 80, "bf16"),
+                                                      (64, 4, 192, "bf16"), (32, 8, 256, "f16")])
+def test_prompts_in_whole_tiles(q_heads, heads, size, dtype):
+    """Enough rows for the tiles that large calls take; a few heads and rows of each sequence against the definition."""
+    lens = [1217, 0, 3, 64, 65, 400, 1]
+    q, k, v = prompt(lens, q_heads, heads, size, dtype, 27)
+    at = starts(lens)
+    Y = tg.tst_attention(q, k, v, int32(at))
+    few = [0, q_heads // 2 + 1, q_heads - 1]
+    rows = np.unique(np.r_[np.arange(0, 70), np.arange(120, 135), np.arange(250, 262), np.arange(1200, 1217)])
+    want, bound = prompt_reference(f32(q), f32(k), f32(v), at, 1 / math.sqrt(size), dtype, few, rows)
+    seen = np.concatenate([a + rows[rows < b - a] for a, b in zip(at, at[1:])])
+    assert_within(Y[torch.from_numpy(seen).cuda()][:, few], want[seen][:, few], bound[seen][:, few], dtype)
+    assert torch.equal(tg.tst_attention(q, k, v, int32(at)), Y)
+    # each sequence by itself, in smaller tiles: the same up to the rounding of its sums
+    for a, b in zip(at, at[1:]):
+        alone = tg.tst_attention(q[a:b], k[a:b], v[a:b], int32([0, b - a]))
+        assert torch.allclose(alone.float(), Y[a:b].float(), rtol=8 * LAST[dtype], atol=0.02)
+
+
+@pytest.mark.parametrize("q_heads,lens", [(4, [90, 40]), (64, [1217, 64])])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_prompts_what_a_row_does_not_see_does_not_touch_it(dtype, q_heads, lens):
+    """Infinities and NaN in keys and values behind a row, in other sequences and in rows of no sequence."""
+    heads, size = 2, 64
+    T = sum(lens)
+    q, k, v = prompt([T + 9], q_heads, heads, size, dtype, 28)
+    offsets = int32([5, 5 + lens[0], 5 + T])
+    clean = tg.tst_attention(q, k, v, offsets)[5:5 + T]
+    k2, v2 = k.clone(), v.clone()
+    k2[:5], v2[:5], k2[5 + T:], v2[5 + T:] = float("nan"), float("inf"), float("inf"), float("nan")
+    cut = 5 + lens[0] - 27           # from here on the first sequence is spoilt, a channel of a head's values
+    k2[cut:5 + lens[0], 1] = float("nan")
+    v2[cut + 2, 0, 7], v2[cut + 3, 0, 63], v2[cut + 4, 0, 0], v2[cut + 2, 1] = float("nan"), float("inf"), -float("inf"), float("inf")
+    Y = tg.tst_attention(q, k2, v2, offsets)[5:5 + T]
+    group, n = q_heads // heads, cut - 5
+    assert torch.equal(Y[:n], clean[:n]) and torch.equal(Y[lens[0]:], clean[lens[0]:])
+    assert torch.equal(Y[:n + 2, :group], clean[:n + 2, :group])
+    spoilt = ~torch.isfinite(Y[:lens[0], :group])
+    want = torch.zeros_like(spoilt)
+    want[n + 2:, :, 7], want[n + 3:, :, 63], want[n + 4:, :, 0] = True, True, True
+    assert torch.equal(spoilt, want)
+    assert torch.equal(Y[:lens[0], :group][~want], clean[:lens[0], :group][~want])
+    assert torch.isnan(Y[n:lens[0], group:]).all()
+    q2 = q.clone()
+    q2[5 + 3, 1, 2], q2[5 + 4, 1, 2] = float("nan"), float("inf")
+    Y = tg.tst_attention(q2, k, v, offsets)[5:5 + T]
+    assert torch.isnan(Y[3, 1]).all() and not torch.isfinite(Y[4, 1]).any()
+    Y[3:5, 1] = clean[3:5, 1]
+    assert torch.equal(Y, clean)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_leave_other_rows_as_they_are(dtype):
+    q, k, v = prompt([60], 4, 4, 40, dtype, 29)
+    Y = torch.full((60, 4, 40), 7.0, dtype=TYPES[dtype], device="cuda")
+    out = tg.tst_attention(q, k, v, int32([11, 30, 30, 49]), Y=Y)
+    assert out is Y and (Y[:11] == 7).all() and (Y[49:] == 7).all() and not (Y[11:49] == 7).all(2).any()
+    assert torch.equal(tg.tst_attention(q, k, v, int32([11, 30, 30, 49]))[11:49], Y[11:49])
+    for wrong in ([49, 30, 11], [-5, 20, 2 ** 31 - 1], [60, 0, 60, 0], [0, 100, 30]):     # nothing outside is touched
+        wide = torch.full((80, 4, 40), 7.0, dtype=TYPES[dtype], device="cuda")
+        tg.tst_attention(q, k, v, int32(wrong), Y=wide[10:70])
+        assert (wide[:10] == 7).all() and (wide[70:] == 7).all()
+    Y.fill_(7)
+    tg.tst_attention(q, k, v, int32([0]), Y=Y)      # no sequences
+    tg.tst_attention(q, k, v, int32([20, 20]), Y=Y)
+    assert (Y == 7).all()
+    assert tg.tst_attention(q[:0], k[:0], v[:0], int32([0, 0])).shape == (0, 4, 40)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_over_long_caches(dtype):
+    """Chunks that are joined, of one sequence and of ragged ones; drafts of rows in two tiles; more sequences than are cut."""
+    check_over_cache([20011], [1], 4, 1, 64, 64, dtype, 31)
+    check_over_cache([9000, 17, 4097, 0, 1, 6000], [1] * 6, 7, 1, 128, 256, dtype, 32)
+    check_over_cache([5000, 800, 64], [3, 40, 64], 4, 1, 96, 16, dtype, 33)
+    lens = [int(x) for x in rng(34).integers(0, 300, 1100)]
+    check_over_cache(lens, [1] * 1100, 1, 1, 64, 16, dtype, 34)
+    check_over_cache(lens[:70] + [4000], [2] * 70 + [31], 2, 1, 64, 32, dtype, 35)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_over_the_cache_scales_of_blocks(dtype):
+    """Scales of values and keys that differ by many powers of ten between blocks; blocks of zeros."""
+    w = World([1500, 333], 2, 64, 32, 36)
+    for name, spread in (("k", 3), ("v", 12)):
+        w.ref.scale[name] *= (10.0 ** w.r.integers(-spread, 2, w.ref.scale[name].shape)).astype(np.float32)
+        w.ref.scale[name][w.r.random(w.ref.scale[name].shape) < 0.1] = 0
+    w.upload()
+    pages, lens = w.arrays()
+    Qd = strided(queries(w, 2, 4, 64, 36), dtype)
+    want, bound = reference_over_cache(w, f32(Qd), [1, 1], [0, 1, 2], 0.125, dtype)
+    assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens), want, bound, dtype)
+    w.ref.scale["v"][:] = 0
+    w.upload()
+    assert not tg.tst_kv_attention(Qd, w.cache, pages, lens).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_over_the_cache_what_a_row_does_not_see(dtype):
+    """Blocks without a scale behind a row; rows that see one, or whose query is none, are NaN."""
+    w = World([700, 90, 350], 2, 64, 16, 37)
+    new = [40, 1, 3]
+    at = starts(new)
+    Qd = strided(queries(w, at[-1], 4, 64, 37), dtype)
+    pages, lens = w.arrays()
+    clean = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at))
+    want, bound = reference_over_cache(w, f32(Qd), new, at, 0.125, dtype)
+    assert_within(clean, want, bound, dtype)
+    for name in "kv":
+        saved = w.ref.scale[name].copy()
+        for scale in (np.nan, np.float32(1e30)):
+            w.ref.scale[name][w.table[0, 688 // 16], 1, 0] = scale       # positions 688 .. of head 1: rows 28 .. of the first sequence's 40
+            w.upload()
+            Y = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at))
+            assert np.isfinite(scale) or torch.isnan(Y[28:40, 2:]).all()
+            Y[28:40, 2:] = clean[28:40, 2:]
+            assert torch.equal(Y, clean)
+        w.ref.scale[name] = saved
+    w.upload()
+    Q2 = Qd.clone()
+    Q2[3, 1, 5], Q2[40, 2, 0] = float("inf"), float("nan")
+    Y = tg.tst_kv_attention(Q2, w.cache, pages, lens, int32(at))
+    assert torch.isnan(Y[3, 1]).all() and torch.isnan(Y[40, 2]).all()
+    Y[3, 1], Y[40, 2] = clean[3, 1], clean[40, 2]
+    assert torch.equal(Y, clean)
+
+
+def test_attention_over_the_cache_where_there_are_no_pages():
+    """Pages that are none of the cache's make the rows that see them NaN, and so do positions behind the table; rows of negative positions see nothing."""
+    w = World([400, 70, 33, 20], 2, 64, 16, 38, columns=30)
+    w.table[0, 23], w.table[1, 0], w.table[2, 2] = w.ref.pages, -7, 2 ** 31 - 1
+    new = [40, 2, 1, 24]
+    at = starts(new)
+    Qd = strided(queries(w, at[-1], 2, 64, 38), "f32")
+    pages, lens = w.arrays()
+    Y = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at))
+    # page 23 is positions 368 ..: rows 8 .. of the first sequence
+    good = np.r_[np.arange(8), np.arange(at[3], at[4])]
+    want, bound = reference_over_cache(w, f32(Qd), new, at, 0.125, "f32")
+    assert_within(Y[good], want[good], bound[good], "f32")
+    assert (Y[at[3]:at[3] + 4] == 0).all()
+    assert torch.isnan(Y[8:at[3]]).all()
+    lens[:] = torch.tensor([2 ** 31 - 1, 481, -5, -2 ** 31], dtype=torch.int32)     # the table holds 480
+    w.table[:] = w.r.integers(0, w.ref.pages, w.table.shape)
+    Y = tg.tst_kv_attention(Qd, w.cache, cuda(w.table), lens, int32(at))
+    assert torch.isnan(Y[:40]).all() and torch.isnan(Y[41]).all() and torch.isfinite(Y[40]).all() and (Y[42:] == 0).all()
+    for wrong in ([40, 0, 67, 10, 50], [-9, 5, 2 ** 31 - 1, 4, 67], [67, 60, 40, 20, 0], [0, 67, 0, 67, 0]):
+        wide = torch.full((87, 2, 64), 7.0, device="cuda")
+        tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(wrong), Y=wide[10:77])
+        assert (wide[:10] == 7).all() and (wide[77:] == 7).all()
+
+
+def test_attention_over_the_cache_leaves_other_rows_as_they_are():
+    w = World([300, 50], 1, 64, 16, 39)
+    Qd = strided(queries(w, 12, 2, 64, 39), "bf16")
+    pages, lens = w.arrays()
+    Y = torch.full((12, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(8 << 20, dtype=torch.uint8, device="cuda")
+    out = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32([3, 7, 9]), Y=Y, workspace=ws)
+    assert out is Y and (Y[:3] == 7).all() and (Y[9:] == 7).all()
+    assert torch.equal(tg.tst_kv_attention(Qd, w.cache, pages, lens, int32([3, 7, 9]))[3:9], Y[3:9])
+    with pytest.raises(tg.TstgemmError) as e:
+        tg.tst_kv_attention(Qd, w.cache, pages, lens, int32([3, 7, 9]), workspace=ws[:256])
+    assert e.value.code == -8
+
+
+def test_a_cache_of_more_than_4_gib():
+    """Pages whose codes lie behind 2^31 and 2^32 bytes."""
+    heads, size, page = 8, 128, 256
+    pages = (1 << 32) // (heads * page * size) + 40
+    cache = tg.tst_kv_cache(pages, page, heads, size)
+    small = tg.tst_kv_cache(8, page, heads, size)
+    lens = int32([700, 300])
+    far = torch.tensor([[pages - 1, 3, pages // 2 + 7], [pages - 2, pages // 2, -1]], dtype=torch.int32, device="cuda")
+    near = torch.tensor([[0, 1, 2], [5, 4, -1]], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(40)
+    K, V = (torch.randn((1000, heads, size), generator=g, device="cuda").bfloat16() for _ in "kv")
+    Q = torch.randn((2, 16, size), generator=g, device="cuda").bfloat16()
+    offsets, out = int32([0, 700, 1000]), []
+    for c, table in ((cache, far), (small, near)):
+        tg.tst_kv_append(c, K, V, table, lens, offsets)
+        out.append((*tg.tst_kv_read(c, table, lens, 1000, offsets), tg.tst_kv_attention(Q, c, table, lens)))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert (out[0][0].float() - K.float()).abs().max() < 0.05
+
+
+def test_views_that_start_far_into_large_tensors():
+    """Rows, heads and pages at offsets behind 2^31 entries."""
+    big = torch.zeros((3, 1 << 30), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(41)
+    x = torch.randn((3, 6, 64), generator=g, device="cuda").bfloat16()
+    view = big[:, (1 << 30) - 384:].view(3, 6, 64)
+    view.copy_(x)
+    assert view.stride(0) == 1 << 30
+    offsets = int32([0, 3])
+    assert torch.equal(tg.tst_attention(view[:, :4], view[:, 4:5], view[:, 5:], offsets), tg.tst_attention(x[:, :4], x[:, 4:5], x[:, 5:], offsets))
+    caches = [tg.tst_kv_cache(4, 16, 1, 64) for _ in range(2)]
+    pages, lens = int32([[2]]), int32([3])
+    for c, t in zip(caches, (view, x)):
+        tg.tst_kv_append(c, t[:, 4:5], t[:, 5:], pages, lens, offsets)
+    a, b = (tg.tst_kv_read(c, pages, lens, 3, offsets) for c in caches)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].any()
+    assert torch.equal(tg.tst_kv_attention(view[:, :4], caches[0], pages, lens, offsets), tg.tst_kv_attention(x[:, :4], caches[1], pages, lens, offsets))
+
+
+# ------------------------------------------------------------------------------------------------------------------------ together, streams, graphs
+def sequence_of_calls(cache, x, q_heads, pages, lens, offsets, cos, sin, **kw):
+    """Append and attend, the newest tokens by the cache and by themselves."""
+    heads = cache.heads
+    q, k = tg.tst_kv_append(cache, x[:, q_heads:q_heads + heads], x[:, q_heads + heads:], pages, lens, offsets, Q=x[:, :q_heads], cos=cos, sin=sin, keys=True, **kw)
+    return q, k, tg.tst_kv_attention(q, cache, pages, lens, offsets, **kw), *tg.tst_kv_read(cache, pages, lens, x.shape[0], offsets, dtype=x.dtype, **kw)
+
+
+def test_a_prompt_and_what_follows_it():
+    """A prompt by itself and over the cache that it was appended to agree up to the codes; further tokens go by the cache.  Each against the definition."""
+    heads, q_heads, size, page = 2, 6, 64, 32
+    lens = [75, 20, 130]
+    w = World(lens, heads, size, page, 42, spare=9)
+    w.table = np.concatenate([w.table, np.full((3, 1), -1, np.int32)], 1)
+    free = sorted(set(range(w.ref.pages)) - set(w.table[w.table >= 0].tolist()))
+    for i, n in enumerate(lens):
+        w.table[i, -(-n // page)] = free[i]
+    r = rng(42, 5)
+    cos, sin = angles(200, size // 2)
+    cos_d, sin_d, at = cuda(cos), cuda(sin), starts(lens)
+    x = r.standard_normal((at[-1], q_heads + 2 * heads, size)).astype(np.float32)
+    xd, pages, lens_d, offsets = cuda(x), cuda(w.table), int32(lens), int32(at)
+    q, k, over, k_back, v_back = sequence_of_calls(w.cache, xd, q_heads, pages, lens_d, offsets, cos_d, sin_d)
+    alone = tg.tst_attention(q, k, xd[:, q_heads + heads:], offsets)
+    position = np.concatenate([np.arange(n) for n in lens])
+    K, Q = (ref.rotate(x[:, a:b], position, cos, sin, False) for a, b in ((q_heads, q_heads + heads), (0, q_heads)))
+    for i, n in enumerate(lens):
+        w.ref.append("k", K[at[i]:at[i + 1]], w.table, i, 0)
+        w.ref.append("v", x[at[i]:at[i + 1], q_heads + heads:], w.table, i, 0)
+    w.assert_cache()
+    want, bound = prompt_reference(Q, K, x[:, q_heads + heads:], at, 0.125, "f32")
+    assert_within(alone, want, bound, "f32")
+    want, bound = reference_over_cache(w, Q, lens, at, 0.125, "f32")
+    assert_within(over, want, bound, "f32")
+    # what a code stands for is off by half a step, a largest entry of a block over 254: logits by 64 of them, results by as much of the values
+    assert (over - alone).abs().max() < 0.1
+    for step in range(20):
+        lens = [n + 1 for n in lens]
+        w.lens = lens
+        x = r.standard_normal((3, q_heads + 2 * heads, size)).astype(np.float32) * 1.5
+        q, k, over, *_ = sequence_of_calls(w.cache, cuda(x), q_heads, pages, int32(lens), None, cos_d, sin_d)
+        K, Q = (ref.rotate(x[:, a:b], np.array(lens) - 1, cos, sin, False) for a, b in ((q_heads, q_heads + heads), (0, q_heads)))
+        for i, n in enumerate(lens):
+            w.ref.append("k", K[i:i + 1], w.table, i, n - 1)
+            w.ref.append("v", x[i:i + 1, q_heads + heads:], w.table, i, n - 1)
+        w.assert_cache(f"step {step}")
+        want, bound = reference_over_cache(w, Q, [1] * 3, [0, 1, 2, 3], 0.125, "f32")
+        assert_within(over, want, bound, "f32")
+
+
+def test_from_a_graph_and_on_another_stream():
+    """Captured once, replayed as the sequences grow, with eager work between; the same on a stream that is given."""
+    heads, q_heads, size, page = 2, 8, 128, 16
+    start = [30, 500, 16]
+    worlds = [World([n + 8 for n in start], heads, size, page, 43) for _ in range(3)]
+    g = torch.Generator(device="cuda").manual_seed(43)
+    cos, sin = (cuda(t) for t in angles(600, size // 2))
+    x = torch.randn((3, q_heads + 2 * heads, size), generator=g, device="cuda").bfloat16()
+    pages, lens = cuda(worlds[0].table), int32([n + 1 for n in start])
+    offsets = int32([0, 3])
+    side = torch.cuda.Stream()
+
+    def eager(w, **kw):
+        return (*sequence_of_calls(w.cache, x, q_heads, pages, lens, None, cos, sin, **kw),
+                tg.tst_attention(x[:, :q_heads], x[:, q_heads:q_heads + heads], x[:, q_heads + heads:], offsets, **kw))
+
+    eager(worlds[0])
+    eager(worlds[1])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = eager(worlds[1])
+    for step in range(6):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        lens += 1
+        want = eager(worlds[0])
+        graph.replay()
+        side.wait_stream(torch.cuda.current_stream())
+        other = eager(worlds[2], stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        for a, b, c in zip(want, captured, other):
+            assert torch.equal(a, b) and (step == 0 or torch.equal(a, c))
+        if step == 0:      # the third cache has not had the first token
+            worlds[2].cache.k_codes.copy_(worlds[0].cache.k_codes)
+            worlds[2].cache.v_codes.copy_(worlds[0].cache.v_codes)
+            worlds[2].cache.k_scale.copy_(worlds[0].cache.k_scale)
+            worlds[2].cache.v_scale.copy_(worlds[0].cache.v_scale)
+        torch.randn((1000, 1000), device="cuda").sum().item()
+
+
+def test_two_graphs_that_share_a_workspace():
+    w = World([3000, 40], 1, 64, 64, 44)
+    pages, lens = w.arrays()
+    Q = [strided(queries(w, 2, 4, 64, s), "f16") for s in (44, 45)]
+    want = [tg.tst_kv_attention(q, w.cache, pages, lens) for q in Q]
+    ws, out, graphs = torch.empty(8 << 20, dtype=torch.uint8, device="cuda"), [torch.empty_like(q) for q in Q], []
+    for q, y in zip(Q, out):
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            tg.tst_kv_attention(q, w.cache, pages, lens, Y=y, workspace=ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for y in out:
+            y.zero_()
+        ws.fill_(255)
+        for graph in (*graphs, *graphs[::-1]):
+            graph.replay()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_same_results_both_ways(dtype, monkeypatch):
+    """Through the binding's native half and past it."""
+    from paper_2510_06957_amd import attention
+    heads, q_heads, size = 2, 4, 80
+    worlds = [World([65, 300, 9], heads, size, 32, 46) for _ in range(2)]
+    x = strided(rng(46, 2).standard_normal((6, q_heads + 2 * heads, size)), dtype)
+    pages, lens, offsets = cuda(worlds[0].table), int32([65, 300, 9]), int32([0, 3, 5, 6])
+    cos, sin = (cuda(t) for t in angles(300, 20))
+    assert attention._native is not None
+    a = sequence_of_calls(worlds[0].cache, x, q_heads, pages, lens, offsets, cos, sin)
+    a += (tg.tst_attention(x[:, :4], x[:, 4:6], x[:, 6:], offsets), tg.tst_attention(x[:, :4], x[:, 4:6], x[:, 6:], offsets, scale=0.2))
+    monkeypatch.setattr(attention, "_native", None)
+    b = sequence_of_calls(worlds[1].cache, x, q_heads, pages, lens, offsets, cos, sin)
+    b += (tg.tst_attention(x[:, :4], x[:, 4:6], x[:, 6:], offsets), tg.tst_attention(x[:, :4], x[:, 4:6], x[:, 6:], offsets, scale=0.2))
+    for s, t in zip(a, b):
+        assert torch.equal(s, t) and s.dtype == t.dtype
+    for s, t in zip(worlds[0].cache._tensors, worlds[1].cache._tensors):
+        assert torch.equal(s, t)
+
+
+def test_what_does_not_fit_is_refused():
+    w = World([40, 9], 2, 64, 16, 47)
+    pages, lens = w.arrays()
+    x = torch.zeros((2, 8, 64), device="cuda")
+    K, Q = x[:, :2], x[:, :4]
+    cos = torch.zeros((50, 32), device="cuda")
+    two = int32([0, 1, 2])
+    before = w.download()
+
+    def refused(call, *args, **kw):
+        with pytest.raises((ValueError, tg.TstgemmError)):
+            call(*args, **kw)
+
+    for bad in (K.cpu(), K.double(), K.to(torch.int8), x[:, :3], x[:1, :2], x[:, :2, :32], x[:, :2].transpose(1, 2), K[0], None):
+        refused(tg.tst_kv_append, w.cache, bad, K, pages, lens)
+        refused(tg.tst_kv_append, w.cache, K, bad, pages, lens)
+    for bad in (pages.long(), pages[0], pages[:, :0], pages.cpu(), pages.float(), pages.t().contiguous().t(), pages[:1], None):
+        refused(tg.tst_kv_append, w.cache, K, K, bad, lens)
+        refused(tg.tst_kv_attention, Q, w.cache, bad, lens)
+        refused(tg.tst_kv_read, w.cache, bad, lens, 2)
+    for bad in (lens.long(), lens[:1], lens.cpu(), torch.zeros(4, dtype=torch.int32, device="cuda")[::2], None):
+        refused(tg.tst_kv_append, w.cache, K, K, pages, bad)
+        refused(tg.tst_kv_attention, Q, w.cache, pages, bad)
+        refused(tg.tst_kv_read, w.cache, pages, bad, 2)
+    for bad in (two.long(), two[:2], two.cpu(), int32([0, 1, 2, 2])):
+        refused(tg.tst_kv_append, w.cache, K, K, pages, lens, bad)
+        refused(tg.tst_kv_attention, Q, w.cache, pages, lens, bad)
+        refused(tg.tst_kv_read, w.cache, pages, lens, 2, bad)
+    refused(tg.tst_kv_append, w.cache, K[:1], K[:1], pages, lens)          # a token for each sequence
+    refused(tg.tst_kv_append, None, K, K, pages, lens)
+    refused(tg.tst_kv_append, w.cache, K, K.bfloat16(), pages, lens)
+    for kw in (dict(Q=Q), dict(keys=True), dict(cos=cos), dict(sin=cos), dict(Q=Q, cos=cos, sin=cos[:, :31]), dict(Q=Q.half(), cos=cos, sin=cos), dict(Q=Q[:1], cos=cos, sin=cos),
+               dict(Q=Q[:, :, :32], cos=cos, sin=cos), dict(cos=cos.half(), sin=cos), dict(cos=torch.zeros((50, 33), device="cuda"), sin=torch.zeros((50, 33), device="cuda")),
+               dict(cos=cos[:, :0], sin=cos[:, :0]), dict(cos=cos[:0], sin=cos[:0]), dict(cos=cos[0], sin=cos[0])):
+        refused(tg.tst_kv_append, w.cache, K, K, pages, lens, **kw)
+    for bad in (x[:, :3], x[:, :4, :32], Q.double(), Q.cpu(), Q[:1], Q[0], None):
+        refused(tg.tst_kv_attention, bad, w.cache, pages, lens)
+    refused(tg.tst_kv_attention, Q, None, pages, lens)
+    for scale in (float("nan"), float("inf"), -float("inf")):
+        refused(tg.tst_kv_attention, Q, w.cache, pages, lens, scale=scale)
+        refused(tg.tst_attention, Q, K, K, two, scale=scale)
+    for Y in (Q.bfloat16(), Q[:1], torch.empty((4, 2, 64), device="cuda").transpose(0, 1), Q.cpu()):
+        refused(tg.tst_kv_attention, Q, w.cache, pages, lens, Y=Y)
+        refused(tg.tst_attention, Q, K, K, two, Y=Y)
+    refused(tg.tst_kv_read, w.cache, pages, lens, -1, two)
+    refused(tg.tst_kv_read, w.cache, pages, lens, 3)
+    refused(tg.tst_kv_read, w.cache, pages, lens, 2, dtype=torch.float64)
+    refused(tg.tst_kv_read, w.cache, pages, lens, (1 << 22) + 1, two)
+    for q, k, v in ((Q, K, x[:, :1]), (x[:, :3], K, K), (Q, K.half(), K), (Q, K, K.half()), (Q, K[:1], K[:1]), (Q, K[:, :, :32], K[:, :, :32]), (Q.cpu(), K, K), (Q, K, None), (Q[0], K, K)):
+        refused(tg.tst_attention, q, k, v, two)
+    for bad in (two.long(), two.cpu(), two[:0], two[None], [0, 2], torch.zeros(6, dtype=torch.int32, device="cuda")[::2]):
+        refused(tg.tst_attention, Q, K, K, bad)
+    wide = torch.zeros((2, 4, 257), device="cuda")
+    refused(tg.tst_attention, wide, wide, wide, two)
+    neg = torch._neg_view(K)
+    refused(tg.tst_kv_append, w.cache, neg, K, pages, lens)
+    refused(tg.tst_attention, Q, neg, K, two)
+    for bad in (dict(pages=0), dict(page=17), dict(page=8), dict(page=512), dict(heads=0), dict(heads=1025), dict(head_size=0), dict(head_size=257)):
+        refused(tg.tst_kv_cache, **{**dict(pages=2, page=16, heads=1, head_size=8), **bad})
+    c = w.cache
+    for bad in ((c.k_codes[:1], c.v_codes, c.k_scale, c.v_scale), (c.k_codes, c.k_codes, c.k_scale, c.v_scale), (c.k_codes.float(), c.v_codes, c.k_scale, c.v_scale),
+                (c.k_codes, c.v_codes, c.k_scale[:1], c.v_scale), (c.k_codes, c.v_codes, c.k_scale, c.v_scale.double()), (c.k_codes, c.v_codes, c.k_scale, None)):
+        refused(tg.KvCache, 16, 64, *bad)
+    refused(tg.KvCache, 32, 64, *c._tensors)
+    refused(tg.KvCache, 16, 65, *c._tensors)
+    torch.cuda.synchronize()
+    after = w.download()
+    for name in "kv":
+        same(after[name][0], before[name][0])
+        same(after[name][1], before[name][1])
