@@ -27,6 +27,7 @@ extern "C" {
 #define TST_MAX_SEQUENCES (1 << 20)
 #define TST_MAX_TOKENS (1 << 22) /* rows of packed operands */
 #define TST_MAX_ROWS (1 << 27)   /* rows x query heads */
+#define TST_MAX_SEQUENCE_HEADS (1 << 22) /* sequences x heads of keys, of tst_attention (a grid counts no more) */
 
 /*
  * A cache of one layer: `pages` pages of page_tokens tokens.  A code q in a block of 16 tokens of a head stands for q * scale.
@@ -125,8 +126,9 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
  * Causal attention over whole prompts: rows offsets[i] .. offsets[i + 1] - 1 are sequence i; its row p, head h, sees keys of rows 0 .. p of the sequence,
  * head h / (q_heads / heads), as above.  offsets: DEVICE, sequences + 1, ascending.  Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Rows outside the sequences
  * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 and 24 for fp32 in the second product, sums are fp32.
- * What a row does not see does not touch it, infinities and NaN among it; a row that holds or sees one that matters is NaN or infinite.
- * Errors: EINVAL, EHIP.
+ * What a row does not see does not touch it, infinities and NaN among it.  A row of Q that holds one is NaN or infinite, and so is a row that sees one in a key (but for keys
+ * whose logit is -infinity, which weigh nothing) and a channel of a row that sees one in that channel of a value.
+ * tokens * q_heads <= 2^27, sequences * heads <= 2^22.  Errors: EINVAL, EHIP.
  */
 int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t *V, int type, int q_heads, int heads, int head_size, const int32_t *offsets,
                   int sequences, int tokens, float scale, void *Y, void *stream);

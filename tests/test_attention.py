@@ -135,6 +135,7 @@ def test_refusals_of_attention():
                  (10, float("nan")), (10, float("-inf")), (11, None), (11, a + 1)):
         assert lib.tst_attention(*ok[:i], v, *ok[i + 1:]) == EINVAL, i
     assert lib.tst_attention(ref(q), ref(q), ref(q), 1, 64, 2, 64, a, 1, 1 << 22, 0.5, a, None) == EINVAL           # rows x heads
+    assert lib.tst_attention(ref(q), ref(q), ref(q), 1, 1024, 1024, 64, a, 4097, 5, 0.5, a, None) == EINVAL         # sequences x heads
     for i in (8, 9):
         args = [None, None, None, 1, 4, 2, 64, None, 1, 5, 0.5, None, None]
         args[i] = 0
