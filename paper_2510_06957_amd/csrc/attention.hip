@@ -132,17 +132,19 @@ __device__ __forceinline__ float across_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// How rows are read and dealt: anywhere, an entry at a time; on 16-byte borders; so, and few of them, in tiles of half the rows.
-enum Way { kAny, kFast, kFew };
+// How rows are read and dealt: anywhere, an entry at a time; on 16-byte borders; so, and few of them, in tiles of half the rows; so few that several wavefronts share
+// the keys of the same rows and join their sums at the end.
+enum Way { kAny, kFast, kFew, kShared };
 template <int TYPE, int ROW, int WAY> struct Shape {
     static constexpr int kPlanes = Planes<TYPE>::kCount;
-    static constexpr bool kAhead = WAY != kAny && TYPE != TST_F32;      // the next keys' logits beside these keys' weights
-    static constexpr int kWaves = kAhead && WAY == kFast && ROW <= 128 ? 8 : 4;   // two for a SIMD where their registers fit
-    static constexpr int kOccupancy = kAhead && ROW <= 64 ? 4 : kAhead && ROW <= 128 ? 2 : 1;
-    static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;      // of a tile
-    static constexpr int kKeys = kAhead && WAY == kFast && ROW <= 128 ? 64 : 32;            // of a tile in the LDS
+    static constexpr bool kAhead = (WAY == kFast || WAY == kFew) && TYPE != TST_F32;      // the next keys' logits beside these keys' weights
+    static constexpr int kGroups = WAY != kShared ? 1 : TYPE == TST_F32 ? 2 : 4;           // wavefronts that share the keys of 32 rows
+    static constexpr int kWaves = (kAhead && WAY == kFast && ROW <= 128) || (WAY == kShared && TYPE != TST_F32) ? 8 : 4;   // two for a SIMD where their registers fit
+    static constexpr int kOccupancy = kAhead && ROW <= 64 ? 4 : (kAhead || (WAY == kShared && TYPE != TST_F32)) && ROW <= 128 ? 2 : 1;
+    static constexpr int kThreads = 64 * kWaves, kRows = 32 * (kWaves / kGroups);          // of a tile
+    static constexpr int kKeys = kAhead && WAY == kFast && ROW <= 128 ? 64 : 32 * kGroups;  // of a tile in the LDS
     // (kAhead: K's next tile is read while another wavefront still reads this one, and K is stored a tile ahead)
-    static constexpr int kBuffersK = kAhead ? 3 : ROW <= 128 ? 2 : 1, kBuffersV = kAhead || ROW <= 128 ? 2 : 1;
+    static constexpr int kOfPlain = ROW <= 128 && (kGroups == 1 || TYPE != TST_F32) ? 2 : 1, kBuffersK = kAhead ? 3 : kOfPlain, kBuffersV = kAhead ? 2 : kOfPlain;
     // bytes from key to key: 16 rows of keys, and 4 rows of 32 channels of values, fall into different banks
     static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + (ROW % 128 == 96 ? 0 : 64);
     static constexpr int kPlaneK = kKeys * kStrideK, kPlaneV = kKeys * kStrideV;
@@ -262,11 +264,12 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
     typedef Shape<TYPE, ROW, WAY> S;
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int P = S::kPlanes, kSteps = ROW / 16, kTiles = ROW / 32, kSub = S::kKeys / 32;   // 32 keys at a time
-    __shared__ __attribute__((aligned(16))) char lds_k[S::kBuffersK * S::kBufferK];
-    __shared__ __attribute__((aligned(16))) char lds_v[S::kBuffersV * S::kBufferV];
+    __shared__ __attribute__((aligned(16))) char lds_k[S::kBuffersK * S::kBufferK + S::kBuffersV * S::kBufferV];
+    char *const lds_v = lds_k + S::kBuffersK * S::kBufferK;
     __shared__ int spoilt[ROW];   // the first key whose value of the channel is not finite, among the keys that some of the tile's rows do not see
     __shared__ int any_spoilt;
-    const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+    const int wave = uniform(threadIdx.x / 64) % (S::kWaves / S::kGroups), sharer = uniform(threadIdx.x / 64) / (S::kWaves / S::kGroups);   // of its rows; of those with the same
+    const int lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
     const int head = blockIdx.x % a.heads;
     const Place place = place_of(a, S::kRows, (int)(blockIdx.x / a.heads));
     if (place.tile < 0) return;
@@ -422,8 +425,8 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
         for (int kt = 0; kt < tiles; ++kt) {
             if (kt + 1 < tiles) load_k(kt + 1), load_v(kt + 1);
 #pragma unroll
-            for (int s = 0; s < kSub; ++s) {
-                const int sub = kt * kSub + s;
+            for (int s = 0; s < kSub / S::kGroups; ++s) {
+                const int sub = kt * kSub + s * S::kGroups + sharer;
                 if (sub < own) {
                     f32x16 z;
                     Weights w;
@@ -494,9 +497,49 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
         }
     }
 
+    sum = across_sum(sum);
+    if constexpr (S::kGroups > 1) {
+        // sharers' sums, relative to their own bases, through the LDS that held the tiles
+        constexpr int kOthers = (S::kGroups - 1) * (S::kWaves / S::kGroups);
+        static_assert(kOthers * 64 * (kTiles * 64 + 8) <= (int)sizeof(lds_k), "sums fit where tiles were");
+        f32x4 *sums = reinterpret_cast<f32x4 *>(lds_k);
+        float2 *states = reinterpret_cast<float2 *>(sums + kOthers * kTiles * 4 * 64);
+        if (sharer > 0) {
+            const int slot = (sharer - 1) * (S::kWaves / S::kGroups) + wave;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) sums[((slot * kTiles + t) * 4 + r / 4) * 64 + lane] = f32x4{o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]};
+            states[slot * 64 + lane] = float2{base, sum};
+        }
+        __syncthreads();
+        if (sharer > 0) return;
+        float all = base;
+#pragma unroll
+        for (int i = 1; i < S::kGroups; ++i) all = fmaxf(all, states[((i - 1) * (S::kWaves / S::kGroups) + wave) * 64 + lane].x);
+        const float from = all == -INFINITY ? 0.f : all, mine = __builtin_amdgcn_exp2f(base - from);
+        sum *= mine;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) o[t] *= mine;
+#pragma unroll
+        for (int i = 1; i < S::kGroups; ++i) {
+            const int slot = (i - 1) * (S::kWaves / S::kGroups) + wave;
+            const float2 state = states[slot * 64 + lane];
+            const float w = __builtin_amdgcn_exp2f(state.x - from);
+            sum += w * state.y;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 v = sums[((slot * kTiles + t) * 4 + r / 4) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][r + e] += w * v[e];
+                }
+        }
+    }
     if (!there) return;
     const bool bad = any_spoilt;
-    const float inverse = 1.f / across_sum(sum);
+    const float inverse = 1.f / sum;
     Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(first + token) * a.q_heads + q_head) * a.size;
     const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
 #pragma unroll
@@ -551,13 +594,29 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                 tst::k_attention<TYPE, ROW, WAY><<<(unsigned)a.tiles * heads, S::kThreads, 0, st>>>(a);
             };
             if (!a.wide || a.k.token > 1 << 24 || a.v.token > 1 << 24) launch(std::integral_constant<int, tst::kAny>{});
-            else if constexpr (TYPE != TST_F32 && ROW <= 128) {
-                // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole, 32 heads of
-                // 128, 8 of keys: 256 tokens 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149)
-                const int64_t whole = (int64_t)tokens * group / tst::Shape<TYPE, ROW, tst::kFast>::kRows * heads;
-                if (2 * whole < 3 * tst::compute_units()) launch(std::integral_constant<int, tst::kFew>{});
-                else launch(std::integral_constant<int, tst::kFast>{});
-            } else launch(std::integral_constant<int, tst::kFast>{});
+            else {
+                const int64_t whole = (int64_t)tokens * group / tst::Shape<TYPE, ROW, tst::kFast>::kRows * heads;   // tiles
+                if constexpr (ROW <= 128) {
+                    // Rows whose keys are shared, where there are fewer tiles than compute units (fp32, whose tiles are half as large: than twice as many) and keys to share.  us, shared
+                    // and not, 32 heads of 128, 8 of keys: bf16 256 tokens 14.9 and 15.8, 512 18.7 and 22.2 (heads of 64 12.0 and 16.8), 1024 36.3 and 35.0, 64 12.6 and 10.7;
+                    // fp32 32 tokens 11.7 and 11.7, 256 26 and 33, 1024 86 and 103, 2048 291 and 217; bf16 512 tokens, heads of 256 60 and 46
+                    const bool few = TYPE == TST_F32 ? whole < 2 * tst::compute_units() && tokens > 32 * (int64_t)sequences
+                                                     : whole < tst::compute_units() && tokens > 128 * (int64_t)sequences;
+                    if (few) {
+                        launch(std::integral_constant<int, tst::kShared>{});
+                        return hipGetLastError();
+                    }
+                }
+                if constexpr (TYPE != TST_F32 && ROW <= 128) {
+                    // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole: 256 tokens
+                    // 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149)
+                    if (2 * whole < 3 * tst::compute_units()) {
+                        launch(std::integral_constant<int, tst::kFew>{});
+                        return hipGetLastError();
+                    }
+                }
+                launch(std::integral_constant<int, tst::kFast>{});
+            }
             return hipGetLastError();
         });
     }));

@@ -402,6 +402,14 @@ def test_prompts_of_many_sequences():
         check_prompt(lens, 2, 1, 64, "bf16", 26)
 
 
+@pytest.mark.parametrize("lens,q_heads,heads,size", [([700], 3, 1, 64), ([129, 300, 161], 4, 2, 80), ([1030, 1], 1, 1, 128), ([400] * 3, 7, 1, 100), ([33, 66], 2, 2, 128)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_prompts_whose_keys_are_shared(lens, q_heads, heads, size, dtype):
+    """Few rows and many keys."""
+    check_prompt(lens, q_heads, heads, size, dtype, 30)
+    check_prompt(lens, q_heads, heads, size, dtype, 30, scale=1.5)
+
+
 @pytest.mark.parametrize("q_heads,heads,size,dtype", [(64, 8, 64, "bf16"), (64, 8, 96, "f16"), (64, 16, 128, "bf16"), (66, 2, 128, "f16"), (64, 64, 64, "f16"), (64, 8, 80, "bf16"),
                                                       (64, 4, 192, "bf16"), (32, 8, 256, "f16")])
 def test_prompts_in_whole_tiles(q_heads, heads, size, dtype):
@@ -422,7 +430,7 @@ def test_prompts_in_whole_tiles(q_heads, heads, size, dtype):
         assert torch.allclose(alone.float(), Y[a:b].float(), rtol=8 * LAST[dtype], atol=0.02)
 
 
-@pytest.mark.parametrize("q_heads,lens", [(4, [90, 40]), (64, [1217, 64])])
+@pytest.mark.parametrize("q_heads,lens", [(4, [90, 40]), (4, [300, 77]), (64, [1217, 64])])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_prompts_what_a_row_does_not_see_does_not_touch_it(dtype, q_heads, lens):
     """Infinities and NaN in keys and values behind a row, in other sequences and in rows of no sequence."""
