@@ -9,8 +9,8 @@
 // cut into fp16 (11 bits, and 11 more in a second plane for fp32).  Weights meet a value's scale relative to the largest seen so far, times 2^15: with 11 bits (22 for
 // fp32) down to 2^-29 of the largest, an absolute 2^-40 of it below.  Sums are fp32.
 //
-// The keys of a sequence are cut into chunks of one length, found from all sequences' lengths on the device so that the workgroups have about as much to do
-// each whatever the batch is; the host knows how many there are at most.  Chunks of one tile of rows are joined by k_join.
+// The keys of a long sequence are cut into equal chunks, about as long as those of the others: the device finds the length from the lengths of all sequences, so that
+// the workgroups have about as much to do each whatever the batch is, and the host knows how many there are at most.  k_kv_join joins the chunks of a tile of rows.
 #include "attention_internal.h"
 
 namespace tst {
@@ -71,8 +71,8 @@ __device__ __forceinline__ int64_t lane_of(int64_t v, int lane)
 }
 __device__ __forceinline__ int64_t wave_sum(int64_t v) { return lane_of(wave_scan(v), 63); }
 
-// The length of chunks, in units of 64 tokens: all of them in a.parts equal ones, and up to one more for each tile.  Whole rounds of the four wavefronts.  Every wavefront
-// of the call comes to the same length, which is no shorter than that.
+// About how long chunks are, in units of 64 tokens: all of them in a.parts equal ones.  Whole rounds of the four wavefronts.  Every wavefront of the call comes to the
+// same length, which is no shorter than that.
 template <int ROWS> __device__ __forceinline__ int chunk_length(const KvArgs &a)
 {
     int64_t all = 0;
@@ -81,7 +81,8 @@ template <int ROWS> __device__ __forceinline__ int chunk_length(const KvArgs &a)
     return ((int)fminf(length, 1 << 30) + kWaves - 1) / kWaves * kWaves;
 }
 
-__device__ __forceinline__ int chunks_of(const KvArgs &a, int i, int length) { return max((int)((unsigned)(units_of(a, i) + length - 1) / (unsigned)length), 1); }
+// A sequence is cut into so many equal chunks that they come nearest to that length: at most a.parts and one for each tile in all.
+__device__ __forceinline__ int chunks_of(const KvArgs &a, int i, int length) { return max((int)((unsigned)(units_of(a, i) + length / 2) / (unsigned)length), 1); }
 
 // Item `at`: sequences in order, a sequence's tiles in order, a tile's chunks in order.  seq -1: there are fewer.
 struct Item {
@@ -227,8 +228,9 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         const int length = uniform(chunk_length<16 * RT>(a));
         it = find_item<16 * RT>(a, length, blockIdx.x);
         if (it.seq < 0) return;
-        begin = it.chunk * length;
-        end = min(begin + length, units_of(a, it.seq));
+        const unsigned units = units_of(a, it.seq);   // at most 2^16 + 1, in a quarter as many chunks
+        begin = units * it.chunk / it.chunks;
+        end = units * (it.chunk + 1) / it.chunks;
     } else {
         const Slot slot = find_slot<16 * RT>(a, blockIdx.x);
         if (slot.tile < 0) return;
@@ -540,9 +542,13 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     }
 }
 
-// How a call is cut: the sequences of a head into about as many chunks as the card holds workgroups of it, so that all have as much to do, where these are more than twice
-// the tiles; else into three times as many, since the ends of sequences make them uneven and a second and third turn fill what the first leaves.  (us, once and three times as
-// many: 1 x 131072 tokens 61.6 and 71.5, 64 sequences of up to 8192 105 and 99.)
+// How a call is cut.  To know the chunks every workgroup reads all lengths, and their sums make a second launch: 5 us and more, which short sequences do not give back.
+// No sequence of at most kShort units is cut, and none of up to kMiddle where the tiles of all heads are enough to share the card in turns (us, cut and whole, 32 query and 8
+// key heads of 128, sequences x tokens of the table: 1 x 500 12.5 and 9.5, 64 x 2000 36.9 and 30.0, 128 x 2000 62.5 and 52.7, 64 x 4000 55.7 and 55.4, 8 x 4000 19.8 and 28.2,
+// 64 x 8000 88 and 101, 16 x 16000 48 and 102).  Else the sequences of a head are cut into about as many chunks as the card holds workgroups of it where these are more than
+// twice the tiles, and into twice as many where not, since lengths are uneven and a second turn fills what the first leaves (once, twice and three times: 64 sequences of up to
+// 8192 96.0, 90.2 and 91.2; 8 of 8000 in 32 rows each 88, 82 and 87; 64 of 8000 alike 188, 199 and 205).
+constexpr int kShort = 32, kMiddle = 80;
 struct Cut {
     int row_tiles, parts;
     int64_t tiles, items;   // of a head, at most
@@ -557,7 +563,8 @@ Cut cut_of(const tst_kv_cache_t *c, const tst_sequences_t *s, int q_heads)
     k.tiles = rows / (16 * k.row_tiles) + s->sequences;
     const int slots = blocks_of((row * k.row_tiles <= 128 ? 2 : 1) * compute_units(), c->heads);   // by the kernels' registers
     const int64_t longest = ((int64_t)s->columns * c->page_tokens + kUnit) / kUnit;   // units that a sequence can have
-    if (s->sequences <= 1024 && k.tiles <= 16 * (int64_t)slots && longest > kWaves) k.parts = 2 * k.tiles > slots ? 3 * slots : slots;
+    const bool whole = longest <= kShort || (longest <= kMiddle && 3 * longest <= k.tiles * c->heads);
+    if (s->sequences <= 1024 && k.tiles <= 16 * (int64_t)slots && !whole) k.parts = 2 * k.tiles > slots ? 2 * slots : slots;
     k.items = k.tiles + k.parts;
     const size_t states = (size_t)k.items * c->heads * k.row_tiles * 16;
     k.states = k.parts ? round256(states * row * sizeof(float)) : 0;

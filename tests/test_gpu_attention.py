@@ -292,6 +292,11 @@ def queries(w, T, q_heads, size, seed, large=1.0):
     return rng(seed, T, q_heads).standard_normal((T, q_heads, size)) * large
 
 
+def with_room(pages, page):
+    """The table with columns for 16384 tokens more: sequences that may be as long as that are cut into chunks."""
+    return torch.cat([pages, torch.full((pages.shape[0], 16384 // page), -1, dtype=torch.int32, device="cuda")], 1)
+
+
 def check_over_cache(lens, new, q_heads, heads, size, page, dtype, seed, large=1.0, gap=0, scale=None, columns=None, **kw):
     w = World(lens, heads, size, page, seed, columns=columns)
     at = starts(new)
@@ -304,6 +309,8 @@ def check_over_cache(lens, new, q_heads, heads, size, page, dtype, seed, large=1
     want, bound = reference_over_cache(w, f32(Qd), new, at, 1 / math.sqrt(size) if scale is None else scale, dtype)
     assert_within(Y, want, bound, dtype, f"lens {lens[:6]} new {new[:6]}")
     assert torch.equal(tg.tst_kv_attention(Qd, w.cache, pages, lens_d, offsets, scale=scale, **kw), Y)
+    for _ in range(2):
+        assert_within(tg.tst_kv_attention(Qd, w.cache, with_room(pages, page), lens_d, offsets, scale=scale, **kw), want, bound, dtype, f"cut: lens {lens[:6]} new {new[:6]}")
     return w, Qd, Y
 
 
@@ -492,9 +499,10 @@ def test_attention_over_long_caches(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-def test_attention_over_the_cache_scales_of_blocks(dtype):
+@pytest.mark.parametrize("columns", [100, 1000])
+def test_attention_over_the_cache_scales_of_blocks(dtype, columns):
     """Scales of values and keys that differ by many powers of ten between blocks; blocks of zeros."""
-    w = World([1500, 333], 2, 64, 32, 36)
+    w = World([1500, 333], 2, 64, 32, 36, columns=columns)
     for name, spread in (("k", 3), ("v", 12)):
         w.ref.scale[name] *= (10.0 ** w.r.integers(-spread, 2, w.ref.scale[name].shape)).astype(np.float32)
         w.ref.scale[name][w.r.random(w.ref.scale[name].shape) < 0.1] = 0
@@ -509,9 +517,10 @@ def test_attention_over_the_cache_scales_of_blocks(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_attention_over_the_cache_what_a_row_does_not_see(dtype):
+@pytest.mark.parametrize("columns", [100, 1000])
+def test_attention_over_the_cache_what_a_row_does_not_see(dtype, columns):
     """Blocks without a scale behind a row; rows that see one, or whose query is none, are NaN."""
-    w = World([700, 90, 350], 2, 64, 16, 37)
+    w = World([700, 90, 350], 2, 64, 16, 37, columns=columns)
     new = [40, 1, 3]
     at = starts(new)
     Qd = strided(queries(w, at[-1], 4, 64, 37), dtype)
@@ -538,9 +547,10 @@ def test_attention_over_the_cache_what_a_row_does_not_see(dtype):
     assert torch.equal(Y, clean)
 
 
-def test_attention_over_the_cache_where_there_are_no_pages():
+@pytest.mark.parametrize("columns", [30, 1000])
+def test_attention_over_the_cache_where_there_are_no_pages(columns):
     """Pages that are none of the cache's make the rows that see them NaN, and so do positions behind the table; rows of negative positions see nothing."""
-    w = World([400, 70, 33, 20], 2, 64, 16, 38, columns=30)
+    w = World([400, 70, 33, 20], 2, 64, 16, 38, columns=columns)
     w.table[0, 23], w.table[1, 0], w.table[2, 2] = w.ref.pages, -7, 2 ** 31 - 1
     new = [40, 2, 1, 24]
     at = starts(new)
@@ -553,7 +563,7 @@ def test_attention_over_the_cache_where_there_are_no_pages():
     assert_within(Y[good], want[good], bound[good], "f32")
     assert (Y[at[3]:at[3] + 4] == 0).all()
     assert torch.isnan(Y[8:at[3]]).all()
-    lens[:] = torch.tensor([2 ** 31 - 1, 481, -5, -2 ** 31], dtype=torch.int32)     # the table holds 480
+    lens[:] = torch.tensor([2 ** 31 - 1, 16 * columns + 1, -5, -2 ** 31], dtype=torch.int32)     # one more than the table holds
     w.table[:] = w.r.integers(0, w.ref.pages, w.table.shape)
     Y = tg.tst_kv_attention(Qd, w.cache, cuda(w.table), lens, int32(at))
     assert torch.isnan(Y[:40]).all() and torch.isnan(Y[41]).all() and torch.isfinite(Y[40]).all() and (Y[42:] == 0).all()
@@ -564,7 +574,7 @@ def test_attention_over_the_cache_where_there_are_no_pages():
 
 
 def test_attention_over_the_cache_leaves_other_rows_as_they_are():
-    w = World([300, 50], 1, 64, 16, 39)
+    w = World([300, 50], 1, 64, 16, 39, columns=1000)     # room for sequences that are cut, which needs a workspace
     Qd = strided(queries(w, 12, 2, 64, 39), "bf16")
     pages, lens = w.arrays()
     Y = torch.full((12, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
@@ -667,11 +677,12 @@ def test_a_prompt_and_what_follows_it():
         assert_within(over, want, bound, "f32")
 
 
-def test_from_a_graph_and_on_another_stream():
+@pytest.mark.parametrize("columns", [40, 1000])
+def test_from_a_graph_and_on_another_stream(columns):
     """Captured once, replayed as the sequences grow, with eager work between; the same on a stream that is given."""
     heads, q_heads, size, page = 2, 8, 128, 16
     start = [30, 500, 16]
-    worlds = [World([n + 8 for n in start], heads, size, page, 43) for _ in range(3)]
+    worlds = [World([n + 8 for n in start], heads, size, page, 43, columns=columns) for _ in range(3)]
     g = torch.Generator(device="cuda").manual_seed(43)
     cos, sin = (cuda(t) for t in angles(600, size // 2))
     x = torch.randn((3, q_heads + 2 * heads, size), generator=g, device="cuda").bfloat16()
