@@ -228,9 +228,9 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         const int length = uniform(chunk_length<16 * RT>(a));
         it = find_item<16 * RT>(a, length, blockIdx.x);
         if (it.seq < 0) return;
-        const unsigned units = units_of(a, it.seq);   // at most 2^16 + 1, in a quarter as many chunks
-        begin = units * it.chunk / it.chunks;
-        end = units * (it.chunk + 1) / it.chunks;
+        const int units = units_of(a, it.seq), each = (unsigned)units / (unsigned)it.chunks, longer = units - each * it.chunks;   // the first ones by a unit
+        begin = it.chunk * each + min(it.chunk, longer);
+        end = begin + each + (it.chunk < longer);
     } else {
         const Slot slot = find_slot<16 * RT>(a, blockIdx.x);
         if (slot.tile < 0) return;

@@ -608,6 +608,21 @@ def test_a_cache_of_more_than_4_gib():
     assert (out[0][0].float() - K.float()).abs().max() < 0.05
 
 
+def test_sequences_of_2_30_tokens():
+    """As long as a table can be, over pages that repeat: keys all alike, so that a result says how many tokens of either value were seen."""
+    cache = tg.tst_kv_cache(2, 256, 1, 64)
+    cache.v_codes[0], cache.v_codes[1] = 100, -30
+    cache.v_scale.fill_(1.0)
+    columns = (1 << 30) // 256
+    page = torch.zeros((3, columns), dtype=torch.int32, device="cuda")
+    page[0, columns // 2:], page[1, columns // 8:], page[2, columns - columns // 8:] = 1, 1, 1
+    Y = tg.tst_kv_attention(torch.ones((3, 2, 64), device="cuda"), cache, page, int32([1 << 30, 1 << 30, (1 << 30) - 77]))
+    # a quarter of a chunk (a 170th of a sequence) adds 2^16 products of 32 tokens at most, each rounded by 2^-24 of a sum whose magnitude is below 100 for each token: 2^-8 of 100,
+    # and as much of the weights
+    for y, want in zip(f32(Y), (35.0, -30 + 130 / 8, 100 - 130 / 8)):
+        assert (np.abs(y - want) <= 2.0 ** -7 * 100).all()
+
+
 def test_views_that_start_far_into_large_tensors():
     """Rows, heads and pages at offsets behind 2^31 entries."""
     big = torch.zeros((3, 1 << 30), dtype=torch.bfloat16, device="cuda")
