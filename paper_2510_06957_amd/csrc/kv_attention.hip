@@ -456,7 +456,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         for (int w = 0; w < kWaves; ++w) total[rt] += states[w][rt][m16].y * weight_of(states[w][rt][m16].x, all[rt]);
         const float times = weight_of(most[rt], all[rt]) * (reference[rt] * (1.f / S::kShift));
 #pragma unroll
-        for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = times == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rt][dt] * times;
+        for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;   // (a NaN of a row whose weights here are nothing beside others stays one)
     }
 #pragma unroll
     for (int half = kWaves / 2; half; half >>= 1) {
@@ -522,7 +522,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
             const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
             const float w = weight_of(s.x, all);
             total += w * s.y;
-            o += w != 0.f ? w * v : f32x4{0.f, 0.f, 0.f, 0.f};
+            o += w * v;
         }
         if (share) {
             shared[wave][lane] = o;

@@ -547,6 +547,28 @@ def test_attention_over_the_cache_what_a_row_does_not_see(dtype, columns):
     assert torch.equal(Y, clean)
 
 
+@pytest.mark.parametrize("columns", [100, 1000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_over_the_cache_blocks_without_a_scale_whose_tokens_weigh_nothing(dtype, columns):
+    """A row that sees one is NaN however far below others its logits lie, also where another wavefront or chunk has those."""
+    w = World([1500], 1, 64, 16, 49, columns=columns)
+    pages, lens = w.arrays()
+    Qd = strided(np.ones((1, 2, 64)), dtype)
+    w.ref.codes["k"][w.table[0, 60]] = 127
+    w.ref.scale["k"][w.table[0, 60]] = 100.0       # logits of 0.125 * 64 * 12700; the others' are below 130
+    w.upload()
+    want = f32(tg.tst_kv_attention(Qd, w.cache, pages, lens))
+    assert np.isfinite(want).all()
+    for block in (0, 3, 61, 70, 93):
+        w.ref.scale["v"][w.table[0, block]] = np.nan
+        w.upload()
+        assert torch.isnan(tg.tst_kv_attention(Qd, w.cache, pages, lens)).all(), block
+        w.ref.scale["v"][w.table[0, block]] = 1.0
+        w.upload()
+        # the scale of a block changes what weights are relative to, and so how each is rounded, here and before: twice half a step of values of at most 127 * 1.5 / 64
+        assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens), want, np.full(want.shape, 2 * WEIGHT[dtype] * 127 * 1.5 / 64), dtype, block)
+
+
 @pytest.mark.parametrize("columns", [30, 1000])
 def test_attention_over_the_cache_where_there_are_no_pages(columns):
     """Pages that are none of the cache's make the rows that see them NaN, and so do positions behind the table; rows of negative positions see nothing."""
