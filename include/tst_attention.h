@@ -111,7 +111,7 @@ int tst_kv_read(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, i
 /*
  * Attention over the cache: the row of Q at position p of its sequence, head h, sees the keys of head h / (q_heads / heads) at positions 0 .. p:
  *   Y = sum_j w_j v_j / sum_j w_j,   w_j = e^(scale q.k_j - max)
- * with the values that codes stand for.  The new tokens have been appended before.  A row that sees nothing is zeros.
+ * with the values that codes stand for; |scale| <= 2^127.  The new tokens have been appended before.  A row that sees nothing is zeros.
  * q_heads: a multiple of the cache's heads, at most 1024 of them, tokens * q_heads <= 2^27; Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Queries keep 22 bits or those of their type
  * relative to the largest of their row, weights 11 bits in 16-bit types and 22 in fp32.
  * A row of Q that holds an infinity or a NaN is NaN, and so is a row that sees a block whose scale is none.
@@ -128,7 +128,7 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
  * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 and 24 for fp32 in the second product, sums are fp32.
  * What a row does not see does not touch it, infinities and NaN among it.  A row of Q that holds one is NaN or infinite, and so is a row that sees one in a key (but for keys
  * whose logit is -infinity, which weigh nothing) and a channel of a row that sees one in that channel of a value.
- * tokens * q_heads <= 2^27, sequences * heads <= 2^22.  Errors: EINVAL, EHIP.
+ * tokens * q_heads <= 2^27, sequences * heads <= 2^22, |scale| <= 2^127.  Errors: EINVAL, EHIP.
  */
 int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t *V, int type, int q_heads, int heads, int head_size, const int32_t *offsets,
                   int sequences, int tokens, float scale, void *Y, void *stream);

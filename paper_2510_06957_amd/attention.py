@@ -205,8 +205,8 @@ def tst_kv_read(cache: KvCache, pages, lens, tokens: int, offsets=None, dtype=No
 
 def _scale(scale, size):
     scale = 1 / math.sqrt(size) if scale is None else float(scale)
-    if not math.isfinite(scale):
-        raise ValueError("scale must be finite")
+    if not abs(scale) <= 2.0 ** 127:
+        raise ValueError("scale must be finite, and no more than 2^127")
     return scale
 
 

@@ -575,7 +575,7 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                   int sequences, int tokens, float scale, void *Y, void *stream)
 {
     if (!tst::type_ok(type) || heads < 1 || q_heads < heads || q_heads > TST_MAX_HEADS || q_heads % heads || head_size < 1 || head_size > TST_MAX_HEAD_SIZE || sequences < 0 ||
-        sequences > TST_MAX_SEQUENCES || tokens < 0 || tokens > TST_MAX_TOKENS || (int64_t)tokens * q_heads > TST_MAX_ROWS || (int64_t)sequences * heads > TST_MAX_SEQUENCE_HEADS || !(scale - scale == 0.f))
+        sequences > TST_MAX_SEQUENCES || tokens < 0 || tokens > TST_MAX_TOKENS || (int64_t)tokens * q_heads > TST_MAX_ROWS || (int64_t)sequences * heads > TST_MAX_SEQUENCE_HEADS || !tst::scale_ok(scale))
         return TSTGEMM_EINVAL;
     if (sequences == 0 || tokens == 0) return TSTGEMM_OK;
     if (!tst::rows_ok(Q, type) || !tst::rows_ok(K, type) || !tst::rows_ok(V, type) || !offsets || !tst::aligned(offsets, 4) || !Y || !tst::aligned(Y, tst::type_bytes(type)))

@@ -42,6 +42,7 @@ struct Rows {
 int check_cache(const tst_kv_cache_t *c);                              // TSTGEMM_OK or EINVAL (kv_cache.hip)
 int check_sequences(const tst_kv_cache_t *c, const tst_sequences_t *s);
 bool rows_ok(const tst_heads_t *x, int type);
+inline bool scale_ok(float scale) { return scale <= 0x1p127f && scale >= -0x1p127f; }   // times log2 e it is finite
 inline Cache cache_of(const tst_kv_cache_t *c)
 {
     return Cache{c->k_codes, c->v_codes, c->k_scale, c->v_scale, c->pages, __builtin_ctz((unsigned)c->page_tokens), c->heads, c->head_size};

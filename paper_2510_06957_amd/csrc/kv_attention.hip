@@ -591,7 +591,7 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
 {
     size_t need = 0;
     if (int rc = tst_kv_attention_workspace_bytes(cache, sequences, q_heads, &need)) return rc;
-    if (!tst::type_ok(type) || !(scale - scale == 0.f)) return TSTGEMM_EINVAL;
+    if (!tst::type_ok(type) || !tst::scale_ok(scale)) return TSTGEMM_EINVAL;
     if (sequences->sequences == 0 || sequences->tokens == 0) return TSTGEMM_OK;
     if (!tst::rows_ok(Q, type) || !Y || !tst::aligned(Y, tst::type_bytes(type))) return TSTGEMM_EINVAL;
     if (need && (!workspace || workspace_bytes < need)) return TSTGEMM_EWORKSPACE;

@@ -187,7 +187,7 @@ PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Call c(a[1], a[2], a[3], a[4], qt->size(0), dev);
         const float scale = scale_of(a[5], qt->size(2));
         size_t bytes = 0;
-        if (!c.ok || qt->size(2) != c.cache->head_size || !(scale - scale == 0.f) || g_cached_bytes(c.cache, &c.s, (int)qt->size(1), &bytes) != 0) Py_RETURN_NONE;
+        if (!c.ok || qt->size(2) != c.cache->head_size || !(scale <= 0x1p127f && scale >= -0x1p127f) || g_cached_bytes(c.cache, &c.s, (int)qt->size(1), &bytes) != 0) Py_RETURN_NONE;
         at::Tensor y, ws;
         int rc;
         {
@@ -212,7 +212,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             Py_RETURN_NONE;
         const int32_t *offsets = int32(a[3], dev, o->size(0));
         const float scale = scale_of(a[4], qt->size(2));
-        if (offsets == nullptr || !(scale - scale == 0.f)) Py_RETURN_NONE;
+        if (offsets == nullptr || !(scale <= 0x1p127f && scale >= -0x1p127f)) Py_RETURN_NONE;
         at::Tensor y;
         int rc;
         {

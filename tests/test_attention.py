@@ -127,12 +127,12 @@ def test_refusals_of_attention():
     assert lib.tst_kv_attention_workspace_bytes(ref(c), ref(sequences(tokens=1 << 22)), 64, ref(need)) == EINVAL     # rows x heads
     n = need.value
     ok = [ref(q), 1, 4, ref(c), ref(s), 0.5, a, a, n, None]              # Q, type, q_heads, cache, sequences, scale, Y, workspace, bytes, stream
-    for i, v, code in ((0, None, EINVAL), (1, 3, EINVAL), (2, 5, EINVAL), (5, float("nan"), EINVAL), (5, float("inf"), EINVAL), (6, None, EINVAL), (6, a + 1, EINVAL), (7, None, EWORKSPACE),
+    for i, v, code in ((0, None, EINVAL), (1, 3, EINVAL), (2, 5, EINVAL), (5, float("nan"), EINVAL), (5, float("inf"), EINVAL), (5, 2.5e38, EINVAL), (6, None, EINVAL), (6, a + 1, EINVAL), (7, None, EWORKSPACE),
                        (8, n - 1, EWORKSPACE), (7, a + 128, EINVAL)):
         assert lib.tst_kv_attention(*ok[:i], v, *ok[i + 1:]) == code, i
     ok = [ref(q), ref(q), ref(q), 1, 4, 2, 64, a, 1, 5, 0.5, a, None]    # Q, K, V, type, q_heads, heads, size, offsets, sequences, tokens, scale, Y, stream
     for i, v in ((0, None), (1, None), (2, None), (3, 3), (4, 0), (4, 3), (4, 1026), (5, 0), (5, 3), (6, 0), (6, 257), (7, None), (7, a + 1), (8, -1), (8, (1 << 20) + 1), (9, -1), (9, (1 << 22) + 1),
-                 (10, float("nan")), (10, float("-inf")), (11, None), (11, a + 1)):
+                 (10, float("nan")), (10, float("-inf")), (10, -2.5e38), (11, None), (11, a + 1)):
         assert lib.tst_attention(*ok[:i], v, *ok[i + 1:]) == EINVAL, i
     assert lib.tst_attention(ref(q), ref(q), ref(q), 1, 64, 2, 64, a, 1, 1 << 22, 0.5, a, None) == EINVAL           # rows x heads
     assert lib.tst_attention(ref(q), ref(q), ref(q), 1, 1024, 1024, 64, a, 4097, 5, 0.5, a, None) == EINVAL         # sequences x heads
