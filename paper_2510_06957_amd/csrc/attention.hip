@@ -1,12 +1,16 @@
 // Causal attention over whole prompts, packed one behind another, with grouped heads (tst_attention).
 //
 // A workgroup has a tile of rows of one key head, a row being (token, query head of the group), so that the keys and values that it loads serve all heads of
-// the group, and goes through the keys from the first to the tile's last, 64 (fp32: 32) at a time, with the running largest logit and sum of each row.  Z^T = K Q^T and
+// the group, and goes through the keys from the first to the tile's last, 32 to 128 at a time, with the running largest logit and sum of each row.  Z^T = K Q^T and
 // Y^T = V^T P^T with the 32 x 32 x 16 instructions: a row's logits, weights and sums stay in the lanes with its number (mod 32), and the weights are the second
 // product's operand as they come out of the first, since keys may stand in any order there: lanes of half h hold keys 8 (r / 4) + 4 h + r % 4 of 32.
 // K and V go through the LDS as rows; the second product's operand, four keys of a channel in a lane, comes out of it by reads that transpose.
 //
 // fp32 operands are cut into three bf16 planes by cutting mantissas off (exact) and six products of planes are summed: all but 2^-24 of a product.
+//
+// Matrix cores and vector units share the time: a weight costs 6 vector instructions (largest, exponential, sum, rounding, operands) beside 256 multiplications of heads of 128.  In bf16 the next 32 keys'
+// logits are therefore made beside the weights of these.  8192 tokens, 32 query and 8 key heads of 128: 549 GFLOP in 548 to 565 us (1.0 PFLOP/s, matrix cores busy 43 % of the cycles; matrix
+// instructions and barriers alone 287 us); heads of 64 335, 4096 tokens of 256 520, 24 prompts of up to 2048 281; 2048 tokens of fp32, 16 query heads, 158.
 #include "attention_internal.h"
 
 #include <cmath>

