@@ -613,8 +613,10 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                 }
                 if constexpr (TYPE != TST_F32 && ROW <= 128) {
                     // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole: 256 tokens
-                    // 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149)
-                    if (2 * whole < 3 * tst::compute_units()) {
+                    // 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149), and for prompts that are short, so that a tile's start and end hide behind
+                    // another's keys (prompts x tokens at most: 128 x 128 46.5 and 61.4, 64 x 512 126 and 144, 64 x 1024 286 and 307, 24 x 2048 288 and 287, 8 x 4096 375 and 360;
+                    // heads of 64: 128 x 128 25 and 31, 64 x 1024 155 and 160, 24 x 2048 169 and 165)
+                    if (2 * whole < 3 * tst::compute_units() || tokens <= 768 * (int64_t)sequences) {
                         launch(std::integral_constant<int, tst::kFew>{});
                         return hipGetLastError();
                     }

@@ -419,9 +419,9 @@ def test_prompts_whose_keys_are_shared(lens, q_heads, heads, size, dtype):
 
 @pytest.mark.parametrize("q_heads,heads,size,dtype", [(64, 8, 64, "bf16"), (64, 8, 96, "f16"), (64, 16, 128, "bf16"), (66, 2, 128, "f16"), (64, 64, 64, "f16"), (64, 8, 80, "bf16"),
                                                       (64, 4, 192, "bf16"), (32, 8, 256, "f16")])
-def test_prompts_in_whole_tiles(q_heads, heads, size, dtype):
-    """Enough rows for the tiles that large calls take; a few heads and rows of each sequence against the definition."""
-    lens = [1217, 0, 3, 64, 65, 400, 1]
+@pytest.mark.parametrize("lens", [[1217, 0, 3, 64, 65, 400, 1], [1217, 835]])
+def test_prompts_in_whole_tiles(lens, q_heads, heads, size, dtype):
+    """Enough rows for the tiles that large calls take, of short prompts and of long ones; a few heads and rows of each sequence against the definition."""
     q, k, v = prompt(lens, q_heads, heads, size, dtype, 27)
     at = starts(lens)
     Y = tg.tst_attention(q, k, v, int32(at))
@@ -437,7 +437,7 @@ def test_prompts_in_whole_tiles(q_heads, heads, size, dtype):
         assert torch.allclose(alone.float(), Y[a:b].float(), rtol=8 * LAST[dtype], atol=0.02)
 
 
-@pytest.mark.parametrize("q_heads,lens", [(4, [90, 40]), (4, [300, 77]), (64, [1217, 64])])
+@pytest.mark.parametrize("q_heads,lens", [(4, [90, 40]), (4, [300, 77]), (64, [1217, 64]), (64, [2100, 64])])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_prompts_what_a_row_does_not_see_does_not_touch_it(dtype, q_heads, lens):
     """Infinities and NaN in keys and values behind a row, in other sequences and in rows of no sequence."""
