@@ -153,6 +153,10 @@ template <int TYPE, int ROW, int WAY> struct Shape {
     static constexpr int kStrideK = ROW * 2 + 16, kStrideV = ROW * 2 + (ROW % 128 == 96 ? 0 : 64);
     static constexpr int kPlaneK = kKeys * kStrideK, kPlaneV = kKeys * kStrideV;
     static constexpr int kBufferK = kPlanes * kPlaneK, kBufferV = kPlanes * kPlaneV;
+    // results of a wavefront's 32 rows go through the LDS, where the tiles were, and out as rows
+    static constexpr bool kByRows = kAhead;
+    static constexpr int kStrideRow = ROW * 2 + 16, kRowsBytes = 32 * kStrideRow;
+    static_assert(!kByRows || kWaves * kRowsBytes <= kBuffersK * kBufferK + kBuffersV * kBufferV, "rows fit where tiles were");
     static constexpr int kChunks = (kKeys * (ROW / 8) + kThreads - 1) / kThreads;   // of 8 entries that a thread stages, of K and as many of V
 };
 
@@ -541,9 +545,42 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                 }
         }
     }
-    if (!there) return;
-    const bool bad = any_spoilt;
+    if (uniform(any_spoilt)) {     // (asked once: asked for each result, it took as long as the stores)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (spoilt[32 * t + 8 * (r / 4) + 4 * half + r % 4] < limit) o[t][r] = kNan;
+    }
     const float inverse = 1.f / sum;
+    if constexpr (S::kByRows) {
+        // From the lanes as they are, 8 bytes of each of 32 rows, results took 2.6 us of every workgroup's (128 prompts of up to 128 tokens 42.6 us, so 37.3; 24 of up to 2048 276 and
+        // 268).  In fp32 a lane has 16 bytes of a row, and it is the other way round (2048 tokens 215 and 219).
+        if (((uintptr_t)a.y & 15) == 0) {
+            constexpr int per = ROW * (int)sizeof(Bits) / 16, each = 16 / (int)sizeof(Bits);
+            char *rows = lds_k + wave * S::kRowsBytes;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int d = 32 * t + 2 * r + 4 * half;
+                    Bits four[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e] * inverse);
+                    __builtin_memcpy(__builtin_assume_aligned(rows + col * S::kStrideRow + d * (int)sizeof(Bits), 4 * sizeof(Bits)), four, sizeof(four));
+                }
+            order_wave();
+            const int at = there ? (first + token) * a.q_heads + q_head : -1;     // rows * query heads <= 2^27
+#pragma unroll
+            for (int i = 0; i < 32 * per / 64; ++i) {
+                const int r = (lane + 64 * i) / per, d = (lane + 64 * i) % per * each, to = __shfl(at, r);
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(rows + r * S::kStrideRow + d * (int)sizeof(Bits));
+                if (to >= 0 && d < a.size) *reinterpret_cast<u32x4 *>(static_cast<Bits *>(a.y) + (int64_t)to * a.size + d) = v;
+            }
+            return;
+        }
+    }
+    if (!there) return;
     Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(first + token) * a.q_heads + q_head) * a.size;
     const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
 #pragma unroll
@@ -553,7 +590,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
             const int d = 32 * t + 2 * r + 4 * half;
             Bits four[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(bad && spoilt[d + e] < limit ? kNan : o[t][r + e] * inverse);
+            for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e] * inverse);
             if (whole) {
                 if (d < a.size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), four, sizeof(four));
             } else {

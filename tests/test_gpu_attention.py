@@ -431,6 +431,10 @@ def test_prompts_in_whole_tiles(lens, q_heads, heads, size, dtype):
     seen = np.concatenate([a + rows[rows < b - a] for a, b in zip(at, at[1:])])
     assert_within(Y[torch.from_numpy(seen).cuda()][:, few], want[seen][:, few], bound[seen][:, few], dtype)
     assert torch.equal(tg.tst_attention(q, k, v, int32(at)), Y)
+    for off in (1, 4):      # results that lie off 16-byte borders, and off 8-byte ones
+        room = torch.full((Y.numel() + 16,), 7.0, dtype=Y.dtype, device="cuda")
+        assert torch.equal(tg.tst_attention(q, k, v, int32(at), Y=room[off:off + Y.numel()].view(Y.shape)), Y)
+        assert (room[:off] == 7).all() and (room[off + Y.numel():] == 7).all()
     # each sequence by itself, in smaller tiles: the same up to the rounding of its sums
     for a, b in zip(at, at[1:]):
         alone = tg.tst_attention(q[a:b], k[a:b], v[a:b], int32([0, b - a]))
