@@ -553,6 +553,14 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                 if (spoilt[32 * t + 8 * (r / 4) + 4 * half + r % 4] < limit) o[t][r] = kNan;
     }
     const float inverse = 1.f / sum;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float x = o[t][r] * inverse;
+            asm("" : "+v"(x));     // rounded to fp32 however it is stored (else to fp16 at once where the compiler sees that)
+            o[t][r] = x;
+        }
     if constexpr (S::kByRows) {
         // From the lanes as they are, 8 bytes of each of 32 rows, results took 2.6 us of every workgroup's (128 prompts of up to 128 tokens 42.6 us, so 37.3; 24 of up to 2048 276 and
         // 268).  In fp32 a lane has 16 bytes of a row, and it is the other way round (2048 tokens 215 and 219).
@@ -566,7 +574,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                     const int d = 32 * t + 2 * r + 4 * half;
                     Bits four[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e] * inverse);
+                    for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e]);
                     __builtin_memcpy(__builtin_assume_aligned(rows + col * S::kStrideRow + d * (int)sizeof(Bits), 4 * sizeof(Bits)), four, sizeof(four));
                 }
             order_wave();
@@ -590,7 +598,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
             const int d = 32 * t + 2 * r + 4 * half;
             Bits four[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e] * inverse);
+            for (int e = 0; e < 4; ++e) four[e] = Entry<TYPE>::put(o[t][r + e]);
             if (whole) {
                 if (d < a.size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), four, sizeof(four));
             } else {
