@@ -238,6 +238,27 @@ template <int TYPE, int ROW, int WAY> struct Staged {
     // is remembered.
     __device__ __forceinline__ void mend(int tile, int *spoilt, int &any)
     {
+        // whether there is one at all, by the largest bits without sign: a branch for each entry takes longer than the rest of the tile's way into the LDS (128 prompts of up to 128 tokens
+        // 38.0 us, so 36.2; 24 of up to 2048 275.6 and 273.2)
+        if constexpr (TYPE == TST_F32) {
+            unsigned most = 0;
+#pragma unroll
+            for (int i = 0; i < S::kChunks; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(raw[i].e[e]) & 0x7fffffffu);
+            if (most < 0x7f800000u) return;
+        } else {
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 most = {0, 0};
+#pragma unroll
+            for (int i = 0; i < S::kChunks; ++i) {
+                unsigned two[4];
+                __builtin_memcpy(two, raw[i].e, 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, two[e] & 0x7fff7fffu));
+            }
+            if (max(most[0], most[1]) < (TYPE == TST_BF16 ? 0x7f80 : 0x7c00)) return;
+        }
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i)
 #pragma unroll
