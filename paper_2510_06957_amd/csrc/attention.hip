@@ -10,7 +10,7 @@
 //
 // Matrix cores and vector units share the time: a weight costs 6 vector instructions (largest, exponential, sum, rounding, operands) beside 256 multiplications of heads of 128.  In bf16 the next 32 keys'
 // logits are therefore made beside the weights of these.  8192 tokens, 32 query and 8 key heads of 128: 549 GFLOP in 548 to 565 us (1.0 PFLOP/s, matrix cores busy 43 % of the cycles; matrix
-// instructions and barriers alone 287 us); heads of 64 335, 4096 tokens of 256 520, 24 prompts of up to 2048 281; 2048 tokens of fp32, 16 query heads, 158.
+// instructions and barriers alone 287 us); heads of 64 335, 4096 tokens of 256 480, 24 prompts of up to 2048 266; 2048 tokens of fp32, 16 query heads, 158.
 #include "attention_internal.h"
 
 #include <cmath>
@@ -680,9 +680,9 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                 if constexpr (TYPE != TST_F32 && ROW <= 128) {
                     // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole: 256 tokens
                     // 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149), and for prompts that are short, so that a tile's start and end hide behind
-                    // another's keys (prompts x tokens at most: 128 x 128 46.5 and 61.4, 64 x 512 126 and 144, 64 x 1024 286 and 307, 24 x 2048 288 and 287, 8 x 4096 375 and 360;
-                    // heads of 64: 128 x 128 25 and 31, 64 x 1024 155 and 160, 24 x 2048 169 and 165)
-                    if (2 * whole < 3 * tst::compute_units() || tokens <= 768 * (int64_t)sequences) {
+                    // another's keys (prompts x their mean: 128 x 43 46.5 and 61.4, 64 x 175 126 and 144,
+                    // before a step of both; 64 x 350 260 and 280, 64 x 700 708 and 718, 24 x 725 269 and 266; heads of 64: 64 x 350 151 and 151, 24 x 725 166 and 159)
+                    if (2 * whole < 3 * tst::compute_units() || tokens <= 640 * (int64_t)sequences) {
                         launch(std::integral_constant<int, tst::kFew>{});
                         return hipGetLastError();
                     }
