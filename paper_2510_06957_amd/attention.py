@@ -70,6 +70,14 @@ class _RotationStruct(ctypes.Structure):
     _fields_ = [("struct_size", _sz), ("cos", _vp), ("sin", _vp), ("positions", _ci), ("pairs", _ci), ("interleaved", _ci)]
 
 
+def _struct(kind, what, *values):
+    """A struct of the call `what`; refuses integers of which a field would take the low 32 bits."""
+    for (_, field), value in zip(kind._fields_, values):
+        if field is _ci and not -2 ** 31 <= value < 2 ** 31:
+            raise TstgemmError(-1, what)
+    return kind(*values)
+
+
 class KvCache:
     """Keys and values of one layer in 8 bits (tst_kv_cache): pages of `page` tokens, a scale for each block of 16 tokens and head.
 
@@ -91,7 +99,7 @@ class KvCache:
         self.pages, self.page, self.heads, self.head_size, self.device_index = pages, page, heads, head_size, k_codes.get_device()
         self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
         self._tensors = (k_codes, v_codes, k_scale, v_scale)
-        self._struct = _CacheStruct(ctypes.sizeof(_CacheStruct), pages, page, heads, head_size, *(t.data_ptr() for t in self._tensors))   # their addresses
+        self._struct = _struct(_CacheStruct, "tst_kv_cache_bytes", ctypes.sizeof(_CacheStruct), pages, page, heads, head_size, *(t.data_ptr() for t in self._tensors))   # their addresses
         self._ref, self._raw = ctypes.byref(self._struct), ctypes.addressof(self._struct)
 
 
@@ -129,7 +137,7 @@ def _int32(x, what, shape, dev):
     return _dense(x, what, torch.int32, shape, dev)
 
 
-def _sequences(cache, pages, lens, offsets, T):
+def _sequences(cache, pages, lens, offsets, T, what):
     """tst_sequences_t of packed rows; pages may have rows that lie apart."""
     import torch
     if not isinstance(cache, KvCache) or cache.device_index != torch.cuda.current_device():
@@ -146,7 +154,7 @@ def _sequences(cache, pages, lens, offsets, T):
     offsets_ptr = None if offsets is None else _int32(offsets, "offsets", (S + 1,), dev)
     if offsets is None and T != S:
         raise ValueError("without offsets there is a token for each sequence")
-    return _SequencesStruct(ctypes.sizeof(_SequencesStruct), S, T, offsets_ptr, lens_ptr, pages.data_ptr(), columns, stride)
+    return _struct(_SequencesStruct, what, ctypes.sizeof(_SequencesStruct), S, T, offsets_ptr, lens_ptr, pages.data_ptr(), columns, stride)
 
 
 def tst_kv_append(cache: KvCache, K, V, pages, lens, offsets=None, Q=None, cos=None, sin=None, interleaved=False, keys=False, stream=None):
@@ -162,7 +170,7 @@ def tst_kv_append(cache: KvCache, K, V, pages, lens, offsets=None, Q=None, cos=N
     import torch
     k = _heads(K, "K")
     kind, T, dev = _type(K.dtype, "K"), K.shape[0], K.get_device()
-    s = _sequences(cache, pages, lens, offsets, T)
+    s = _sequences(cache, pages, lens, offsets, T, "tst_kv_append")
     if K.shape[1:] != (cache.heads, cache.head_size) or not isinstance(V, torch.Tensor) or V.shape != K.shape:
         raise ValueError(f"K and V must be [tokens, {cache.heads}, {cache.head_size}]")
     v = _heads(V, "V", K.dtype)
@@ -173,8 +181,8 @@ def tst_kv_append(cache: KvCache, K, V, pages, lens, offsets=None, Q=None, cos=N
     if cos is not None:
         if not isinstance(cos, torch.Tensor) or cos.dim() != 2 or cos.shape[0] < 1 or not 1 <= cos.shape[1] <= cache.head_size // 2:
             raise ValueError("cos and sin must be [positions, pairs], with at most head_size / 2 pairs")
-        rotation = _RotationStruct(ctypes.sizeof(_RotationStruct), _dense(cos, "cos", torch.float32, cos.shape, dev), _dense(sin, "sin", torch.float32, cos.shape, dev),
-                                   *cos.shape, int(bool(interleaved)))
+        rotation = _struct(_RotationStruct, "tst_kv_append", ctypes.sizeof(_RotationStruct), _dense(cos, "cos", torch.float32, cos.shape, dev), _dense(sin, "sin", torch.float32, cos.shape, dev),
+                           *cos.shape, int(bool(interleaved)))
     q_out = None if Q is None else _result(None, "", K.dtype, tuple(Q.shape), stream, dev)
     k_out = _result(None, "", K.dtype, tuple(K.shape), stream, dev) if keys else None
     _call("tst_kv_append", cache._ref, ctypes.byref(s), kind, ctypes.byref(k), ctypes.byref(v), None if q is None else ctypes.byref(q), 0 if q is None else Q.shape[1],
@@ -195,7 +203,7 @@ def tst_kv_read(cache: KvCache, pages, lens, tokens: int, offsets=None, dtype=No
     kind, tokens = _type(dtype, "dtype"), int(tokens)
     if tokens < 0:
         raise ValueError("tokens is a number of rows")
-    s = _sequences(cache, pages, lens, offsets, tokens)
+    s = _sequences(cache, pages, lens, offsets, tokens, "tst_kv_read")
     dev, shape = cache.device_index, (tokens, cache.heads, cache.head_size)
     K, V = _result(None, "", dtype, shape, stream, dev), _result(None, "", dtype, shape, stream, dev)
     _call("tst_kv_read", cache._ref, ctypes.byref(s), kind, K.data_ptr(), V.data_ptr(), _launch_stream(stream, dev))
@@ -219,7 +227,7 @@ def tst_kv_attention(Q, cache: KvCache, pages, lens, offsets=None, scale=None, Y
             return done
     q = _heads(Q, "Q")
     kind, (T, q_heads, size), dev = _type(Q.dtype, "Q"), Q.shape, Q.get_device()
-    s = _sequences(cache, pages, lens, offsets, T)
+    s = _sequences(cache, pages, lens, offsets, T, "tst_kv_attention")
     if size != cache.head_size or q_heads % cache.heads:
         raise ValueError(f"Q must be [tokens, a multiple of {cache.heads}, {cache.head_size}]")
     scale = _scale(scale, size)

@@ -149,6 +149,19 @@ def test_sizes_beyond_32_bits_are_refused():
             attention._call("tst_kv_cache_bytes", *args, ctypes.byref(codes), ctypes.byref(scales))
 
 
+@pytest.mark.parametrize("kind,at", [("_CacheStruct", 1), ("_CacheStruct", 3), ("_SequencesStruct", 1), ("_SequencesStruct", 2), ("_SequencesStruct", 6), ("_RotationStruct", 3),
+                                     ("_RotationStruct", 4)])
+@pytest.mark.parametrize("value", [2 ** 32 + 5, 2 ** 32, 2 ** 31, -2 ** 31 - 1])
+def test_counts_of_structs_beyond_32_bits_are_refused(kind, at, value):
+    kind = getattr(attention, kind)
+    fields = [1] * len(kind._fields_)
+    assert getattr(attention._struct(kind, "call", *fields), kind._fields_[at][0]) == 1
+    fields[at] = value
+    with pytest.raises(tg.TstgemmError) as e:
+        attention._struct(kind, "call", *fields)
+    assert e.value.code == EINVAL
+
+
 def test_the_binding_and_its_native_half_refuse_what_is_not_on_a_gpu():
     import torch
     x, i = torch.zeros((2, 2, 64)), torch.zeros((2, 1), dtype=torch.int32)
