@@ -78,11 +78,19 @@ def _struct(kind, what, *values):
     return kind(*values)
 
 
+def _tensor_of_cache(i, name):
+    def put(self, t):   # cache.k_scale *= 2 comes here with the tensor that is there
+        if t is not self._tensors[i]:
+            raise AttributeError(f"{name} stays the tensor it is: copy into it, or make a KvCache of others")
+    return property(lambda self: self._tensors[i], put)
+
+
 class KvCache:
     """Keys and values of one layer in 8 bits (tst_kv_cache): pages of `page` tokens, a scale for each block of 16 tokens and head.
 
     k_codes int8 [pages, heads, page, row], v_codes int8 [pages, heads, page / 16, row, 16], k_scale and v_scale float32 [pages, heads, page / 16]; row is
-    head_size padded to 64, 96, 128, 192 or 256."""
+    head_size padded to 64, 96, 128, 192 or 256.  What a cache is made of stays: calls go by the addresses of its tensors, so none can be
+    put in another's place, and a cache whose tensors have been given other memory since is refused."""
 
     def __init__(self, page, head_size, k_codes, v_codes, k_scale, v_scale):
         import torch
@@ -96,11 +104,19 @@ class KvCache:
             _dense(t, name, dtype, shape, k_codes.get_device())
         codes, scales = _sz(), _sz()
         _call("tst_kv_cache_bytes", pages, page, heads, head_size, ctypes.byref(codes), ctypes.byref(scales))   # refuses sizes that no call takes
-        self.pages, self.page, self.heads, self.head_size, self.device_index = pages, page, heads, head_size, k_codes.get_device()
-        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
-        self._tensors = (k_codes, v_codes, k_scale, v_scale)
+        self._device_index, self._tensors = k_codes.get_device(), (k_codes, v_codes, k_scale, v_scale)
         self._struct = _struct(_CacheStruct, "tst_kv_cache_bytes", ctypes.sizeof(_CacheStruct), pages, page, heads, head_size, *(t.data_ptr() for t in self._tensors))   # their addresses
         self._ref, self._raw = ctypes.byref(self._struct), ctypes.addressof(self._struct)
+
+    pages, page = property(lambda self: self._struct.pages), property(lambda self: self._struct.page_tokens)
+    heads, head_size = property(lambda self: self._struct.heads), property(lambda self: self._struct.head_size)
+    device_index = property(lambda self: self._device_index)
+    k_codes, v_codes, k_scale, v_scale = (_tensor_of_cache(i, name) for i, name in enumerate(("k_codes", "v_codes", "k_scale", "v_scale")))
+
+    def _check(self):
+        s = self._struct
+        if tuple(t.data_ptr() for t in self._tensors) != (s.k_codes, s.v_codes, s.k_scale, s.v_scale):
+            raise ValueError("the cache's tensors have been given other memory: make a KvCache of them")
 
 
 def tst_kv_cache(pages: int, page: int, heads: int, head_size: int, device=None) -> KvCache:
@@ -142,6 +158,7 @@ def _sequences(cache, pages, lens, offsets, T, what):
     import torch
     if not isinstance(cache, KvCache) or cache.device_index != torch.cuda.current_device():
         raise ValueError("cache must be a KvCache on the current device")
+    cache._check()
     dev = cache.device_index
     if not (isinstance(pages, torch.Tensor) and pages.is_cuda and pages.dtype == torch.int32 and pages.dim() == 2 and pages.shape[1] >= 1 and not pages.is_neg()
             and pages.get_device() == dev and (pages.shape[1] == 1 or pages.stride(1) == 1)):

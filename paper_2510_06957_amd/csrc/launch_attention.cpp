@@ -21,7 +21,7 @@ decltype(&tst_kv_attention_workspace_bytes) g_cached_bytes;
 decltype(&tst_kv_attention) g_cached;
 decltype(&tst_attention) g_prompt;
 PyObject *g_error, *g_cache_class;   // TstgemmError, KvCache
-PyObject *s_raw, *s_device_index;
+PyObject *s_raw, *s_device_index, *s_tensors;
 
 // A tensor of torch's own class with memory of its own on device dev, which holds its values as they are.
 const at::Tensor *plain(PyObject *o, int dev)
@@ -61,11 +61,26 @@ struct Call {
     const tst_kv_cache_t *cache = nullptr;
     tst_sequences_t s{};
     bool ok = false;
+    // The struct has the tensors' addresses: they have to be where they were.
+    bool as_it_was(PyObject *c) const
+    {
+        PyObject *tensors = PyObject_GetAttr(c, s_tensors);
+        const void *const at[4] = {cache->k_codes, cache->v_codes, cache->k_scale, cache->v_scale};
+        bool same = tensors != nullptr && PyTuple_CheckExact(tensors) && PyTuple_GET_SIZE(tensors) == 4;
+        for (int i = 0; same && i < 4; ++i) {
+            PyObject *t = PyTuple_GET_ITEM(tensors, i);
+            same = THPVariable_Check(t) && THPVariable_Unpack(t).data_ptr() == at[i];
+        }
+        Py_XDECREF(tensors);
+        PyErr_Clear();
+        return same;
+    }
     Call(PyObject *c, PyObject *pages, PyObject *lens, PyObject *offsets, int64_t tokens, int dev)
     {
         unsigned long long raw = 0, index = 0;
         if ((PyObject *)Py_TYPE(c) != g_cache_class || !int_attr(c, s_raw, &raw) || !int_attr(c, s_device_index, &index) || raw == 0 || (int)index != dev) return;
         cache = reinterpret_cast<const tst_kv_cache_t *>(raw);
+        if (!as_it_was(c)) return;
         const at::Tensor *p = plain(pages, dev);
         if (p == nullptr || p->scalar_type() != at::kInt || p->dim() != 2 || p->size(0) > TST_MAX_SEQUENCES || p->size(1) < 1 || p->size(1) > INT_MAX ||
             (p->size(1) > 1 && p->stride(1) != 1))
@@ -256,8 +271,9 @@ PyMethodDef attention_methods[] = {{"kv_append", fast(kv_append), METH_FASTCALL,
 bool attention_init()
 {
     s_raw = PyUnicode_InternFromString("_raw");
-    s_device_index = PyUnicode_InternFromString("device_index");
-    return s_raw != nullptr && s_device_index != nullptr;
+    s_device_index = PyUnicode_InternFromString("_device_index");
+    s_tensors = PyUnicode_InternFromString("_tensors");
+    return s_raw != nullptr && s_device_index != nullptr && s_tensors != nullptr;
 }
 
 }  // namespace launch

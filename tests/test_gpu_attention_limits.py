@@ -30,3 +30,30 @@ def test_counts_beyond_32_bits_are_refused():
     for name in "kv":
         same(after[name][0], before[name][0])
         same(after[name][1], before[name][1])
+
+
+def test_a_cache_keeps_its_tensors():
+    """What a cache says of itself cannot be set, and one whose tensors have been given other memory is refused, both halves of the binding."""
+    from paper_2510_06957_amd import attention
+    w = World([40, 9], 2, 64, 16, 66)
+    pages, lens = w.arrays()
+    x = torch.ones((2, 8, 64), device="cuda")
+    c = w.cache
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name).clone())
+    for name in ("pages", "page", "heads", "head_size", "device_index"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name) + 1)
+    c.v_scale *= 1.0       # what is there already
+    calls = (lambda: tg.tst_kv_append(c, x[:, :2], x[:, :2], pages, lens), lambda: tg.tst_kv_read(c, pages, lens, 2), lambda: tg.tst_kv_attention(x[:, :4], c, pages, lens))
+    for t in (c.k_codes, c.v_codes, c.k_scale, c.v_scale):
+        saved, other = t.data, t.clone()
+        t.data = other
+        for call in calls:
+            with pytest.raises(ValueError):
+                call()
+        assert attention._native.kv_read(c, pages, lens, 2, None, None) is None
+        t.data = saved
+        for call in calls:
+            call()
