@@ -1,12 +1,14 @@
 // Shared by the operators of tst_attention.h.
 #pragma once
+#include <climits>
+
 #include "ops_internal.h"
 #include "tst_attention.h"
 
 namespace tst {
 
 constexpr int kKvBlock = TST_KV_BLOCK;
-constexpr int kMaxPosition = 1 << 30;
+constexpr int kMaxPositions = 1 << 30;   // of a table; a length may be any int, and positions go by it as it is
 
 inline __host__ __device__ int kv_row(int size) { return size <= 64 ? 64 : size <= 96 ? 96 : size <= 128 ? 128 : size <= 192 ? 192 : 256; }
 

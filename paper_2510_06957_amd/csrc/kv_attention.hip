@@ -244,13 +244,13 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     const int seq = uniform(it.seq), tile = uniform(it.tile);
     begin = uniform(begin), end = uniform(end);
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
-    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition);
+    const int len = max(a.seqs.lens[seq], 0);
 
     // queries
     f16x8 q[RT][S::kPlanes][S::kSteps];
     float factor[RT];
     int limit[RT];   // keys that the row sees
-    int least = kMaxPosition;
+    int least = INT_MAX;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const unsigned rho = tile * (16 * RT) + rt * 16 + m16;
@@ -508,7 +508,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     const int n = (int)min((int64_t)chunks, a.items - first);   // (fewer where offsets do not ascend)
     const int64_t place = (int64_t)head * a.items + first;
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, slot.seq);
-    const int sees_from = rows.n - min(max(a.seqs.lens[slot.seq], 0), kMaxPosition), size = a.cache.size;   // tokens of the call below it see nothing
+    const int sees_from = rows.n - max(a.seqs.lens[slot.seq], 0), size = a.cache.size;   // tokens of the call below it see nothing
     const bool share = gridDim.z > 1;
     for (int part = share ? blockIdx.z : wave; part < RT * kTiles; part += share ? RT * kTiles : kWaves) {
         const int rt = part / kTiles, dt = part % kTiles;

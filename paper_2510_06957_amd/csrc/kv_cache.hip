@@ -346,11 +346,11 @@ template <int TYPE, int HOW, int SIZES> __global__ void __launch_bounds__(64 * k
     const int seq = a.seqs.offsets ? uniform(find_sequence(a.seqs.offsets, a.seqs.tokens, a.seqs.count, kKvBlock, 2, at)) : at;
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
     const int piece = a.seqs.offsets ? at - (rows.first / kKvBlock + 2 * seq) : 0;
-    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition), first = len - rows.n;   // position of the first row; negative where there are more rows
+    const int len = max(a.seqs.lens[seq], 0), first = len - rows.n;   // position of the first row; negative where there are more rows
     const int block = (first >> 4) + piece;
     if (rows.n == 0 || piece < 0 || block > (len - 1) >> 4) return;
     const int from = max(first - block * kKvBlock, 0), to = min(len - 1 - block * kKvBlock, kKvBlock - 1);
-    Piece p{0, seq, block, from, to, rows.first + block * kKvBlock + from - first};
+    Piece p{0, seq, block, from, to, rows.first + (block * kKvBlock + from - first)};
     if ((int)blockIdx.y >= a.kv_groups) {
         rotate_queries<TYPE, HOW, SIZES>(a, p, ((blockIdx.y - a.kv_groups) * kWaves + wave) * 4);
         return;
@@ -384,12 +384,12 @@ template <int TYPE, bool WIDE> __global__ void __launch_bounds__(64 * kWaves) k_
     const int seq = a.seqs.offsets ? uniform(find_sequence(a.seqs.offsets, a.seqs.tokens, a.seqs.count, kKvBlock, 2, at)) : at;
     const Span rows = span_of(a.seqs.offsets, a.seqs.tokens, seq);
     const int piece = a.seqs.offsets ? at - (rows.first / kKvBlock + 2 * seq) : 0;
-    const int len = min(max(a.seqs.lens[seq], 0), kMaxPosition), first = len - rows.n;
+    const int len = max(a.seqs.lens[seq], 0), first = len - rows.n;
     const int block = (first >> 4) + piece;
     const int item = blockIdx.y * kWaves + wave;
     if (rows.n == 0 || piece < 0 || block > (len - 1) >> 4 || item >= 2 * a.cache.heads) return;
     const int from = max(first - block * kKvBlock, 0), to = min(len - 1 - block * kKvBlock, kKvBlock - 1);
-    const int row0 = rows.first + block * kKvBlock + from - first;
+    const int row0 = rows.first + (block * kKvBlock + from - first);
     const bool values = item & 1;
     const int head = item >> 1, size = a.cache.size, units = (size + 7) / 8, row = kv_row(size);
     const int page = page_of(a.cache, a.seqs, seq, block);
@@ -458,7 +458,7 @@ int check_sequences(const tst_kv_cache_t *c, const tst_sequences_t *s)
     if (!s || s->struct_size != sizeof(tst_sequences_t) || s->sequences < 0 || s->sequences > TST_MAX_SEQUENCES || s->tokens < 0 || s->tokens > TST_MAX_TOKENS)
         return TSTGEMM_EINVAL;
     if (!s->offsets && s->tokens != s->sequences) return TSTGEMM_EINVAL;
-    if (s->columns < 1 || s->table_stride < s->columns || s->table_stride > INT64_MAX / 4 / (TST_MAX_SEQUENCES + 1) || (int64_t)s->columns * c->page_tokens > kMaxPosition)
+    if (s->columns < 1 || s->table_stride < s->columns || s->table_stride > INT64_MAX / 4 / (TST_MAX_SEQUENCES + 1) || (int64_t)s->columns * c->page_tokens > kMaxPositions)
         return TSTGEMM_EINVAL;
     if (s->sequences == 0 || s->tokens == 0) return TSTGEMM_OK;
     return s->lens && s->table && aligned(s->offsets, 4) && aligned(s->lens, 4) && aligned(s->table, 4) ? TSTGEMM_OK : TSTGEMM_EINVAL;

@@ -57,3 +57,24 @@ def test_a_cache_keeps_its_tensors():
         t.data = saved
         for call in calls:
             call()
+
+
+def test_lengths_beyond_2_30_tokens():
+    """Behind the largest table there is: positions from 2^30 on have no page, whatever the length says."""
+    columns = (1 << 30) // 256
+    r = rng(65)
+    for k, there in ((4, 3), (1000, 0), (2 ** 30 - 1, 0)):
+        cache = tg.tst_kv_cache(2, 256, 1, 64)
+        pages = torch.zeros((1, columns), dtype=torch.int32, device="cuda")
+        pages[0, -1] = 1
+        K, V = (cuda(r.standard_normal((7, 1, 64)).astype(np.float32)) for _ in "kv")
+        lens, offsets = int32([(1 << 30) + k]), int32([0, 7])
+        tg.tst_kv_append(cache, K, V, pages, lens, offsets)
+        assert not cache.k_codes[0].any() and not cache.v_codes[0].any() and not cache.k_scale[0].any() and not cache.v_scale[0].any()
+        assert not cache.k_codes[1, :, :253].any() and not cache.k_scale[1, :, :15].any()
+        assert cache.k_codes[1, 0, 253:].any(1).tolist() == [there > 0] * 3
+        for x, got in zip((K, V), tg.tst_kv_read(cache, pages, lens, 7, offsets, dtype=torch.float32)):
+            assert torch.isnan(got[there:]).all() and (not there or (got[:there] - x[:there]).abs().max() < 0.03)
+        if k < 2 ** 29:
+            Y = tg.tst_kv_attention(K, cache, pages, lens, offsets)
+            assert torch.isfinite(Y[:there]).all() and torch.isnan(Y[there:]).all()
