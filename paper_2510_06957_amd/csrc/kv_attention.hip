@@ -6,8 +6,9 @@
 // t-th tile of keys is token 4 t + m % 4 of block m / 4, and a lane's 16 weights are those that the 16 codes of one channel in its block's layout meet.
 //
 // Codes become fp16 exactly (1024 + code + 128 by its bits, less 1152).  A query's row is scaled by a power of two so that its largest entry is in [2^14, 2^15) and
-// cut into fp16 (11 bits, and 11 more in a second plane for fp32).  Weights meet a value's scale relative to the largest seen so far, times 2^15: with 11 bits (22 for
-// fp32) down to 2^-29 of the largest, an absolute 2^-40 of it below.  Sums are fp32.
+// cut into fp16 (11 bits, and 11 more in a second plane for fp32).  Weights are multiplied by their value's scale, and the products are held relative to the largest of
+// them so far, at 2^7 of which fp16 begins (fp32: 2^15): with 11 bits down to 2^-21 of the largest and 2^-32 of it below (22 bits down to 2^-18, and 2^-40).  It is the
+// product that counts: relative to the largest scale, a block that weighs nothing would cost others their bits (or, 2^33 above theirs, all of them).  Sums are fp32.
 //
 // The keys of a long sequence are cut into equal chunks, about as long as those of the others: the device finds the length from the lengths of all sequences, so that
 // the workgroups have about as much to do each whatever the batch is, and the host knows how many there are at most.  k_kv_join joins the chunks of a tile of rows.
@@ -26,7 +27,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kWaves = 4, kUnit = 64;   // tokens of a wavefront at a time
 constexpr float kNan = __builtin_nanf("");
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLeastScale = 1e-33f;   // of values, as what weights are relative to: 2^15 over it is finite
+constexpr float kLeastProduct = 1e-33f;   // that products are relative to: 2^15 over it is finite
 
 struct KvArgs {
     Cache cache;
@@ -161,9 +162,9 @@ template <int TYPE, int ROW, int RT> struct Shape {
     static constexpr int kSteps = ROW / 32;      // of 32 channels
     static constexpr int kWide = ROW / 64;       // loads of 16 bytes of a lane in a row of keys; 8 more bytes where ROW % 64 = 32
     static constexpr int kTiles = ROW / 16;      // of 16 channels
-    // Weights are 2^kShift times those relative to the largest logit and scale of values that all was last scaled by; what comes later may pass them by
-    // 2^kSlack and kScaleSlack times before all is scaled anew.  fp16 holds 2^15.  fp32 has no room for that: weights down to 2^-29 of the largest keep their bits.
-    static constexpr float kShift = TYPE == TST_F32 ? 32768.f : 128.f, kSlack = TYPE == TST_F32 ? 0.f : 6.f, kScaleSlack = TYPE == TST_F32 ? 1.f : 4.f;
+    // Products of weights and scales are kShift times those relative to the largest by which all was last scaled; what comes later may pass it kProductSlack times, and a logit the
+    // largest by kSlack, before all is scaled anew.  fp16 holds 2^15.  fp32 has no room for that: the second plane's bits reach 2^-24.
+    static constexpr float kShift = TYPE == TST_F32 ? 32768.f : 128.f, kSlack = TYPE == TST_F32 ? 0.f : 6.f, kProductSlack = TYPE == TST_F32 ? 1.f : 256.f;
 };
 // The channel that entry i of step j stands for in a lane of quarter g: 16 bytes of a row are two steps.
 template <int ROW> __device__ __forceinline__ int channel(int j, int g) { return j < ROW / 64 * 2 ? j / 2 * 64 + g * 16 + j % 2 * 8 : j / 2 * 64 + g * 8; }
@@ -299,11 +300,11 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     least = uniform(least);   // all rows see the keys below this
 
     f32x4 o[RT][S::kTiles];
-    // What a row's weights are relative to, of logits and of scales of values, by what the row itself sees alone; 2^kShift over the latter.
+    // What a row's weights are relative to, and its products of weights and scales (those weights), by what the row itself sees alone; kShift over the latter.
     float most[RT], reference[RT], inverse[RT], sum[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        most[rt] = -INFINITY, sum[rt] = 0.f, reference[rt] = kLeastScale, inverse[rt] = S::kShift / kLeastScale;
+        most[rt] = -INFINITY, sum[rt] = 0.f, reference[rt] = kLeastProduct, inverse[rt] = S::kShift / kLeastProduct;
 #pragma unroll
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -396,14 +397,16 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top[rt] = fmaxf(top[rt], z[rt][t][e]);
-                anew |= top[rt] > most[rt] + S::kSlack || v_own[rt] > reference[rt] * S::kScaleSlack;
+                // (where nothing was seen before, the first question says it)
+                anew |= top[rt] > most[rt] + S::kSlack || __builtin_amdgcn_exp2f(top[rt] - most[rt]) * v_own[rt] > reference[rt] * S::kProductSlack;
             }
             if (__any(anew)) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    const float t = quarters_max(top[rt]), v = quarters_max(v_own[rt]);
-                    const float now = t > most[rt] + S::kSlack ? t : most[rt], largest = v > reference[rt] * S::kScaleSlack ? v : reference[rt];
-                    const float keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most[rt] - now), times = keep * (reference[rt] / largest);
+                    const float t = quarters_max(top[rt]), now = t > most[rt] + S::kSlack ? t : most[rt];
+                    const float keep = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most[rt] - now), was = fmaxf(keep * reference[rt], kLeastProduct);
+                    const float v = quarters_max(__builtin_amdgcn_exp2f(top[rt] - now) * v_own[rt]), largest = v > was * S::kProductSlack ? v : was;
+                    const float times = keep * reference[rt] / largest;     // 1 for a row that asked for nothing
                     most[rt] = now, reference[rt] = largest, inverse[rt] = S::kShift / largest;
                     sum[rt] *= keep;
 #pragma unroll
@@ -413,7 +416,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
             f16x8 w[RT][S::kPlanes][2];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const float base = most[rt] == -INFINITY ? 0.f : most[rt], v_part = v_own[rt] * inverse[rt];
+                const float base = most[rt] == -INFINITY ? 0.f : most[rt];
                 float s = 0.f;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
@@ -421,7 +424,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
                     for (int e = 0; e < 4; ++e) {
                         const float p = __builtin_amdgcn_exp2f(z[rt][t][e] - base);
                         s += p;
-                        float x = p * v_part;
+                        float x = p * v_own[rt] * inverse[rt];     // (the scale over the reference may be beyond 32 bits)
                         if (cut) x = z[rt][t][e] == -INFINITY ? 0.f : x;
                         const _Float16 hi = (_Float16)x;
                         w[rt][0][t / 2][t % 2 * 4 + e] = hi;

@@ -78,3 +78,30 @@ def test_lengths_beyond_2_30_tokens():
         if k < 2 ** 29:
             Y = tg.tst_kv_attention(K, cache, pages, lens, offsets)
             assert torch.isfinite(Y[:there]).all() and torch.isnan(Y[there:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("columns", [100, 1000])
+@pytest.mark.parametrize("new", [1, 20])
+def test_attention_over_the_cache_scales_of_blocks_that_weigh_nothing(new, columns, dtype):
+    """A block whose tokens weigh nothing, with a scale of values far above the others', leaves them their bits.  Weights keep theirs (11; 22 in fp32) relative to the largest
+    product of a weight and a scale, and 2^-32 (2^-40) of it below: n terms of 127 of that."""
+    w = World([1500], 1, 64, 16, 64, columns=columns)
+    w.ref.codes["k"][:] = np.abs(w.ref.codes["k"])
+    at = [0, new]
+    Qd = strided(np.abs(queries(w, new, 2, 64, 64)) + 0.5, dtype)
+    pages, lens = w.arrays()
+    for block in (0, 3, 40, 61, 91):
+        page = w.table[0, block]
+        saved = {n: (w.ref.codes[n][page].copy(), w.ref.scale[n][page].copy()) for n in "kv"}
+        w.ref.codes["k"][page] = -127
+        w.ref.scale["k"][page] = 0.2           # logits 100 and more below the others'
+        w.ref.scale["v"][page] = 0
+        want, bound = reference_over_cache(w, f32(Qd), [new], at, 0.125, dtype)
+        bound = bound + 1500 * 2.0 ** (-40 if dtype == "f32" else -32) * 127 * 1.5 / 64
+        for large in (1e6, 1e12, 1e30):
+            w.ref.scale["v"][page] = large
+            w.upload()
+            assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at)), want, bound, dtype, f"block {block} scale {large}")
+        for n in "kv":
+            w.ref.codes[n][page], w.ref.scale[n][page] = saved[n]
