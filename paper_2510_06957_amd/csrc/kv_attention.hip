@@ -38,7 +38,7 @@ struct KvArgs {
     float scale;
     bool wide;                  // rows of Q on 16-byte borders, of a multiple of 8 entries
     void *y;
-    f32x4 *sums;                // [heads][items][tiles][64 lanes]
+    f32x4 *sums;                // [heads][items][tiles][64 lanes]: a chunk's own results
     float2 *states;             // [heads][items][16 x row tiles]: largest logit, sum of weights
     int items;                  // of a head, at most
 };
@@ -191,7 +191,16 @@ __device__ __forceinline__ float quarters_max(float v)
 // Adds what another wavefront or chunk has, relative to largest logits of its own.
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(const KvArgs &a, const Span &rows, int tile, int head, const f32x4 (&o)[RT][ROW / 16], const float (&sum)[RT], const int (&limit)[RT])
+// A mean of values is no larger than they are, however its last bits are rounded.
+template <int TYPE> __device__ __forceinline__ float bounded(float v)
+{
+    if constexpr (TYPE != TST_F32) return v;
+    else return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -3.402823466e38f), 3.402823466e38f);   // (a NaN stays one)
+}
+
+// o: sums of weights and values, in units of `unit` times the sum of weights.
+template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(const KvArgs &a, const Span &rows, int tile, int head, const f32x4 (&o)[RT][ROW / 16], const float (&sum)[RT], const float (&unit)[RT],
+                                                                                const int (&limit)[RT])
 {
     typedef typename Entry<TYPE>::bits Bits;
     const int lane = threadIdx.x % 64, g = lane / 16, size = a.cache.size;
@@ -208,7 +217,7 @@ template <int TYPE, int ROW, int RT> __device__ __forceinline__ void write_rows(
             const int d = 16 * dt + 4 * g;
             Bits b[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) b[e] = Entry<TYPE>::put(o[rt][dt][e] * inverse);
+            for (int e = 0; e < 4; ++e) b[e] = Entry<TYPE>::put(bounded<TYPE>(o[rt][dt][e] * inverse * unit[rt]));
             if (whole) {
                 if (d < size) __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(Bits)), b, sizeof(b));
             } else {
@@ -226,6 +235,7 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     typedef typename Entry<TYPE>::bits Bits;
     __shared__ f32x4 shared[kWaves / 2][RT * S::kTiles][64];
     __shared__ float2 states[kWaves][RT][16];
+    __shared__ float references[kWaves][RT][16];
     const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y;
     Item it;
     int begin = 0, end = 0;
@@ -445,23 +455,29 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         }
     }
 
-    // the wavefronts' sums: relative to the largest logit of all, then two and two
-    float all[RT], total[RT];
+    // the wavefronts' sums: relative to the largest logit of all, and to the largest reference, so that they stay as far from the ends of 32 bits as they are; then two and two
+    float all[RT], total[RT], unit[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         sum[rt] += __shfl_xor(sum[rt], 16);
         sum[rt] += __shfl_xor(sum[rt], 32);
-        if (g == 0) states[wave][rt][m16] = float2{most[rt], sum[rt]};
+        if (g == 0) states[wave][rt][m16] = float2{most[rt], sum[rt]}, references[wave][rt][m16] = reference[rt];
     }
     __syncthreads();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         all[rt] = -INFINITY, total[rt] = 0.f;
+        float common = kLeastProduct;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) all[rt] = fmaxf(all[rt], states[w][rt][m16].x);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) total[rt] += states[w][rt][m16].y * weight_of(states[w][rt][m16].x, all[rt]);
-        const float times = weight_of(most[rt], all[rt]) * (reference[rt] * (1.f / S::kShift));
+        for (int w = 0; w < kWaves; ++w) {
+            const float weight = weight_of(states[w][rt][m16].x, all[rt]);
+            total[rt] += states[w][rt][m16].y * weight;
+            common = fmaxf(common, references[w][rt][m16] * weight);
+        }
+        unit[rt] = common * (1.f / S::kShift);
+        const float times = weight_of(most[rt], all[rt]) * reference[rt] / common;
 #pragma unroll
         for (int dt = 0; dt < S::kTiles; ++dt) o[rt][dt] *= times;   // (a NaN of a row whose weights here are nothing beside others stays one)
     }
@@ -482,26 +498,26 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
     }
     if (wave != 0) return;
     if (it.chunks == 1) {
-        write_rows<TYPE, ROW, RT>(a, rows, tile, head, o, total, limit);
+        write_rows<TYPE, ROW, RT>(a, rows, tile, head, o, total, unit, limit);
         return;
     }
     const int64_t place = (int64_t)head * a.items + blockIdx.x;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+        const float inverse = total[rt] == 0.f ? 0.f : 1.f / total[rt];     // (where nothing weighs anything sums are 0, or NaN)
 #pragma unroll
-        for (int dt = 0; dt < S::kTiles; ++dt) a.sums[(place * (RT * S::kTiles) + rt * S::kTiles + dt) * 64 + lane] = o[rt][dt];
+        for (int dt = 0; dt < S::kTiles; ++dt) a.sums[(place * (RT * S::kTiles) + rt * S::kTiles + dt) * 64 + lane] = o[rt][dt] * inverse * unit[rt];
         if (g == 0) a.states[place * (RT * 16) + rt * 16 + m16] = float2{all[rt], total[rt]};
     }
 }
 
 // Joins the chunks of a tile, 16 channels of 16 rows at a time: where there are few tiles, each such part is a workgroup's, whose wavefronts share the chunks, else a
-// wavefront's, one after another.
+// wavefront's, one after another.  Chunks have results of their own, of which this is the mean: nothing in between is larger than they are.
 template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWaves) k_kv_join(KvArgs a)
 {
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int kTiles = ROW / 16;
     __shared__ f32x4 shared[kWaves][64];
-    __shared__ float totals[kWaves][64];
     const int wave = uniform(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16, m16 = lane % 16, head = blockIdx.y;
     const Slot slot = find_slot<16 * RT>(a, blockIdx.x);
     if (slot.tile < 0) return;
@@ -517,35 +533,40 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         const int rt = part / kTiles, dt = part % kTiles;
         const float2 *states = a.states + place * (RT * 16) + rt * 16 + m16;
         const f32x4 *sums = a.sums + (place * (RT * kTiles) + part) * 64 + lane;
-        float all = -INFINITY;
+        // the largest logit, and the sum of weights relative to it: a quarter's lanes have every fourth chunk
+        float own = -INFINITY, total = 0.f;
 #pragma unroll 4
-        for (int c = g; c < n; c += 4) all = fmaxf(all, states[(int64_t)c * (RT * 16)].x);
-        all = quarters_max(all);
-        float total = 0.f;
+        for (int c = g; c < n; c += 4) {
+            const float2 s = states[(int64_t)c * (RT * 16)];
+            const float now = fmaxf(own, s.x);
+            total = total * weight_of(own, now) + s.y * weight_of(s.x, now);
+            own = now;
+        }
+        const float all = quarters_max(own);
+        total *= weight_of(own, all);
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        const float inverse = 1.f / total;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int c = share ? wave : 0; c < n; c += share ? kWaves : 1) {
             const float2 s = states[(int64_t)c * (RT * 16)];
             const f32x4 v = sums[(int64_t)c * (RT * kTiles) * 64];
-            const float w = weight_of(s.x, all);
-            total += w * s.y;
-            o += w * v;
+            o += weight_of(s.x, all) * s.y * inverse * v;
         }
         if (share) {
             shared[wave][lane] = o;
-            totals[wave][lane] = total;
             __syncthreads();
             if (wave != 0) return;
-            for (int w = 1; w < kWaves; ++w) o += shared[w][lane], total += totals[w][lane];
+            for (int w = 1; w < kWaves; ++w) o += shared[w][lane];
         }
         const unsigned rho = slot.tile * (16 * RT) + rt * 16 + m16;
         if (rho >= (unsigned)(rows.n * a.group)) continue;
         const int t = rho / (unsigned)a.group, h = head * a.group + (int)(rho - t * a.group);
         Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(rows.first + t) * a.q_heads + h) * size;
-        const float inverse = 1.f / total;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(t >= sees_from ? o[e] * inverse : 0.f);
+            if (16 * dt + 4 * g + e < size) out[16 * dt + 4 * g + e] = Entry<TYPE>::put(t >= sees_from ? bounded<TYPE>(o[e]) : 0.f);
     }
 }
 

@@ -105,3 +105,27 @@ def test_attention_over_the_cache_scales_of_blocks_that_weigh_nothing(new, colum
             assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at)), want, bound, dtype, f"block {block} scale {large}")
         for n in "kv":
             w.ref.codes[n][page], w.ref.scale[n][page] = saved[n]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("columns", [100, 1000])
+@pytest.mark.parametrize("new", [[1, 1], [30, 4]])
+@pytest.mark.parametrize("alike", [False, True])
+def test_attention_over_the_cache_of_large_values(alike, new, columns, dtype):
+    """A result lies between the values it is a mean of, of hundreds of tokens that weigh about the same and stand for the largest there are."""
+    w = World([900, 77], 2, 64, 16, 63, columns=columns)
+    scale = np.nextafter(np.float32(LARGEST[dtype] / 127), np.float32(0))
+    if alike:
+        w.ref.codes["v"][:, 0], w.ref.codes["v"][:, 1] = 127, -127
+        w.ref.scale["v"][:] = scale
+    else:
+        w.ref.codes["v"][:] = np.abs(w.ref.codes["v"])
+        w.ref.scale["v"][:] = scale * (0.5 + 0.5 * w.r.random(w.ref.scale["v"].shape))
+    w.upload()
+    at = starts(new)
+    Qd = strided(queries(w, at[-1], 4, 64, 63, 0.01), dtype)
+    pages, lens = w.arrays()
+    want, bound = reference_over_cache(w, f32(Qd), new, at, 0.125, dtype)
+    Y = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at))
+    assert torch.isfinite(Y).all()
+    assert_within(Y, want, bound, dtype)
