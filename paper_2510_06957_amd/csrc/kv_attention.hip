@@ -259,8 +259,11 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
 
     // queries
     f16x8 q[RT][S::kPlanes][S::kSteps];
-    float factor[RT];
-    int limit[RT];   // keys that the row sees
+    // A logit is a sum of products times scale, log2 e, the keys' scale and 2^-up: mantissas and exponents apart, since the factors may be beyond 32 bits where logits are not.
+    const float scale_mantissa = __builtin_amdgcn_frexp_mantf(a.scale) * (kLog2e / 2);
+    const int scale_exponent = __builtin_amdgcn_frexp_expf(a.scale) + 1;
+    float valid[RT]; // 1, or NaN for a row of Q that holds what is not finite
+    int up[RT], limit[RT];   // keys that the row sees
     int least = INT_MAX;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -294,13 +297,13 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
         most = max(most, (unsigned)__shfl_xor((int)most, 16));
         most = max(most, (unsigned)__shfl_xor((int)most, 32));
         const bool finite = most < 0x7f800000u;
-        const int up = most == 0 || !finite ? 0 : 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(most));
-        factor[rt] = finite ? __builtin_ldexpf(a.scale * kLog2e, -up) : kNan;
+        up[rt] = most == 0 || !finite ? 0 : 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(most));
+        valid[rt] = finite ? 1.f : kNan;
 #pragma unroll
         for (int j = 0; j < S::kSteps; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float v = finite ? __builtin_ldexpf(x[j][e], up) : 0.f;
+                const float v = finite ? __builtin_ldexpf(x[j][e], up[rt]) : 0.f;
                 const _Float16 hi = (_Float16)v;
                 q[rt][0][j][e] = hi;
                 if constexpr (S::kPlanes == 2) q[rt][1][j][e] = (_Float16)(v - (float)hi);
@@ -384,10 +387,13 @@ template <int TYPE, int ROW, int RT> __global__ void __launch_bounds__(64 * kWav
 
             const bool cut = (u + 1) * kUnit > least;
             bool anew = false;
+            const float mantissa = scale_mantissa * __builtin_amdgcn_frexp_mantf(k_scale);
+            const int exponent = scale_exponent + __builtin_amdgcn_frexp_expf(k_scale);
             float top[RT], v_own[RT];     // v_own: 0 for a block that the row does not see
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const float f = factor[rt] * k_scale;
+                // at most 2^128 times a mantissa below 1: 0 times an infinity would be a NaN
+                const float f = __builtin_ldexpf(mantissa * valid[rt], min(exponent - up[rt], 128));
                 top[rt] = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)

@@ -129,3 +129,17 @@ def test_attention_over_the_cache_of_large_values(alike, new, columns, dtype):
     Y = tg.tst_kv_attention(Qd, w.cache, pages, lens, int32(at))
     assert torch.isfinite(Y).all()
     assert_within(Y, want, bound, dtype)
+
+
+@pytest.mark.parametrize("columns", [100, 1000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_over_the_cache_queries_and_scales_far_from_one(dtype, columns):
+    """Logits are ordinary numbers, or 0, where a query times the factor is beyond 32 bits, or below."""
+    w = World([500, 30], 2, 64, 16, 68, columns=columns)
+    pages, lens = w.arrays()
+    for large, factor, keys in ((2.0 ** 60, 2.0 ** 127, 0.0), (2.0 ** 100, 2.0 ** 46, 2.0 ** -148), (2.0 ** -126, 2.0 ** -2, 2.0 ** 119), (2.0 ** -140, 2.0 ** 8, 2.0 ** 119), (2.0 ** 100, 2.0 ** -145, 2.0 ** 38)):
+        w.ref.scale["k"][:] = keys
+        w.upload()
+        Qd = strided(queries(w, 2, 4, 64, 68, large), dtype)
+        want, bound = reference_over_cache(w, f32(Qd), [1, 1], [0, 1, 2], factor, dtype)
+        assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens, scale=factor), want, bound, dtype, f"{large} {factor} {keys}")
