@@ -31,7 +31,7 @@ struct PromptArgs {
     Rows q, k, v;
     int q_heads, heads, group, size, sequences, tokens, tiles;
     const int32_t *offsets;
-    float scale;   // its magnitude times log2 e; 2^-126 for 0 and less, so that -inf stays what it is
+    float scale;   // its magnitude times log2 e; 2^-149 for 0, so that -inf stays what it is (and others are below 2^-21)
     bool negative;
     void *y;
     bool wide;     // rows of Q, K and V on 16-byte borders, of a multiple of 8 entries
@@ -651,7 +651,7 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
     if (!tst::rows_ok(Q, type) || !tst::rows_ok(K, type) || !tst::rows_ok(V, type) || !offsets || !tst::aligned(offsets, 4) || !Y || !tst::aligned(Y, tst::type_bytes(type)))
         return TSTGEMM_EINVAL;
     const int group = q_heads / heads;
-    tst::PromptArgs a{tst::rows_of(Q), tst::rows_of(K), tst::rows_of(V), q_heads, heads, group, head_size, sequences, tokens, 0, offsets, std::fmax(std::fabs(scale) * tst::kLog2e, 1.17549435e-38f), scale < 0, Y, false};
+    tst::PromptArgs a{tst::rows_of(Q), tst::rows_of(K), tst::rows_of(V), q_heads, heads, group, head_size, sequences, tokens, 0, offsets, std::fmax(std::fabs(scale) * tst::kLog2e, 0x1p-149f), scale < 0, Y, false};
     a.wide = tst::wide(a.q, type, head_size) && tst::wide(a.k, type, head_size) && tst::wide(a.v, type, head_size);
     return tst::status(tst::for_type(type, [&](auto t) {
         return tst::for_row(head_size, [&](auto r) {

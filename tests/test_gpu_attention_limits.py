@@ -143,3 +143,19 @@ def test_attention_over_the_cache_queries_and_scales_far_from_one(dtype, columns
         Qd = strided(queries(w, 2, 4, 64, 68, large), dtype)
         want, bound = reference_over_cache(w, f32(Qd), [1, 1], [0, 1, 2], factor, dtype)
         assert_within(tg.tst_kv_attention(Qd, w.cache, pages, lens, scale=factor), want, bound, dtype, f"{large} {factor} {keys}")
+
+
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -140, -2.0 ** -133, 2.0 ** -126])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[200, 33], [100] * 30])
+def test_prompts_small_scales(lens, dtype, scale):
+    """Products of queries and keys near 2^126, times next to nothing."""
+    q, k, v = prompt(lens, 4, 2, 64, dtype, 67, large=2e18)
+    at = starts(lens)
+    want, bound = prompt_reference(f32(q), f32(k), f32(v), at, scale, dtype, None, np.arange(0, 200, 7))
+    rows = np.concatenate([a + np.arange(0, b - a, 7) for a, b in zip(at, at[1:])])
+    assert_within(f32_rows(tg.tst_attention(q, k, v, int32(at), scale=scale), rows), want[rows], bound[rows], dtype)
+
+
+def f32_rows(Y, rows):
+    return Y[torch.from_numpy(rows).cuda()]
