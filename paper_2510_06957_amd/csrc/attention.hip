@@ -164,6 +164,10 @@ template <int TYPE, int ROW, int WAY> struct Shape {
 // down to 2^-21 of the largest.
 constexpr float kSlack = 8.f;
 template <int TYPE> constexpr float kShift = TYPE == TST_F16 ? 7.f : 0.f;
+// Sums of up to 2^22 values with weights of up to 2^kSlack can pass 2^128 in bf16 and fp32 where their mean does not.  A tile with results that are not finite therefore goes through
+// its keys again, with values 2^-32 times as large, and the rows that those results are of take what comes of that: the same bits, but for values below 2^-94.  (fp16 has no such values.)
+constexpr float kLess = 0x1p-32f, kLargest = 3.402823466e38f;
+template <int TYPE> constexpr bool kMayPass = TYPE != TST_F16;
 
 // The tile of rows that workgroups of a number have, -1: none.  A sequence's tiles come one after another, since they read the same keys and values, the last,
 // which sees most of them, first.  Of up to 64 sequences the shortest come first: what is left at the end are then the shortest tiles of the longest (4096 and 1024 tokens, 32
@@ -209,8 +213,10 @@ __device__ __forceinline__ Place place_of(const PromptArgs &a, int rows, int num
 template <int TYPE, int ROW, int WAY> struct Staged {
     typedef Shape<TYPE, ROW, WAY> S;
     Raw<TYPE> raw[S::kChunks];
-    static __device__ __forceinline__ int key_of(int i) { return (threadIdx.x + S::kThreads * i) / (ROW / 8); }
-    static __device__ __forceinline__ int channel_of(int i) { return (threadIdx.x + S::kThreads * i) % (ROW / 8) * 8; }
+    const unsigned thread;
+    __device__ __forceinline__ explicit Staged(unsigned t) : thread(t) {}
+    __device__ __forceinline__ int key_of(int i) const { return (thread + S::kThreads * i) / (ROW / 8); }
+    __device__ __forceinline__ int channel_of(int i) const { return (thread + S::kThreads * i) % (ROW / 8) * 8; }
 
     // the tile's keys; zeros behind `keys`
     __device__ __forceinline__ void load(const typename Entry<TYPE>::bits *data, int64_t stride, int tile, int keys, int size, bool wide)
@@ -271,6 +277,13 @@ template <int TYPE, int ROW, int WAY> struct Staged {
                 }
             }
     }
+    __device__ __forceinline__ void shrink()
+    {
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) raw[i].e[e] = Entry<TYPE>::put(Entry<TYPE>::get(raw[i].e[e]) * kLess);
+    }
     __device__ __forceinline__ void store(char *to, int stride, int plane, int left, int size)
     {
         if (WAY != kAny && (left < S::kKeys || size < ROW)) {
@@ -288,21 +301,25 @@ template <int TYPE, int ROW, int WAY> struct Staged {
     }
 };
 
-template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<TYPE, ROW, WAY>::kThreads), (Shape<TYPE, ROW, WAY>::kOccupancy)) k_attention(PromptArgs a)
+template <int TYPE, int ROW, int WAY> struct Shared {
+    typedef Shape<TYPE, ROW, WAY> S;
+    __attribute__((aligned(16))) char tiles[S::kBuffersK * S::kBufferK + S::kBuffersV * S::kBufferV];
+    int spoilt[ROW];   // the first key whose value of the channel is not finite, among the keys that some of the tile's rows do not see
+    int any_spoilt, any_passed;
+};
+
+// The results of a tile's rows; of those alone that `mine` says.  LESS: by values kLess times as large.  Whether the lane's row has results that are not finite, by values that it sees all of.
+template <int TYPE, int ROW, int WAY, bool LESS> __device__ __forceinline__ bool attend(const PromptArgs &a, int tile, int n, int first, int head, Shared<TYPE, ROW, WAY> &shared, bool mine)
 {
     typedef Shape<TYPE, ROW, WAY> S;
     typedef typename Entry<TYPE>::bits Bits;
     constexpr int P = S::kPlanes, kSteps = ROW / 16, kTiles = ROW / 32, kSub = S::kKeys / 32;   // 32 keys at a time
-    __shared__ __attribute__((aligned(16))) char lds_k[S::kBuffersK * S::kBufferK + S::kBuffersV * S::kBufferV];
-    char *const lds_v = lds_k + S::kBuffersK * S::kBufferK;
-    __shared__ int spoilt[ROW];   // the first key whose value of the channel is not finite, among the keys that some of the tile's rows do not see
-    __shared__ int any_spoilt;
-    const int wave = uniform(threadIdx.x / 64) % (S::kWaves / S::kGroups), sharer = uniform(threadIdx.x / 64) / (S::kWaves / S::kGroups);   // of its rows; of those with the same
-    const int lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
-    const int head = blockIdx.x % a.heads;
-    const Place place = place_of(a, S::kRows, (int)(blockIdx.x / a.heads));
-    if (place.tile < 0) return;
-    const int tile = uniform(place.tile), n = uniform(place.n), first = uniform(place.first);
+    char *const lds_k = shared.tiles, *const lds_v = lds_k + S::kBuffersK * S::kBufferK;
+    int *const spoilt = shared.spoilt, &any_spoilt = shared.any_spoilt;
+    unsigned thread = threadIdx.x;
+    if constexpr (LESS) asm volatile("" : "+v"(thread));     // (or the compiler keeps what goes by it from the first time on)
+    const int wave = uniform(thread / 64) % (S::kWaves / S::kGroups), sharer = uniform(thread / 64) / (S::kWaves / S::kGroups);   // of its rows; of those with the same
+    const int lane = thread % 64, half = lane / 32, col = lane % 32;
 
     const unsigned group = a.group, rho0 = tile * S::kRows;
     const int first_token = rho0 / group, last_token = min((int)((rho0 + S::kRows - 1) / group), n - 1);
@@ -311,14 +328,14 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
 
     const Bits *k_data = static_cast<const Bits *>(a.k.data) + (int64_t)first * a.k.token + head * a.k.head;
     const Bits *v_data = static_cast<const Bits *>(a.v.data) + (int64_t)first * a.v.token + head * a.v.head;
-    Staged<TYPE, ROW, WAY> k_tile, v_tile, k_next;
+    Staged<TYPE, ROW, WAY> k_tile(thread), v_tile(thread), k_next(thread);
     auto load_k = [&](int kt) { k_tile.load(k_data, a.k.token, kt, keys, a.size, WAY != kAny || a.wide); };
     auto load_v = [&](int kt) { v_tile.load(v_data, a.v.token, kt, keys, a.size, WAY != kAny || a.wide); };
     load_k(0), load_v(0);
     if (S::kAhead && tiles > 1) k_next.load(k_data, a.k.token, 1, keys, a.size, true);
 
-    for (int d = threadIdx.x; d < ROW; d += S::kThreads) spoilt[d] = 0x7fffffff;
-    if (threadIdx.x == 0) any_spoilt = 0;
+    for (int d = thread; d < ROW; d += S::kThreads) spoilt[d] = 0x7fffffff;
+    if (thread == 0) any_spoilt = 0;
 
     u32x4 q[P][kSteps];
     const unsigned rho = rho0 + wave * 32 + col;
@@ -358,6 +375,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
     auto store_k = [&](int kt) { k_tile.store(lds_k + kt % S::kBuffersK * S::kBufferK, S::kStrideK, S::kPlaneK, keys - kt * S::kKeys, a.size); };
     auto store_v = [&](int kt) {
         if ((kt + 1) * S::kKeys > first_token + 1) v_tile.mend(kt, spoilt, any_spoilt);
+        if constexpr (LESS) v_tile.shrink();
         v_tile.store(lds_v + kt % S::kBuffersV * S::kBufferV, S::kStrideV, S::kPlaneV, keys - kt * S::kKeys, a.size);
     };
 
@@ -530,7 +548,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
     if constexpr (S::kGroups > 1) {
         // sharers' sums, relative to their own bases, through the LDS that held the tiles
         constexpr int kOthers = (S::kGroups - 1) * (S::kWaves / S::kGroups);
-        static_assert(kOthers * 64 * (kTiles * 64 + 8) <= (int)sizeof(lds_k), "sums fit where tiles were");
+        static_assert(kOthers * 64 * (kTiles * 64 + 8) <= (int)sizeof(shared.tiles), "sums fit where tiles were");
         f32x4 *sums = reinterpret_cast<f32x4 *>(lds_k);
         float2 *states = reinterpret_cast<float2 *>(sums + kOthers * kTiles * 4 * 64);
         if (sharer > 0) {
@@ -542,7 +560,7 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
             states[slot * 64 + lane] = float2{base, sum};
         }
         __syncthreads();
-        if (sharer > 0) return;
+        if (sharer > 0) return false;
         float all = base;
 #pragma unroll
         for (int i = 1; i < S::kGroups; ++i) all = fmaxf(all, states[((i - 1) * (S::kWaves / S::kGroups) + wave) * 64 + lane].x);
@@ -566,6 +584,20 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                 }
         }
     }
+    const float inverse = 1.f / sum;
+    float most = 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float x = o[t][r] * inverse;
+            asm("" : "+v"(x));     // rounded to fp32 however it is stored (else to fp16 at once where the compiler sees that)
+            if constexpr (LESS)      // a mean is no larger than what it is of, however its last bits are rounded
+                if (__builtin_fabsf(x) <= kLargest) x = fminf(fmaxf(x * (1.f / kLess), -kLargest), kLargest);
+            if constexpr (kMayPass<TYPE>) most = __builtin_elementwise_maximum(most, __builtin_fabsf(x));
+            o[t][r] = x;
+        }
+    const bool passed = kMayPass<TYPE> && !LESS && mine && there && !(across_max(most) <= kLargest);
     if (uniform(any_spoilt)) {     // (asked once: asked for each result, it took as long as the stores)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
@@ -573,15 +605,6 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
             for (int r = 0; r < 16; ++r)
                 if (spoilt[32 * t + 8 * (r / 4) + 4 * half + r % 4] < limit) o[t][r] = kNan;
     }
-    const float inverse = 1.f / sum;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float x = o[t][r] * inverse;
-            asm("" : "+v"(x));     // rounded to fp32 however it is stored (else to fp16 at once where the compiler sees that)
-            o[t][r] = x;
-        }
     if constexpr (S::kByRows) {
         // From the lanes as they are, 8 bytes of each of 32 rows, results took 2.6 us of every workgroup's (128 prompts of up to 128 tokens 42.6 us, so 37.3; 24 of up to 2048 276 and
         // 268).  In fp32 a lane has 16 bytes of a row, and it is the other way round (2048 tokens 215 and 219).
@@ -599,17 +622,17 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                     __builtin_memcpy(__builtin_assume_aligned(rows + col * S::kStrideRow + d * (int)sizeof(Bits), 4 * sizeof(Bits)), four, sizeof(four));
                 }
             order_wave();
-            const int at = there ? (first + token) * a.q_heads + q_head : -1;     // rows * query heads <= 2^27
+            const int at = mine && there ? (first + token) * a.q_heads + q_head : -1;     // rows * query heads <= 2^27
 #pragma unroll
             for (int i = 0; i < 32 * per / 64; ++i) {
                 const int r = (lane + 64 * i) / per, d = (lane + 64 * i) % per * each, to = __shfl(at, r);
                 const u32x4 v = *reinterpret_cast<const u32x4 *>(rows + r * S::kStrideRow + d * (int)sizeof(Bits));
                 if (to >= 0 && d < a.size) *reinterpret_cast<u32x4 *>(static_cast<Bits *>(a.y) + (int64_t)to * a.size + d) = v;
             }
-            return;
+            return passed;
         }
     }
-    if (!there) return;
+    if (!there || !mine) return false;
     Bits *out = static_cast<Bits *>(a.y) + ((int64_t)(first + token) * a.q_heads + q_head) * a.size;
     const bool whole = (a.size & 3) == 0 && ((uintptr_t)a.y & (4 * sizeof(Bits) - 1)) == 0;
 #pragma unroll
@@ -628,6 +651,23 @@ template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<T
                     if (d + e < a.size) out[d + e] = four[e];
             }
         }
+    return passed;
+}
+
+template <int TYPE, int ROW, int WAY> __global__ void __launch_bounds__((Shape<TYPE, ROW, WAY>::kThreads), (Shape<TYPE, ROW, WAY>::kOccupancy)) k_attention(PromptArgs a)
+{
+    const int head = blockIdx.x % a.heads;
+    const Place place = place_of(a, Shape<TYPE, ROW, WAY>::kRows, (int)(blockIdx.x / a.heads));
+    if (place.tile < 0) return;
+    const int tile = uniform(place.tile), n = uniform(place.n), first = uniform(place.first);
+    __shared__ Shared<TYPE, ROW, WAY> shared;
+    if (threadIdx.x == 0) shared.any_passed = 0;     // (seen by all behind the workgroup's first meeting)
+    const bool passed = attend<TYPE, ROW, WAY, false>(a, tile, n, first, head, shared, true);
+    if constexpr (kMayPass<TYPE>) {
+        if (passed) shared.any_passed = 1;
+        __syncthreads();
+        if (uniform(shared.any_passed)) attend<TYPE, ROW, WAY, true>(a, tile, n, first, head, shared, passed);
+    }
 }
 
 bool wide(const Rows &x, int type, int size)

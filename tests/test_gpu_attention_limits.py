@@ -159,3 +159,58 @@ def test_prompts_small_scales(lens, dtype, scale):
 
 def f32_rows(Y, rows):
     return Y[torch.from_numpy(rows).cuda()]
+
+
+def large_prompt(lens, q_heads, heads, size, dtype, most, gap):
+    """Logits of 0 and now and then 7 powers of two more; values of up to `most`, of one sign in a channel."""
+    T, r = sum(lens), rng(61, sum(lens), size)
+    Q, K, V = (np.zeros((T, h, size)) for h in (q_heads, heads, heads))
+    Q[..., 0] = 1
+    K[..., 0] = np.where(r.random((T, heads)) < 0.02, 7 * math.log(2), 0)
+    K[20:40, :, 0] = 0
+    V[:] = (0.5 + 0.5 * r.random(V.shape)) * most
+    V[20:45] = most
+    V[..., 1::2] *= -1
+    return [strided(np.clip(x, -LARGEST[dtype], LARGEST[dtype]), dtype, gap) for x in (Q, K, V)]
+
+
+@pytest.mark.parametrize("lens,q_heads,heads,size,gap", [([300, 33], 4, 2, 64, 0), ([100, 33, 1], 4, 2, 96, 0), ([1217, 64], 64, 2, 64, 0), ([1217, 835], 64, 16, 128, 0),
+                                                          ([130, 41], 4, 2, 200, 0), ([130, 41], 4, 2, 64, 3), ([700], 2, 1, 128, 0)])
+@pytest.mark.parametrize("most", [1e37, None])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_of_large_values(dtype, most, lens, q_heads, heads, size, gap):
+    """A result lies between the values it is a mean of, however many there are and however large."""
+    q, k, v = large_prompt(lens, q_heads, heads, size, dtype, most or LARGEST[dtype], gap)
+    at = starts(lens)
+    few = sorted({0, q_heads // 2, q_heads - 1})
+    rows = np.unique(np.r_[np.arange(0, 70), np.arange(120, 135), np.arange(250, 262), np.arange(1200, 1217)])
+    seen = np.concatenate([a + rows[rows < b - a] for a, b in zip(at, at[1:])])
+    Y = tg.tst_attention(q, k, v, int32(at), scale=1.0)
+    want, bound = prompt_reference(f32(q), f32(k), f32(v), at, 1.0, dtype, few, rows)
+    assert torch.isfinite(Y).all()
+    assert_within(Y[torch.from_numpy(seen).cuda()][:, few], want[seen][:, few], bound[seen][:, few], dtype)
+    assert torch.equal(tg.tst_attention(q, k, v, int32(at), scale=1.0), Y)
+
+
+@pytest.mark.parametrize("lens,q_heads,size", [([90, 40], 4, 64), ([300, 77], 4, 64), ([1217, 64], 64, 64), ([130, 41], 4, 200)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_large_values_that_a_row_does_not_see_do_not_touch_it(dtype, lens, q_heads, size):
+    """From a row on values are as large as there are, or none in a channel; rows before it, and the other sequence, keep their last bit."""
+    q, k, v = (strided(x.cpu().float().numpy(), dtype) for x in prompt(lens, q_heads, 2, size, dtype, 62))
+    at = starts(lens)
+    clean = tg.tst_attention(q, k, v, int32(at))
+    cut = lens[0] - 20
+    v[cut:lens[0]] = LARGEST[dtype]
+    v[cut + 5:lens[0], :, 3] = float("inf")
+    v[cut + 9:lens[0], :, 5] = float("nan")
+    Y = tg.tst_attention(q, k, v, int32(at))
+    assert torch.equal(Y[:cut], clean[:cut]) and torch.equal(Y[lens[0]:], clean[lens[0]:])
+    spoilt = torch.zeros(Y.shape, dtype=torch.bool, device="cuda")
+    spoilt[cut + 5:lens[0], :, 3] = True
+    spoilt[cut + 9:lens[0], :, 5] = True
+    assert torch.equal(~torch.isfinite(Y), spoilt)
+    few, rows = [0, q_heads - 1], np.arange(cut, lens[0])
+    finite = np.where(np.isfinite(f32(v)), f32(v), 0)
+    want, bound = prompt_reference(f32(q), f32(k), finite, at, 1 / math.sqrt(size), dtype, few, rows)
+    got, keep = f32(Y)[rows][:, few], ~spoilt[cut:lens[0]].cpu().numpy()[:, few]
+    assert_within(torch.from_numpy(np.where(keep, got, 0)), np.where(keep, want[rows][:, few], 0), np.where(keep, bound[rows][:, few], 0), dtype)
