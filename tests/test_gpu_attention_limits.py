@@ -214,3 +214,18 @@ def test_prompts_large_values_that_a_row_does_not_see_do_not_touch_it(dtype, len
     want, bound = prompt_reference(f32(q), f32(k), finite, at, 1 / math.sqrt(size), dtype, few, rows)
     got, keep = f32(Y)[rows][:, few], ~spoilt[cut:lens[0]].cpu().numpy()[:, few]
     assert_within(torch.from_numpy(np.where(keep, got, 0)), np.where(keep, want[rows][:, few], 0), np.where(keep, bound[rows][:, few], 0), dtype)
+
+
+@pytest.mark.parametrize("q_heads,heads,size", [(64, 8, 64), (64, 8, 80), (64, 16, 128), (66, 2, 96)])
+@pytest.mark.parametrize("lens", [[1217, 835], [1217, 0, 3, 64, 65, 400, 1]])
+def test_prompts_in_whole_tiles_fp32(lens, q_heads, heads, size):
+    """Enough rows for the kernel of large calls, over many tiles of keys; a few heads and rows of each sequence against the definition."""
+    q, k, v = prompt(lens, q_heads, heads, size, "f32", 69)
+    at = starts(lens)
+    Y = tg.tst_attention(q, k, v, int32(at))
+    few = [0, q_heads // 2 + 1, q_heads - 1]
+    rows = np.unique(np.r_[np.arange(0, 70), np.arange(120, 135), np.arange(250, 262), np.arange(820, 835), np.arange(1200, 1217)])
+    seen = np.concatenate([a + rows[rows < b - a] for a, b in zip(at, at[1:])])
+    want, bound = prompt_reference(f32(q), f32(k), f32(v), at, 1 / math.sqrt(size), "f32", few, rows)
+    assert_within(f32_rows(Y, seen)[:, few], want[seen][:, few], bound[seen][:, few], "f32")
+    assert torch.equal(tg.tst_attention(q, k, v, int32(at)), Y)
