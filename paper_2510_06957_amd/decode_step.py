@@ -104,7 +104,10 @@ class Memory:
 def answer(model, prompts, steps, top=4):
     """prompts: lists of tokens.  The prompts at once, then `steps` tokens for each from a step recorded once: [steps, sequences] most likely tokens, their log
     probabilities and the entropies they were chosen from, beginning with what follows the prompts."""
-    lengths = [len(p) for p in prompts]
+    lengths, vocabulary = [len(p) for p in prompts], len(model.embedding)
+    # a prompt without tokens would be answered from another's last, and an index behind the embedding would end the process on the GPU
+    if steps < 1 or not lengths or min(lengths) < 1 or not all(0 <= t < vocabulary for p in prompts for t in p):
+        raise ValueError(f"prompts must be lists of at least one token of 0 to {vocabulary - 1}, and steps at least 1")
     memory = Memory(model, lengths, steps + 1)
     offsets = torch.tensor([0] + lengths, dtype=torch.int32).cumsum(0).int().cuda()
     logits = model.logits(torch.tensor([t for p in prompts for t in p], device="cuda"), memory, offsets, prompt=True)

@@ -179,3 +179,13 @@ def test_the_binding_and_its_native_half_refuse_what_is_not_on_a_gpu():
     for call in (native.attention, native.kv_attention, native.kv_append, native.kv_read):
         with pytest.raises(TypeError):
             call(x)
+
+
+@pytest.mark.parametrize("prompts,steps", [([], 3), ([[1, 2], []], 3), ([[]], 3), ([[1], [2000]], 3), ([[1, -1]], 3), ([[1]], 0)])
+def test_the_example_refuses_prompts_that_it_has_no_answer_to(prompts, steps):
+    import types
+
+    import torch
+    from paper_2510_06957_amd.decode_step import answer
+    with pytest.raises(ValueError):
+        answer(types.SimpleNamespace(embedding=torch.zeros((2000, 1))), prompts, steps)
