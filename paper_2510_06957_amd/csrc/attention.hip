@@ -708,8 +708,8 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                 const int64_t whole = (int64_t)tokens * group / tst::Shape<TYPE, ROW, tst::kFast>::kRows * heads;   // tiles
                 if constexpr (ROW <= 128) {
                     // Rows whose keys are shared, where there are fewer tiles than compute units (fp32, whose tiles are half as large: than twice as many) and keys to share.  us, shared
-                    // and not, 32 heads of 128, 8 of keys: bf16 256 tokens 14.9 and 15.8, 512 18.7 and 22.2 (heads of 64 12.0 and 16.8), 1024 36.3 and 35.0, 64 12.6 and 10.7;
-                    // fp32 32 tokens 11.7 and 11.7, 256 26 and 33, 1024 86 and 103, 2048 291 and 217; bf16 512 tokens, heads of 256 60 and 46
+                    // and not, 32 heads of 128, 8 of keys: bf16 128 tokens 11.0 and 10.4, 256 12.3 and 13.4, 512 15.8 and 20.1 (heads of 64 11.1 and 16.5), 1024 31.0 and 33.2;
+                    // fp32 32 tokens 12.4 and 11.5, 48 12.5 and 13.2, 256 25 and 33, 1024 85 and 104, 2048 295 and 219
                     const bool few = TYPE == TST_F32 ? whole < 2 * tst::compute_units() && tokens > 32 * (int64_t)sequences
                                                      : whole < tst::compute_units() && tokens > 128 * (int64_t)sequences;
                     if (few) {
@@ -718,10 +718,12 @@ int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t 
                     }
                 }
                 if constexpr (TYPE != TST_F32 && ROW <= 128) {
-                    // tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole: 256 tokens
-                    // 15.9 and 18.1, 1024 35 and 40, 2048 63 and 67, 3000 94 and 96, 4096 168 and 149), and for prompts that are short, so that a tile's start and end hide behind
-                    // another's keys (prompts x their mean: 128 x 43 46.5 and 61.4, 64 x 175 126 and 144,
-                    // before a step of both; 64 x 350 260 and 280, 64 x 700 708 and 718, 24 x 725 269 and 266; heads of 64: 64 x 350 151 and 151, 24 x 725 166 and 159)
+                    // Tiles of half the rows, two workgroups on a compute unit, where whole ones would leave compute units without any or with one (us, half and whole: 2048 tokens 61.5
+                    // and 66.5, 3000 94 and 97, 4096 168 and 150), and for prompts that are short, so that a tile's start and end hide behind another's keys.  Prompts x their mean, of
+                    // lengths all the way from the longest down: 128 x 43 37.5 and 48.6, 64 x 175 112 and 130, 64 x 350 264 and 283, 32 x 536 229 and 234, 64 x 614 583 and 603, 24 x 637
+                    // 224 and 223, 16 x 657 157 and 155, 64 x 700 717 and 727, 24 x 725 275 and 268, 128 x 518 807 and 804; heads of 64: 64 x 350 152 and 154, 24 x 637 138 and 134.
+                    // Between means of 500 and 750 the two are within 3 % of one another, so the border is there.  It cannot go by how lengths are spread, which the device alone
+                    // knows: of prompts all alike half tiles stay ahead longer (32 x 640 220 and 227, 32 x 768 285 and 307, 32 x 1024 443 and 461; 128 x 640 772 and 757).
                     if (2 * whole < 3 * tst::compute_units() || tokens <= 640 * (int64_t)sequences) {
                         launch(std::integral_constant<int, tst::kFew>{});
                         return hipGetLastError();
