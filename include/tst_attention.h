@@ -56,7 +56,7 @@ int tst_kv_cache_bytes(int pages, int page_tokens, int heads, int head_size, siz
  * read on the device when the call runs, so that a captured call goes by what they hold then.
  * Rows in front of offsets[0] and behind offsets[sequences] are left as they are.  Rows whose position is negative (more rows than
  * lens[i]) or whose page is not one of the cache's are not appended, and what is read in their place is NaN; nothing is read or written outside
- * the operands whatever the arrays hold.  lens[i] <= 0: an empty sequence.
+ * the operands whatever the arrays hold.  lens[i] <= 0: an empty sequence; a length may be any other number, and positions behind the table's end have no page.
  */
 typedef struct tst_sequences {
     size_t struct_size;          /* sizeof(tst_sequences_t) */
@@ -113,9 +113,11 @@ int tst_kv_read(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, i
  *   Y = sum_j w_j v_j / sum_j w_j,   w_j = e^(scale q.k_j - max)
  * with the values that codes stand for; |scale| <= 2^127.  The new tokens have been appended before.  A row that sees nothing is zeros.
  * q_heads: a multiple of the cache's heads, at most 1024 of them, tokens * q_heads <= 2^27; Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Queries keep 22 bits or those of their type
- * relative to the largest of their row, weights 11 bits in 16-bit types and 22 in fp32.
+ * relative to the largest of their row.  Products of a weight and its value's scale keep 11 bits in 16-bit types and 22 in fp32, down to 2^-21 (2^-18) of the largest of them that the row
+ * sees; those below are off by up to 2^-32 (2^-40) of it.  Logits are fp32: one beyond that is an infinity.
  * A row of Q that holds an infinity or a NaN is NaN, and so is a row that sees a block whose scale is none.
- * workspace: DEVICE, 256-byte aligned, at least tst_kv_attention_workspace_bytes(), which goes by tokens, heads and head_size (0 may be enough).
+ * workspace: DEVICE, 256-byte aligned, at least tst_kv_attention_workspace_bytes() of the same cache, sequences and q_heads on the same device (0 may be enough).  It goes by tokens, sequences,
+ * heads, q_heads, head_size and the table's width in tokens, columns * page_tokens, not by what the arrays hold: ask again when one of these changes, a wider table among them.
  * Calls that may overlap need different workspaces.  Errors: EINVAL, EWORKSPACE, EHIP.
  */
 int tst_kv_attention_workspace_bytes(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, int q_heads, size_t *bytes);
@@ -125,7 +127,9 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
 /*
  * Causal attention over whole prompts: rows offsets[i] .. offsets[i + 1] - 1 are sequence i; its row p, head h, sees keys of rows 0 .. p of the sequence,
  * head h / (q_heads / heads), as above.  offsets: DEVICE, sequences + 1, ascending.  Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Rows outside the sequences
- * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 and 24 for fp32 in the second product, sums are fp32.
+ * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 (down to 2^-21 of the row's largest, and 2^-32 of it below) and 24 for fp32 in the second product, sums are fp32.
+ * Logits are fp32 too: one beyond that is an infinity.  A mean of finite values is finite, however large they are; rows whose sums pass 2^128 on the way take their tile twice as long, and
+ * lose bits of values below 2^-94.
  * What a row does not see does not touch it, infinities and NaN among it.  A row of Q that holds one is NaN or infinite, and so is a row that sees one in a key (but for keys
  * whose logit is -infinity, which weigh nothing) and a channel of a row that sees one in that channel of a value.
  * tokens * q_heads <= 2^27, sequences * heads <= 2^22, |scale| <= 2^127.  Errors: EINVAL, EHIP.
