@@ -128,10 +128,10 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
  * Causal attention over whole prompts: rows offsets[i] .. offsets[i + 1] - 1 are sequence i; its row p, head h, sees keys of rows 0 .. p of the sequence,
  * head h / (q_heads / heads), as above.  offsets: DEVICE, sequences + 1, ascending.  Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Rows outside the sequences
  * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 (down to 2^-21 of the row's largest, and 2^-32 of it below) and 24 for fp32 in the second product, sums are fp32.
- * Logits are fp32 too: one beyond that is an infinity.  A mean of finite values is finite, however large they are; rows whose sums pass 2^128 on the way take their tile twice as long, and
- * lose bits of values below 2^-94.
+ * Logits are fp32 too: one beyond that is an infinity.  A mean of finite values is finite, however large they are; rows whose sums pass 2^128 on the way, or are not finite, take their
+ * tile twice as long, and lose bits of values below 2^-94.
  * What a row does not see does not touch it, infinities and NaN among it.  A row of Q that holds one is NaN or infinite, and so is a row that sees one in a key (but for keys
- * whose logit is -infinity, which weigh nothing) and a channel of a row that sees one in that channel of a value.
+ * whose logit is -infinity, which weigh nothing in 16 bits; in fp32, held in three planes, any infinity makes a NaN) and a channel of a row that sees one in that channel of a value.
  * tokens * q_heads <= 2^27, sequences * heads <= 2^22, |scale| <= 2^127.  Errors: EINVAL, EHIP.
  */
 int tst_attention(const tst_heads_t *Q, const tst_heads_t *K, const tst_heads_t *V, int type, int q_heads, int heads, int head_size, const int32_t *offsets,

@@ -6,8 +6,9 @@ import numpy as np
 import pytest
 import torch
 
+import kv_reference as ref
 import paper_2510_06957_amd as tg
-from test_gpu_attention import (TYPES, World, assert_within, cuda, f32, int32, prompt, prompt_reference, queries, reference_over_cache, rng, same, starts, strided)
+from test_gpu_attention import (PROMPT_CUT, PROMPT_WEIGHT, World, assert_within, cuda, f32, int32, prompt, prompt_reference, queries, reference_over_cache, rng, same, starts, strided)
 
 pytestmark = pytest.mark.gpu
 
@@ -229,3 +230,24 @@ def test_prompts_in_whole_tiles_fp32(lens, q_heads, heads, size):
     want, bound = prompt_reference(f32(q), f32(k), f32(v), at, 1 / math.sqrt(size), "f32", few, rows)
     assert_within(f32_rows(Y, seen)[:, few], want[seen][:, few], bound[seen][:, few], "f32")
     assert torch.equal(tg.tst_attention(q, k, v, int32(at)), Y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lens,q_heads,size", [([90, 40], 4, 64), ([300, 77], 4, 80), ([1217, 64], 64, 64), ([130, 41], 4, 200)])
+def test_prompts_keys_whose_logits_are_minus_infinity(lens, q_heads, size, dtype):
+    """In 16 bits they weigh nothing; in fp32, whose three planes have none for an infinity, rows that see one are NaN."""
+    q, k, v = prompt(lens, q_heads, 2, size, dtype, 70)
+    at, j = starts(lens), 30
+    q[..., 0] = q[..., 0].abs() + 0.5
+    clean = tg.tst_attention(q, k, v, int32(at))
+    k[j, :, 0] = -float("inf")
+    Y = tg.tst_attention(q, k, v, int32(at))
+    assert torch.equal(Y[:j], clean[:j]) and torch.equal(Y[lens[0]:], clean[lens[0]:])
+    if dtype == "f32":
+        assert torch.isnan(Y[j:lens[0]]).all()
+        return
+    rows = np.r_[j, j + 1, np.arange(40, lens[0], 37), lens[0] - 1]
+    for h in (0, q_heads - 1):
+        K, V = (np.delete(f32(t)[:lens[0], h // (q_heads // 2)].astype(np.float64), j, 0) for t in (k, v))
+        want, bound = ref.attention(f32(q)[rows, h].astype(np.float64), K, V, rows, 1 / math.sqrt(size), PROMPT_WEIGHT[dtype], PROMPT_CUT[dtype])
+        assert_within(Y[torch.from_numpy(rows).cuda(), h], want, bound, dtype)
