@@ -9,8 +9,8 @@
 // fp32 operands are cut into three bf16 planes by cutting mantissas off (exact) and six products of planes are summed: all but 2^-24 of a product.
 //
 // Matrix cores and vector units share the time: a weight costs 6 vector instructions (largest, exponential, sum, rounding, operands) beside 256 multiplications of heads of 128.  In bf16 the next 32 keys'
-// logits are therefore made beside the weights of these.  8192 tokens, 32 query and 8 key heads of 128: 549 GFLOP in 548 to 565 us (1.0 PFLOP/s, matrix cores busy 43 % of the cycles; matrix
-// instructions and barriers alone 287 us); heads of 64 335, 4096 tokens of 256 480, 24 prompts of up to 2048 266; 2048 tokens of fp32, 16 query heads, 158.
+// logits are therefore made beside the weights of these.  8192 tokens, 32 query and 8 key heads of 128: 549 GFLOP in 548 to 555 us (1.0 PFLOP/s, matrix cores busy 44 % of the cycles; matrix
+// instructions and barriers alone 287 us); heads of 64 321 to 333, 4096 tokens of 256 487, 24 prompts of up to 2048 264 to 268; 2048 tokens of fp32, 16 query heads, 153.
 #include "attention_internal.h"
 
 #include <cmath>

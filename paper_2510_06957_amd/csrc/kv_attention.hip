@@ -13,8 +13,8 @@
 // The keys of a long sequence are cut into equal chunks, about as long as those of the others: the device finds the length from the lengths of all sequences, so that
 // the workgroups have about as much to do each whatever the batch is, and the host knows how many there are at most.  k_kv_join joins the chunks of a tile of rows.
 //
-// Memory bounds long caches: 131072 tokens of 8 heads of 128 behind one of 32 query heads are 268 MB in 44 us (6.1 TB/s, part of them from the Infinity Cache) and 7 us that join, 64 sequences
-// of up to 8192 tokens 366 MB in 80 us (4.6 TB/s) and 6.7.  A unit's keys and the pages of the one behind it are on their way while the last is worked on; values, which are needed last, are
+// Memory bounds long caches: 131072 tokens of 8 heads of 128 behind one of 32 query heads are 268 MB in 44 us (6.1 TB/s, part of them from the Infinity Cache) and 7.6 us that join, 64 sequences
+// of up to 8192 tokens 366 MB in 81 us (4.5 TB/s) and 7.  A unit's keys and the pages of the one behind it are on their way while the last is worked on; values, which are needed last, are
 // requested first.  Widening codes takes the vector units about as long as the bytes take to come, so two workgroups share a compute unit where registers allow.
 #include "attention_internal.h"
 
