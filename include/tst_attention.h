@@ -94,7 +94,7 @@ typedef struct tst_rotation {
  *   q = clamp(rint(fl(x r)), -127, 127) for new entries;  rint(fl(q fl(old scale / s))) for codes that were there, where s is larger than the old scale
  * (ties to even).  A block of zeros has scale 0; one that has taken in an infinity or a NaN has scale NaN until it is begun anew.  Appending the
  * same rows again changes nothing.  Codes of a block behind its last token are not defined.
- * Two sequences of a call must not append to the same block; where the tables say so all the same, which of them is there is not defined.
+ * A call must not append to a block twice, by two sequences or by one whose table has a page twice; where the tables say so all the same, what is there then is not defined.
  * Q (heads of q_heads) and K come back rotated, rounded to `type`, in q_out [tokens][q_heads][head_size] and k_out [tokens][heads][head_size] where those
  * are not NULL.  q_out needs Q.  Channels that are rotated are NaN in rows whose position is negative or behind what the rotation has.
  * Errors: EINVAL, EHIP.
@@ -114,7 +114,8 @@ int tst_kv_read(const tst_kv_cache_t *cache, const tst_sequences_t *sequences, i
  * with the values that codes stand for; |scale| <= 2^127.  The new tokens have been appended before.  A row that sees nothing is zeros.
  * q_heads: a multiple of the cache's heads, at most 1024 of them, tokens * q_heads <= 2^27; Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Queries keep 22 bits or those of their type
  * relative to the largest of their row.  Products of a weight and its value's scale keep 11 bits in 16-bit types and 22 in fp32, down to 2^-21 (2^-18) of the largest of them that the row
- * sees; those below are off by up to 2^-32 (2^-40) of it.  Logits are fp32: one beyond that is an infinity.
+ * sees; those below are off by up to 2^-32 (2^-40) of it.  Logits are fp32: one beyond that is an infinity; weights are too: below 2^-126 of
+ * the row's largest they are 0.
  * A row of Q that holds an infinity or a NaN is NaN, and so is a row that sees a block whose scale is none.
  * workspace: DEVICE, 256-byte aligned, at least tst_kv_attention_workspace_bytes() of the same cache, sequences and q_heads on the same device (0 may be enough).  It goes by tokens, sequences,
  * heads, q_heads, head_size and the table's width in tokens, columns * page_tokens, not by what the arrays hold: ask again when one of these changes, a wider table among them.
@@ -128,7 +129,7 @@ int tst_kv_attention(const tst_heads_t *Q, int type, int q_heads, const tst_kv_c
  * Causal attention over whole prompts: rows offsets[i] .. offsets[i + 1] - 1 are sequence i; its row p, head h, sees keys of rows 0 .. p of the sequence,
  * head h / (q_heads / heads), as above.  offsets: DEVICE, sequences + 1, ascending.  Y: DEVICE, [tokens][q_heads][head_size] of `type`.  Rows outside the sequences
  * are left as they are.  Weights are rounded to 8 bits for bf16, 11 for fp16 (down to 2^-21 of the row's largest, and 2^-32 of it below) and 24 for fp32 in the second product, sums are fp32.
- * Logits are fp32 too: one beyond that is an infinity.  A mean of finite values is finite, however large they are; rows whose sums pass 2^128 on the way, or are not finite, take their
+ * Logits are fp32 too, one beyond that is an infinity, and weights: below 2^-126 of the row's largest they are 0.  A mean of finite values is finite, however large they are; rows whose sums pass 2^128 on the way, or are not finite, take their
  * tile twice as long, and lose bits of values below 2^-94.
  * What a row does not see does not touch it, infinities and NaN among it.  A row of Q that holds one is NaN or infinite, and so is a row that sees one in a key (but for keys
  * whose logit is -infinity, which weigh nothing in 16 bits; in fp32, held in three planes, any infinity makes a NaN) and a channel of a row that sees one in that channel of a value.
