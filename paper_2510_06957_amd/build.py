@@ -37,7 +37,7 @@ def hipcc() -> str:
 def command(out: pathlib.Path = LIB, extra: list[str] | None = None) -> list[str]:
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared", "-x", "hip",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wall", "-Wno-unused-command-line-argument",
+           "-Wall", "-Wno-unused-command-line-argument", f"-parallel-jobs={min(8, os.cpu_count() or 1)}",
            f"-I{ROOT / 'include'}", f"-I{CSRC}"]
     cmd += [str(CSRC / s) for s in SOURCES]
     cmd += extra or []
